@@ -11,6 +11,7 @@
 #include <vector>
 
 #include "ocean_internal.hpp"
+#include "routed.hpp"
 #include "units.hpp"
 
 using namespace ocean;
@@ -1839,3 +1840,13 @@ const char *ocean_last_error(void) { return g_err.c_str(); }
 int ocean_version(void) { return 100; }
 
 }  // extern "C"
+
+int ocean::set_error(int code, const char *msg) noexcept
+{
+    try {
+        g_err = msg;
+    } catch (...) {
+        g_err.clear();
+    }
+    return code;
+}

@@ -1,0 +1,108 @@
+// C-ABI entry points of the routed products (ocean_routed.h): checks of the arguments, then the launches.
+#include <cstdio>
+
+#include "routed.hpp"
+
+using namespace ocean;
+
+namespace {
+
+int bad(const char *msg) { return set_error(OCEAN_EINVAL, msg); }
+
+int launched(hipError_t e, const char *what)
+{
+    if (e == hipSuccess) return OCEAN_OK;
+    char msg[256];
+    std::snprintf(msg, sizeof msg, "%s: %s", what, hipGetErrorString(e));
+    return set_error(OCEAN_EHIP, msg);
+}
+
+bool known_type(int32_t dtype) { return dtype == OCEAN_F32 || dtype == OCEAN_BF16 || dtype == OCEAN_F16; }
+bool aligned(const void *p, int size) { return reinterpret_cast<uintptr_t>(p) % size == 0; }
+constexpr int64_t MAX_DIM = 1ll << 31;   // rows and widths are below this
+
+// Null where the matrix is fine: base there (if it has elements), aligned to its type, rows apart.
+const char *matrix_fault(const void *p, int64_t rows, int64_t width, int64_t ld, int dtype)
+{
+    if (rows < 0 || rows >= MAX_DIM || width < 0 || width >= MAX_DIM) return "a matrix's size is negative or 2^31 or more";
+    if (ld < width || ld >= (1ll << 40)) return "a row stride is less than the row's width";
+    if (rows > 0 && width > 0 && !p) return "a matrix is null";
+    if (!aligned(p, type_size(dtype))) return "a matrix is not aligned to its type";
+    return nullptr;
+}
+
+const char *routing_fault(const ocean_routing *r, bool need_val, bool need_all)
+{
+    if (!r) return "the routing is null";
+    if (r->tokens < 0 || r->experts < 1 || r->experts > OCEAN_ROUTE_MAX_EXPERTS) return "tokens or experts out of range (experts <= OCEAN_ROUTE_MAX_EXPERTS)";
+    if (r->k < 1 || r->k > OCEAN_ROUTE_MAX_K || r->k > r->experts) return "k must be 1 to min(experts, OCEAN_ROUTE_MAX_K)";
+    if (r->tokens > (1ll << 28) || r->tokens * r->k >= MAX_DIM) return "tokens * k must be below 2^31 (and tokens at most 2^28)";
+    if (!r->row_ptr) return "row_ptr is null";
+    if (r->tokens > 0 && need_val && !r->val) return "val is null";
+    if (need_all && (!r->expert_ptr || (r->tokens > 0 && (!r->col_idx || !r->token || !r->slot)))) return "an array of the routing is null";
+    return nullptr;
+}
+
+#define REFUSE(expr)                                   \
+    do {                                               \
+        if (const char *why__ = (expr)) return bad(why__); \
+    } while (0)
+
+}  // namespace
+
+extern "C" {
+
+size_t ocean_route_workspace(int64_t tokens, int64_t experts, int32_t k)
+{
+    if (tokens < 0 || experts < 1 || k < 1 || tokens > (1ll << 28) || experts > OCEAN_ROUTE_MAX_EXPERTS || k > OCEAN_ROUTE_MAX_K) return 0;
+    return route_workspace(tokens, experts, k);
+}
+
+int ocean_route(const void *logits, int32_t dtype, int64_t ld, int32_t normalize, const ocean_routing *out, void *workspace,
+                size_t workspace_bytes, ocean_stream_t stream)
+{
+    if (!known_type(dtype)) return bad("dtype must be OCEAN_F32, OCEAN_BF16 or OCEAN_F16");
+    REFUSE(routing_fault(out, true, true));
+    REFUSE(matrix_fault(logits, out->tokens, out->experts, ld, dtype));
+    if (!workspace || !aligned(workspace, 256) || workspace_bytes < route_workspace(out->tokens, out->experts, out->k))
+        return bad("workspace is null, not aligned to 256 bytes or smaller than ocean_route_workspace");
+    return launched(launch_route(logits, dtype, ld, normalize != 0, *out, workspace, static_cast<hipStream_t>(stream)), "ocean_route");
+}
+
+int ocean_route_backward(const ocean_routing *r, const float *dval, const void *logits, int32_t dtype, int64_t ld, int32_t normalize,
+                         void *dlogits, int64_t ld_dlogits, ocean_stream_t stream)
+{
+    if (!known_type(dtype)) return bad("dtype must be OCEAN_F32, OCEAN_BF16 or OCEAN_F16");
+    REFUSE(routing_fault(r, true, false));
+    if (r->tokens > 0 && (!r->col_idx || !dval)) return bad("col_idx or dval is null");
+    if (!normalize) REFUSE(matrix_fault(logits, r->tokens, r->experts, ld, dtype));
+    REFUSE(matrix_fault(dlogits, r->tokens, r->experts, ld_dlogits, dtype));
+    return launched(launch_route_backward(*r, dval, logits, dtype, ld, normalize != 0, dlogits, ld_dlogits, static_cast<hipStream_t>(stream)),
+                    "ocean_route_backward");
+}
+
+int ocean_combine(const ocean_routing *r, const void *y, int32_t dtype, int64_t width, int64_t ld_y, void *out, int64_t ld_out,
+                  ocean_stream_t stream)
+{
+    if (!known_type(dtype)) return bad("dtype must be OCEAN_F32, OCEAN_BF16 or OCEAN_F16");
+    REFUSE(routing_fault(r, false, false));
+    if (r->tokens > 0 && !r->slot) return bad("slot is null");
+    REFUSE(matrix_fault(y, r->tokens * r->k, width, ld_y, dtype));
+    REFUSE(matrix_fault(out, r->tokens, width, ld_out, dtype));
+    return launched(launch_combine(*r, y, dtype, width, ld_y, out, ld_out, static_cast<hipStream_t>(stream)), "ocean_combine");
+}
+
+int ocean_combine_backward(const ocean_routing *r, const void *dout, int64_t ld_dout, const void *y, int64_t ld_y, int32_t dtype,
+                           int64_t width, void *dy, int64_t ld_dy, float *dval, ocean_stream_t stream)
+{
+    if (!known_type(dtype)) return bad("dtype must be OCEAN_F32, OCEAN_BF16 or OCEAN_F16");
+    REFUSE(routing_fault(r, false, false));
+    if (r->tokens > 0 && !r->slot) return bad("slot is null");
+    REFUSE(matrix_fault(dout, r->tokens, width, ld_dout, dtype));
+    if (dval) REFUSE(matrix_fault(y, r->tokens * r->k, width, ld_y, dtype));
+    REFUSE(matrix_fault(dy, r->tokens * r->k, width, ld_dy, dtype));
+    return launched(launch_combine_backward(*r, dout, ld_dout, y, ld_y, dtype, width, dy, ld_dy, dval, static_cast<hipStream_t>(stream)),
+                    "ocean_combine_backward");
+}
+
+}  // extern "C"

@@ -1,0 +1,240 @@
+"""Products in which every row chooses its matrix: ctypes binding of include/ocean_routed.h.
+
+A routing matrix (tokens x experts, k entries a row) is made from logits, applied to the rows that the experts gave, and
+differentiated; the ragged groups of rows that it forms are multiplied with their experts' weights; and rows that each name a
+low-rank adapter are projected with it.  Every step runs in the HIP library, on the current stream or the one given; outputs and
+workspaces are torch tensors of that stream, nothing synchronises, and calls can be captured into a graph.  There is no CPU fallback.
+
+A training step of an experts' block, for x [T, D], w1 [E, F, D], w2 [E, D, F]:
+
+    r = route(logits, k)                                            # R, and its entries in the order of the experts
+    h = grouped_matmul(x, w1, r.expert_ptr, rows=r.token)           # [T*k, F], rows gathered from x
+    y = grouped_matmul(act(h), w2, r.expert_ptr)                    # [T*k, D]
+    out = combine(y, r)                                             # [T, D]
+    dy, dval = combine_backward(dout, y, r)
+    dh = grouped_matmul(dy, w2, r.expert_ptr, transposed=True)      # w2 the other way round
+    dw2 = grouped_weight_grad(dy, act(h), r.expert_ptr)
+    dw1 = grouped_weight_grad(dact(dh), x, r.expert_ptr, rows=r.token)
+    dx = combine(grouped_matmul(dact(dh), w1, r.expert_ptr, transposed=True), r, weighted=False)
+    dlogits = route_backward(r, dval, logits)
+"""
+from __future__ import annotations
+
+import ctypes as C
+from contextlib import nullcontext
+from dataclasses import dataclass
+
+from . import binding as _b
+from .binding import DeviceCSR, OceanError  # noqa: F401
+
+F32, BF16, F16 = 1, 2, 3
+MAX_EXPERTS, MAX_K = 1024, 64
+MAX_RANK, MAX_ADAPTERS = 256, 8192
+
+
+class ocean_routing(C.Structure):
+    _fields_ = [("tokens", C.c_int64), ("experts", C.c_int64), ("k", C.c_int32), ("reserved", C.c_int32), ("row_ptr", C.c_void_p),
+                ("col_idx", C.c_void_p), ("val", C.c_void_p), ("expert_ptr", C.c_void_p), ("token", C.c_void_p), ("slot", C.c_void_p)]
+
+
+_lib = None
+
+
+def load():
+    """The HIP library with the argument types of ocean_routed.h set."""
+    global _lib
+    if _lib is not None:
+        return _lib
+    lib = _b.load()
+    P, vp, i64, i32, size = C.POINTER, C.c_void_p, C.c_int64, C.c_int32, C.c_size_t
+    lib.ocean_route_workspace.argtypes = [i64, i64, i32]
+    lib.ocean_route_workspace.restype = size
+    lib.ocean_route.argtypes = [vp, i32, i64, i32, P(ocean_routing), vp, size, vp]
+    lib.ocean_route_backward.argtypes = [P(ocean_routing), vp, vp, i32, i64, i32, vp, i64, vp]
+    lib.ocean_combine.argtypes = [P(ocean_routing), vp, i32, i64, i64, vp, i64, vp]
+    lib.ocean_combine_backward.argtypes = [P(ocean_routing), vp, i64, vp, i64, i32, i64, vp, i64, vp, vp]
+    for name in ("ocean_route", "ocean_route_backward", "ocean_combine", "ocean_combine_backward"):
+        getattr(lib, name).restype = C.c_int
+    _lib = lib
+    return lib
+
+
+@dataclass
+class Routing:
+    """A routing matrix in CSR (row_ptr int64 [tokens+1], col_idx int32, val float32 or None) and in the order of its columns
+    (expert_ptr int64 [experts+1], token int32, slot int32).  The four entry arrays have tokens * k places; those behind the last
+    entry hold -1 (val: 0)."""
+    tokens: int
+    experts: int
+    k: int
+    row_ptr: "object"
+    col_idx: "object"
+    val: "object"
+    expert_ptr: "object"
+    token: "object"
+    slot: "object"
+
+    def csr(self) -> DeviceCSR:
+        """The matrix as an operand of binding.spgemm; reads the number of its entries back."""
+        n = int(self.row_ptr[-1])
+        return DeviceCSR(self.tokens, self.experts, self.row_ptr, self.col_idx[:n], self.val[:n], [self])
+
+    def _struct(self, weighted=True):
+        return ocean_routing(self.tokens, self.experts, self.k, 0, *(_ptr(t) for t in (
+            self.row_ptr, self.col_idx, self.val if weighted else None, self.expert_ptr, self.token, self.slot)))
+
+    def _check(self, device):
+        """The lists are contiguous, of their types, of their sizes and on `device`."""
+        import torch
+        n = self.tokens * self.k
+        for name, dtype, size in (("row_ptr", torch.int64, self.tokens + 1), ("col_idx", torch.int32, n), ("val", torch.float32, n),
+                                  ("expert_ptr", torch.int64, self.experts + 1), ("token", torch.int32, n), ("slot", torch.int32, n)):
+            t = getattr(self, name)
+            if t is not None or name != "val":
+                _vector(t, name, dtype, size, device)
+        return [t for t in (self.row_ptr, self.col_idx, self.val, self.expert_ptr, self.token, self.slot) if t is not None]
+
+
+# ---------------------------------------------------------------- arguments
+_codes = {}
+
+
+def _code(dtype) -> int:
+    if not _codes:
+        torch = _b._torch()
+        _codes.update({torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16})
+    code = _codes.get(dtype)
+    if code is None:
+        raise TypeError(f"{dtype}: matrices are float32, bfloat16 or float16")
+    return code
+
+
+def _ptr(t):
+    return None if t is None or t.numel() == 0 else t.data_ptr()
+
+
+def _vector(t, name, dtype, size, device):
+    if t.dtype != dtype or t.dim() != 1 or t.shape[0] != size or t.device != device or (size > 1 and t.stride(0) != 1):
+        raise ValueError(f"{name} must be a contiguous {dtype} vector of {size} on {device}, not {t.dtype} {tuple(t.shape)} on {t.device}")
+
+
+def _matrix(t, name, rows=None, width=None, like=None):
+    """Row stride of a matrix whose rows are contiguous; rows / width / like: what it has to have."""
+    if t.dim() != 2 or (rows is not None and t.shape[0] != rows) or (width is not None and t.shape[1] != width):
+        raise ValueError(f"{name} must be [{'rows' if rows is None else rows}, {'width' if width is None else width}], not {tuple(t.shape)}")
+    if like is not None and (t.dtype != like.dtype or t.device != like.device):
+        raise ValueError(f"{name} is {t.dtype} on {t.device}, not {like.dtype} on {like.device}")
+    n, w = t.shape
+    if w > 1 and t.stride(1) != 1:
+        raise ValueError(f"{name}: the elements of a row must be adjacent")
+    if n <= 1:
+        return max(w, 1)
+    if t.stride(0) < w:
+        raise ValueError(f"{name}: rows overlap")
+    return max(t.stride(0), 1)
+
+
+class _Call:
+    """One call's device and stream: tensors made inside belong to the stream; tensors that the call reads and that another stream
+    made are kept until it is done with them."""
+
+    def __init__(self, device, stream, *tensors):
+        torch = _b._torch()
+        if device.type != "cuda":
+            raise ValueError(f"tensors must be on a GPU, not {device}")
+        current = torch.cuda.current_stream(device)
+        self.stream = current if stream is None else stream
+        self.ptr = int(self.stream.cuda_stream)
+        other = self.stream != current
+        self.scope = torch.cuda.stream(self.stream) if other else _b._on(device)
+        if other:
+            for t in tensors:
+                if t is not None:
+                    t.record_stream(self.stream)
+
+    def __enter__(self):
+        self.scope.__enter__()
+        return self.ptr
+
+    def __exit__(self, *e):
+        return self.scope.__exit__(*e)
+
+
+def _output(out, shape, like, name="out"):
+    """The caller's output, checked, or a new one."""
+    if out is None:
+        return like.new_empty(shape)
+    if tuple(out.shape) != tuple(shape):
+        raise ValueError(f"{name} must be {tuple(shape)}, not {tuple(out.shape)}")
+    return out
+
+
+# ---------------------------------------------------------------- routing
+def route(logits, k: int, *, normalize: bool = True, stream=None) -> Routing:
+    """The routing matrix of logits [tokens, experts]: each row's k largest, ties to the lowest columns; NaN, -inf and the type's
+    lowest value are never taken.  Weights: softmax over the entries taken, or (normalize=False) over all that may be."""
+    import torch
+    lib = load()
+    ld = _matrix(logits, "logits")
+    code = _code(logits.dtype)
+    T, E = logits.shape
+    if not 1 <= k <= min(E, MAX_K) or E > MAX_EXPERTS:
+        raise ValueError(f"k must be 1 to min(experts, {MAX_K}) and experts at most {MAX_EXPERTS}, not {k} of {E}")
+    dev = logits.device
+    with _Call(dev, stream, logits) as s:
+        n = T * k
+        r = Routing(T, E, k, torch.empty(T + 1, dtype=torch.int64, device=dev), torch.empty(n, dtype=torch.int32, device=dev),
+                    torch.empty(n, dtype=torch.float32, device=dev), torch.empty(E + 1, dtype=torch.int64, device=dev),
+                    torch.empty(n, dtype=torch.int32, device=dev), torch.empty(n, dtype=torch.int32, device=dev))
+        nbytes = lib.ocean_route_workspace(T, E, k)
+        space = torch.empty(nbytes, dtype=torch.uint8, device=dev)
+        c = r._struct()
+        _b._check(lib.ocean_route(_ptr(logits), code, ld, int(normalize), C.byref(c), space.data_ptr(), nbytes, s))
+    return r
+
+
+def route_backward(routing: Routing, dval, logits, *, normalize: bool = True, out=None, stream=None):
+    """Gradient of the logits from dval [tokens*k], that of the weights in the order of routing.val."""
+    import torch
+    lib = load()
+    ld = _matrix(logits, "logits", routing.tokens, routing.experts)
+    lists = routing._check(logits.device)
+    if routing.val is None:
+        raise ValueError("the routing has no weights")
+    _vector(dval, "dval", torch.float32, routing.tokens * routing.k, logits.device)
+    with _Call(logits.device, stream, logits, dval, out, *lists) as s:
+        out = _output(out, logits.shape, logits)
+        ldo = _matrix(out, "out", like=logits)
+        c = routing._struct()
+        _b._check(lib.ocean_route_backward(C.byref(c), _ptr(dval), _ptr(logits), _code(logits.dtype), ld, int(normalize), _ptr(out), ldo, s))
+    return out
+
+
+def combine(y, routing: Routing, *, weighted: bool = True, out=None, stream=None):
+    """out[t] = sum of val[p] * y[slot[p]] over the entries p of row t (weighted=False, or a routing without val: of y[slot[p]])."""
+    lib = load()
+    ldy = _matrix(y, "y", routing.tokens * routing.k)
+    lists = routing._check(y.device)
+    with _Call(y.device, stream, y, out, *lists) as s:
+        out = _output(out, (routing.tokens, y.shape[1]), y)
+        ldo = _matrix(out, "out", like=y)
+        c = routing._struct(weighted)
+        _b._check(lib.ocean_combine(C.byref(c), _ptr(y), _code(y.dtype), y.shape[1], ldy, _ptr(out), ldo, s))
+    return out
+
+
+def combine_backward(dout, y, routing: Routing, *, weighted: bool = True, stream=None):
+    """(dy, dval): gradients of y and of val.  y=None: dval is not wanted, and None."""
+    import torch
+    lib = load()
+    ldo = _matrix(dout, "dout", routing.tokens)
+    width, n = dout.shape[1], routing.tokens * routing.k
+    ldy = _matrix(y, "y", n, width, like=dout) if y is not None else width
+    lists = routing._check(dout.device)
+    with _Call(dout.device, stream, dout, y, *lists) as s:
+        dy = dout.new_empty((n, width))
+        dval = torch.empty(n, dtype=torch.float32, device=dout.device) if y is not None else None
+        c = routing._struct(weighted)
+        _b._check(lib.ocean_combine_backward(C.byref(c), _ptr(dout), ldo, _ptr(y), ldy, _code(dout.dtype), width, _ptr(dy), max(width, 1),
+                                             _ptr(dval), s))
+    return dy, dval
