@@ -63,4 +63,10 @@ hipError_t launch_combine(const ocean_routing &r, const void *y, int dtype, int6
 hipError_t launch_combine_backward(const ocean_routing &r, const void *dout, int64_t ldo, const void *y, int64_t ldy, int dtype,
                                    int64_t width, void *dy, int64_t lddy, float *dval, hipStream_t s);
 
+// grouped.hip
+hipError_t launch_grouped_matmul(const ocean_groups &g, int dtype, int64_t inner, int64_t outer, const void *x, int64_t ldx, const void *w,
+                                 int64_t ldw, int64_t stride, bool transposed, void *y, int64_t ldy, hipStream_t s);
+hipError_t launch_grouped_weight_grad(const ocean_groups &g, int dtype, int64_t inner, int64_t outer, const void *dy, int64_t lddy, const void *x,
+                                      int64_t ldx, void *dw, int64_t lddw, int64_t stride, bool transposed, hipStream_t s);
+
 }  // namespace ocean

@@ -43,6 +43,25 @@ const char *routing_fault(const ocean_routing *r, bool need_val, bool need_all)
     return nullptr;
 }
 
+const char *groups_fault(const ocean_groups *g)
+{
+    if (!g) return "the groups are null";
+    if (g->rows < 0 || g->rows >= MAX_DIM || g->experts < 0 || g->experts > (1 << 20) || g->x_rows < 0 || g->x_rows >= MAX_DIM)
+        return "rows, experts or x_rows out of range";
+    if (!g->group_ptr) return "group_ptr is null";
+    if (!g->row_index && g->rows > 0 && g->x_rows != g->rows) return "without row_index, x_rows must be rows";
+    return nullptr;
+}
+
+// Null where the matrices of the groups are fine, each rows x width and `stride` elements from the next.
+const char *matrices_fault(const void *p, int64_t count, int64_t stride, int64_t rows, int64_t width, int64_t ld, int dtype, bool written)
+{
+    if (const char *why = matrix_fault(p, count > 0 ? rows : 0, width, ld, dtype)) return why;
+    if (stride < 0 || stride >= (1ll << 44)) return "the stride between matrices is out of range";
+    if (written && count > 1 && rows > 0 && stride < (rows - 1) * ld + width) return "matrices that are written overlap";
+    return nullptr;
+}
+
 #define REFUSE(expr)                                   \
     do {                                               \
         if (const char *why__ = (expr)) return bad(why__); \
@@ -103,6 +122,31 @@ int ocean_combine_backward(const ocean_routing *r, const void *dout, int64_t ld_
     REFUSE(matrix_fault(dy, r->tokens * r->k, width, ld_dy, dtype));
     return launched(launch_combine_backward(*r, dout, ld_dout, y, ld_y, dtype, width, dy, ld_dy, dval, static_cast<hipStream_t>(stream)),
                     "ocean_combine_backward");
+}
+
+int ocean_grouped_matmul(const ocean_groups *g, int32_t dtype, int64_t inner, int64_t outer, const void *x, int64_t ld_x, const void *w,
+                         int64_t ld_w, int64_t stride_w, int32_t transposed, void *y, int64_t ld_y, ocean_stream_t stream)
+{
+    if (!known_type(dtype)) return bad("dtype must be OCEAN_F32, OCEAN_BF16 or OCEAN_F16");
+    REFUSE(groups_fault(g));
+    REFUSE(matrix_fault(x, g->x_rows, inner, ld_x, dtype));
+    REFUSE(matrices_fault(w, g->experts, stride_w, transposed ? inner : outer, transposed ? outer : inner, ld_w, dtype, false));
+    REFUSE(matrix_fault(y, g->rows, outer, ld_y, dtype));
+    return launched(launch_grouped_matmul(*g, dtype, inner, outer, x, ld_x, w, ld_w, stride_w, transposed != 0, y, ld_y,
+                                          static_cast<hipStream_t>(stream)), "ocean_grouped_matmul");
+}
+
+int ocean_grouped_weight_grad(const ocean_groups *g, int32_t dtype, int64_t inner, int64_t outer, const void *dy, int64_t ld_dy,
+                              const void *x, int64_t ld_x, void *dw, int64_t ld_dw, int64_t stride_dw, int32_t transposed,
+                              ocean_stream_t stream)
+{
+    if (!known_type(dtype)) return bad("dtype must be OCEAN_F32, OCEAN_BF16 or OCEAN_F16");
+    REFUSE(groups_fault(g));
+    REFUSE(matrix_fault(dy, g->rows, outer, ld_dy, dtype));
+    REFUSE(matrix_fault(x, g->x_rows, inner, ld_x, dtype));
+    REFUSE(matrices_fault(dw, g->experts, stride_dw, transposed ? inner : outer, transposed ? outer : inner, ld_dw, dtype, true));
+    return launched(launch_grouped_weight_grad(*g, dtype, inner, outer, dy, ld_dy, x, ld_x, dw, ld_dw, stride_dw, transposed != 0,
+                                               static_cast<hipStream_t>(stream)), "ocean_grouped_weight_grad");
 }
 
 }  // extern "C"

@@ -37,6 +37,10 @@ class ocean_routing(C.Structure):
                 ("col_idx", C.c_void_p), ("val", C.c_void_p), ("expert_ptr", C.c_void_p), ("token", C.c_void_p), ("slot", C.c_void_p)]
 
 
+class ocean_groups(C.Structure):
+    _fields_ = [("rows", C.c_int64), ("experts", C.c_int64), ("group_ptr", C.c_void_p), ("row_index", C.c_void_p), ("x_rows", C.c_int64)]
+
+
 _lib = None
 
 
@@ -53,7 +57,10 @@ def load():
     lib.ocean_route_backward.argtypes = [P(ocean_routing), vp, vp, i32, i64, i32, vp, i64, vp]
     lib.ocean_combine.argtypes = [P(ocean_routing), vp, i32, i64, i64, vp, i64, vp]
     lib.ocean_combine_backward.argtypes = [P(ocean_routing), vp, i64, vp, i64, i32, i64, vp, i64, vp, vp]
-    for name in ("ocean_route", "ocean_route_backward", "ocean_combine", "ocean_combine_backward"):
+    lib.ocean_grouped_matmul.argtypes = [P(ocean_groups), i32, i64, i64, vp, i64, vp, i64, i64, i32, vp, i64, vp]
+    lib.ocean_grouped_weight_grad.argtypes = [P(ocean_groups), i32, i64, i64, vp, i64, vp, i64, vp, i64, i64, i32, vp]
+    for name in ("ocean_route", "ocean_route_backward", "ocean_combine", "ocean_combine_backward", "ocean_grouped_matmul",
+                 "ocean_grouped_weight_grad"):
         getattr(lib, name).restype = C.c_int
     _lib = lib
     return lib
@@ -238,3 +245,64 @@ def combine_backward(dout, y, routing: Routing, *, weighted: bool = True, stream
         _b._check(lib.ocean_combine_backward(C.byref(c), _ptr(dout), ldo, _ptr(y), ldy, _code(dout.dtype), width, _ptr(dy), max(width, 1),
                                              _ptr(dval), s))
     return dy, dval
+
+
+# ---------------------------------------------------------------- grouped products
+def _matrices(w, name, shape=None, like=None):
+    """(row stride, stride from one matrix to the next) of matrices whose rows are contiguous."""
+    if w.dim() != 3 or (shape is not None and tuple(w.shape) != tuple(shape)):
+        raise ValueError(f"{name} must be [experts, rows, width]{'' if shape is None else f' = {tuple(shape)}'}, not {tuple(w.shape)}")
+    if like is not None and (w.dtype != like.dtype or w.device != like.device):
+        raise ValueError(f"{name} is {w.dtype} on {w.device}, not {like.dtype} on {like.device}")
+    n, rows, width = w.shape
+    if width > 1 and w.stride(2) != 1:
+        raise ValueError(f"{name}: the elements of a row must be adjacent")
+    if rows > 1 and w.stride(1) < width:
+        raise ValueError(f"{name}: rows overlap")
+    return w.stride(1) if rows > 1 else max(width, 1), w.stride(0) if n > 1 else 0
+
+
+def _groups(x, expert_ptr, rows):
+    import torch
+    n = x.shape[0] if rows is None else rows.shape[0]
+    experts = expert_ptr.numel() - 1
+    _vector(expert_ptr, "expert_ptr", torch.int64, max(experts, 0) + 1, x.device)
+    if rows is not None:
+        _vector(rows, "rows", torch.int32, n, x.device)
+    return ocean_groups(n, experts, expert_ptr.data_ptr(), _ptr(rows), x.shape[0])
+
+
+def grouped_matmul(x, w, expert_ptr, *, rows=None, transposed: bool = False, out=None, stream=None):
+    """y[s] = x[rows[s]] @ w[e].T for the slots s of expert e, expert_ptr[e] .. expert_ptr[e+1]-1 (int64 [experts+1]); w [experts, outer, inner].
+    transposed: w is [experts, inner, outer] and y[s] = x[rows[s]] @ w[e].  rows (int32) None: slot s is row s of x; a row number
+    outside x stands for zeros.  Slots of no expert give zeros.  The gradient of x's rows is grouped_matmul(dy, w, expert_ptr,
+    transposed=not transposed)."""
+    lib = load()
+    ldx = _matrix(x, "x")
+    code = _code(x.dtype)
+    ldw, stride = _matrices(w, "w", like=x)
+    g = _groups(x, expert_ptr, rows)
+    outer, inner = (w.shape[2], w.shape[1]) if transposed else (w.shape[1], w.shape[2])
+    if w.shape[0] != g.experts or inner != x.shape[1]:
+        raise ValueError(f"w is {tuple(w.shape)}{' (transposed)' if transposed else ''}: not {g.experts} matrices for rows of {x.shape[1]}")
+    with _Call(x.device, stream, x, w, expert_ptr, rows, out) as s:
+        out = _output(out, (g.rows, outer), x)
+        ldo = _matrix(out, "out", like=x)
+        _b._check(lib.ocean_grouped_matmul(C.byref(g), code, inner, outer, _ptr(x), ldx, _ptr(w), ldw, stride, int(transposed), _ptr(out), ldo, s))
+    return out
+
+
+def grouped_weight_grad(dy, x, expert_ptr, *, rows=None, transposed: bool = False, out=None, stream=None):
+    """Gradient of grouped_matmul's w: the sum over the slots s of expert e of dy[s]^T x[rows[s]], [experts, outer, inner] (transposed:
+    [experts, inner, outer]); zeros for an expert without slots."""
+    lib = load()
+    ldx = _matrix(x, "x")
+    code = _code(x.dtype)
+    g = _groups(x, expert_ptr, rows)
+    ldd = _matrix(dy, "dy", g.rows, like=x)
+    inner, outer = x.shape[1], dy.shape[1]
+    with _Call(x.device, stream, x, dy, expert_ptr, rows, out) as s:
+        out = _output(out, (g.experts, inner, outer) if transposed else (g.experts, outer, inner), x)
+        ldo, stride = _matrices(out, "out", like=x)
+        _b._check(lib.ocean_grouped_weight_grad(C.byref(g), code, inner, outer, _ptr(dy), ldd, _ptr(x), ldx, _ptr(out), ldo, stride, int(transposed), s))
+    return out
