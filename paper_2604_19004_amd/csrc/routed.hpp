@@ -69,4 +69,9 @@ hipError_t launch_grouped_matmul(const ocean_groups &g, int dtype, int64_t inner
 hipError_t launch_grouped_weight_grad(const ocean_groups &g, int dtype, int64_t inner, int64_t outer, const void *dy, int64_t lddy, const void *x,
                                       int64_t ldx, void *dw, int64_t lddw, int64_t stride, bool transposed, hipStream_t s);
 
+// adapter.hip
+size_t adapter_workspace(int64_t rows, int64_t inner, int64_t outer, int64_t adapters, int64_t rank, int dtype);
+hipError_t launch_adapter(const ocean_adapters &l, const int32_t *ids, int dtype, int64_t rows, int64_t inner, int64_t outer, const void *x,
+                          int64_t ldx, const void *w, int64_t ldw, void *y, int64_t ldy, void *workspace, hipStream_t s);
+
 }  // namespace ocean

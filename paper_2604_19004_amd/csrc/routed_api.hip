@@ -149,4 +149,32 @@ int ocean_grouped_weight_grad(const ocean_groups *g, int32_t dtype, int64_t inne
                                                static_cast<hipStream_t>(stream)), "ocean_grouped_weight_grad");
 }
 
+size_t ocean_adapter_workspace(int64_t rows, int64_t inner, int64_t outer, int64_t adapters, int64_t rank, int32_t dtype)
+{
+    if (rows < 0 || rows >= MAX_DIM || inner < 0 || inner >= MAX_DIM || outer < 0 || outer >= MAX_DIM || adapters < 0 || adapters > OCEAN_ADAPTER_MAX ||
+        rank < 0 || rank > OCEAN_ADAPTER_MAX_RANK || !known_type(dtype))
+        return 0;
+    return adapter_workspace(rows, inner, outer, adapters, rank, dtype);
+}
+
+int ocean_adapter_matmul(const ocean_adapters *l, const int32_t *ids, int32_t dtype, int64_t rows, int64_t inner, int64_t outer,
+                         const void *x, int64_t ld_x, const void *w, int64_t ld_w, void *y, int64_t ld_y, void *workspace,
+                         size_t workspace_bytes, ocean_stream_t stream)
+{
+    if (!known_type(dtype)) return bad("dtype must be OCEAN_F32, OCEAN_BF16 or OCEAN_F16");
+    if (!l) return bad("the adapters are null");
+    if (l->adapters < 0 || l->adapters > OCEAN_ADAPTER_MAX || l->rank < 0 || l->rank > OCEAN_ADAPTER_MAX_RANK)
+        return bad("adapters or rank out of range (OCEAN_ADAPTER_MAX, OCEAN_ADAPTER_MAX_RANK)");
+    REFUSE(matrix_fault(x, rows, inner, ld_x, dtype));
+    REFUSE(matrix_fault(w, outer, inner, ld_w, dtype));
+    REFUSE(matrix_fault(y, rows, outer, ld_y, dtype));
+    REFUSE(matrices_fault(l->a, l->adapters, l->stride_a, l->rank, inner, l->ld_a, dtype, false));
+    REFUSE(matrices_fault(l->b, l->adapters, l->stride_b, outer, l->rank, l->ld_b, dtype, false));
+    if (rows > 0 && !ids) return bad("ids is null");
+    if (!workspace || !aligned(workspace, 256) || workspace_bytes < adapter_workspace(rows, inner, outer, l->adapters, l->rank, dtype))
+        return bad("workspace is null, not aligned to 256 bytes or smaller than ocean_adapter_workspace");
+    return launched(launch_adapter(*l, ids, dtype, rows, inner, outer, x, ld_x, w, ld_w, y, ld_y, workspace, static_cast<hipStream_t>(stream)),
+                    "ocean_adapter_matmul");
+}
+
 }  // extern "C"

@@ -41,6 +41,11 @@ class ocean_groups(C.Structure):
     _fields_ = [("rows", C.c_int64), ("experts", C.c_int64), ("group_ptr", C.c_void_p), ("row_index", C.c_void_p), ("x_rows", C.c_int64)]
 
 
+class ocean_adapters(C.Structure):
+    _fields_ = [("adapters", C.c_int64), ("rank", C.c_int64), ("a", C.c_void_p), ("ld_a", C.c_int64), ("stride_a", C.c_int64),
+                ("b", C.c_void_p), ("ld_b", C.c_int64), ("stride_b", C.c_int64), ("ranks", C.c_void_p), ("scale", C.c_void_p)]
+
+
 _lib = None
 
 
@@ -59,8 +64,11 @@ def load():
     lib.ocean_combine_backward.argtypes = [P(ocean_routing), vp, i64, vp, i64, i32, i64, vp, i64, vp, vp]
     lib.ocean_grouped_matmul.argtypes = [P(ocean_groups), i32, i64, i64, vp, i64, vp, i64, i64, i32, vp, i64, vp]
     lib.ocean_grouped_weight_grad.argtypes = [P(ocean_groups), i32, i64, i64, vp, i64, vp, i64, vp, i64, i64, i32, vp]
+    lib.ocean_adapter_workspace.argtypes = [i64, i64, i64, i64, i64, i32]
+    lib.ocean_adapter_workspace.restype = size
+    lib.ocean_adapter_matmul.argtypes = [P(ocean_adapters), vp, i32, i64, i64, i64, vp, i64, vp, i64, vp, i64, vp, size, vp]
     for name in ("ocean_route", "ocean_route_backward", "ocean_combine", "ocean_combine_backward", "ocean_grouped_matmul",
-                 "ocean_grouped_weight_grad"):
+                 "ocean_grouped_weight_grad", "ocean_adapter_matmul"):
         getattr(lib, name).restype = C.c_int
     _lib = lib
     return lib
@@ -305,4 +313,39 @@ def grouped_weight_grad(dy, x, expert_ptr, *, rows=None, transposed: bool = Fals
         out = _output(out, (g.experts, inner, outer) if transposed else (g.experts, outer, inner), x)
         ldo, stride = _matrices(out, "out", like=x)
         _b._check(lib.ocean_grouped_weight_grad(C.byref(g), code, inner, outer, _ptr(dy), ldd, _ptr(x), ldx, _ptr(out), ldo, stride, int(transposed), s))
+    return out
+
+
+# ---------------------------------------------------------------- adapters
+def adapter_matmul(x, w, a, b, ids, *, ranks=None, scale=None, out=None, stream=None):
+    """y[m] = x[m] @ w.T + scale[i] * (x[m] @ a[i].T) @ b[i].T with i = ids[m]; x [rows, inner], w [outer, inner], a [adapters, rank, inner],
+    b [adapters, outer, rank], ids int32 [rows] (outside 0 .. adapters-1: no adapter).  ranks (int32 [adapters]): only the first ranks[i]
+    rows of a[i] and columns of b[i] are used.  scale: float32 [adapters], None for 1."""
+    import torch
+    lib = load()
+    ldx = _matrix(x, "x")
+    code = _code(x.dtype)
+    (rows, inner), dev = x.shape, x.device
+    ldw = _matrix(w, "w", width=inner, like=x)
+    outer = w.shape[0]
+    if a.dim() != 3 or b.dim() != 3:
+        raise ValueError(f"a must be [adapters, rank, inner] and b [adapters, outer, rank], not {tuple(a.shape)} and {tuple(b.shape)}")
+    adapters, rank = a.shape[:2]
+    if adapters > MAX_ADAPTERS or rank > MAX_RANK:
+        raise ValueError(f"at most {MAX_ADAPTERS} adapters of rank {MAX_RANK}, not {adapters} of {rank}")
+    lda, sa = _matrices(a, "a", (adapters, rank, inner), x)
+    ldb, sb = _matrices(b, "b", (adapters, outer, rank), x)
+    _vector(ids, "ids", torch.int32, rows, dev)
+    if ranks is not None:
+        _vector(ranks, "ranks", torch.int32, adapters, dev)
+    if scale is not None:
+        _vector(scale, "scale", torch.float32, adapters, dev)
+    with _Call(dev, stream, x, w, a, b, ids, ranks, scale, out) as s:
+        out = _output(out, (rows, outer), x)
+        ldo = _matrix(out, "out", like=x)
+        nbytes = lib.ocean_adapter_workspace(rows, inner, outer, adapters, rank, code)
+        space = torch.empty(nbytes, dtype=torch.uint8, device=dev)
+        c = ocean_adapters(adapters, rank, _ptr(a), lda, sa, _ptr(b), ldb, sb, _ptr(ranks), _ptr(scale))
+        _b._check(lib.ocean_adapter_matmul(C.byref(c), _ptr(ids), code, rows, inner, outer, _ptr(x), ldx, _ptr(w), ldw, _ptr(out), ldo,
+                                           space.data_ptr(), nbytes, s))
     return out
