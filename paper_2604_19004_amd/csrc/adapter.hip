@@ -140,6 +140,7 @@ hipError_t launch_adapter(const ocean_adapters &l, const int32_t *ids, int dtype
     const int size = type_size(dtype), e = 16 / size, rank = (int)l.rank;
     const bool none = l.adapters == 0 || rank == 0 || inner == 0;
     const int64_t adapters = none ? 0 : l.adapters;
+    const bool x_fits = offsets_fit(std::max<int64_t>(rows, 256), ldx, size);
     const AdapterSpace sp = adapter_space(workspace, rows, inner, l.adapters, l.rank, dtype);
     hipLaunchKernelGGL(k_order_rows, dim3(1), dim3(1024), 0, s, ids, rows, (int)adapters, sp);
     hipError_t err = hipGetLastError();
@@ -154,9 +155,10 @@ hipError_t launch_adapter(const ocean_adapters &l, const int32_t *ids, int dtype
             a.out = sp.part, a.ldo = sp.rank_up;
             a.ptr = sp.ptr, a.groups = adapters;
             a.n = rank, a.c_part = sp.c_part;
-            const bool aligned = pieces_aligned(x, ldx, 0, size) && pieces_aligned(l.a, l.ld_a, l.stride_a, size) && inner % e == 0;
-            hipError_t r = aligned ? launch_gmm<T, false, false, 64, 64, 4, 1, true, GM_SHRINK, float>(a, s)
-                                   : launch_gmm<T, false, false, 64, 64, 4, 1, false, GM_SHRINK, float>(a, s);
+            const bool aligned = pieces_aligned(x, ldx, 0, size) && pieces_aligned(l.a, l.ld_a, l.stride_a, size) && inner % e == 0 && x_fits &&
+                                 offsets_fit(256, l.ld_a, size);
+            hipError_t r = aligned ? launch_gmm<T, false, false, 64, 64, 4, 1, true, 2, GM_SHRINK, float>(a, s)
+                                   : launch_gmm<T, false, false, 64, 64, 4, 1, false, 2, GM_SHRINK, float>(a, s);
             if (r != hipSuccess) return r;
             hipLaunchKernelGGL((k_finish_shrink<T>), dim3((uint32_t)std::min((rows + 3) / 4, (int64_t)1 << 20)), dim3(256), 0, s, sp, rows, rank,
                                l.ranks, l.scale);
@@ -167,12 +169,8 @@ hipError_t launch_adapter(const ocean_adapters &l, const int32_t *ids, int dtype
         a.out = y, a.ldo = ldy, a.n = outer;
         a.slot_id = sp.slot_id, a.adapter_ptr = sp.ptr, a.adapters = adapters;
         a.h = sp.h, a.row_scale = sp.row_scale, a.b = l.b, a.ldb = l.ld_b, a.stride_b = l.stride_b, a.ranks = l.ranks, a.rank = rank, a.rank_up = sp.rank_up;
-        const bool aligned = pieces_aligned(x, ldx, 0, size) && pieces_aligned(w, ldw, 0, size) && inner % e == 0;
-        if constexpr (sizeof(T) == 2) {
-            if (aligned && rows >= 256 && outer >= 256) return launch_gmm<T, false, false, 256, 256, 2, 4, true, GM_EXPAND>(a, s);
-        }
-        return aligned ? launch_gmm<T, false, false, 128, 128, 2, 2, true, GM_EXPAND>(a, s)
-                       : launch_gmm<T, false, false, 128, 128, 2, 2, false, GM_EXPAND>(a, s);
+        const bool aligned = pieces_aligned(x, ldx, 0, size) && pieces_aligned(w, ldw, 0, size) && inner % e == 0 && x_fits && offsets_fit(256, ldw, size);
+        return launch_tiles<T, false, false, GM_EXPAND>(a, [&](int64_t bm) { return (rows + bm - 1) / bm; }, aligned, s);
     });
 }
 

@@ -7,10 +7,12 @@
 // place in LDS is fixed by its number, so the XOR is applied to the source), otherwise through registers by unaligned loads.
 //
 // A 16 x 16 result tile of v_mfma_16x16 has its columns' operand first, so that a lane holds 4 columns of one row; the lines of R that
-// four such tiles read are interleaved in fours, so that a lane holds 16 consecutive columns and writes 32 or 64 bytes side by side.
+// four such tiles read are interleaved in fours, so that a lane holds 16 consecutive columns and writes 32 or 64 bytes side by side (not in a col tile:
+// the transposing read would use half of each piece).
 #pragma once
 
 #include <algorithm>
+#include <type_traits>
 
 #include "routed.hpp"
 
@@ -23,8 +25,8 @@ typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef short s16x8 __attribute__((ext_vector_type(8)));
 
-constexpr int LINE = 128;                                   // bytes of c in a step
-template <class T> constexpr int STEP = LINE / (int)sizeof(T);   // elements of c in a step
+constexpr int LINE = 128;                                   // bytes of c in a step of most kernels
+template <class T> constexpr int STEP = LINE / (int)sizeof(T);   // elements of c in it
 template <class T> constexpr int PIECE = 16 / (int)sizeof(T);    // elements of 16 bytes
 
 __device__ const uint4 g_zero_piece = {0u, 0u, 0u, 0u};     // what stands for pieces behind the end of c
@@ -49,60 +51,78 @@ template <bool INTER> __device__ __forceinline__ int tile_line(int j, int r)
 {
     return INTER ? (j / 4) * 64 + (r / 4) * 16 + (j % 4) * 4 + r % 4 : j * 16 + r;
 }
-// The XOR of a row tile's line: the bits in which the 16 lines that are read at once differ, but the lowest (two lines of 128
-// bytes lie side by side in the 64 banks).
-template <bool INTER> __device__ __forceinline__ int row_xor(int line)
+// The XOR of a row tile's line of PIECES pieces (2 lines of 128 or 4 of 64 bytes lie side by side in the 64 banks).  A 16-byte read of a
+// wave takes four turns, the first of lanes 0 - 3, 12 - 15 and 20 - 27, the second of 4 - 11, 16 - 19 and 28 - 31, and so on: with lane %
+// 16 the line and lane / 16 the piece, the 16 of a turn fall on 16 places (no conflict is counted).
+template <bool INTER, int PIECES> __device__ __forceinline__ int row_xor(int line)
 {
+    if (PIECES == 4) {
+        const int q = (INTER ? line >> 4 : line >> 2) & 3;
+        return ((q ^ q << 1) & 2) | q >> 1;
+    }
     return INTER ? ((line >> 1) & 1) | ((line >> 4) & 3) << 1 : (line >> 1) & 7;
 }
-// The XOR of a col tile's line c: 16-bit types read c = 8 g + 0 .. 3 (and + 4) at once, single precision c = 4 g + j.
-template <class T> __device__ __forceinline__ int col_xor(int c)
+// The XOR of a col tile's line c of PIECES pieces: 16-bit types read two pieces each of c = 8 g + 0 .. 3 (and + 4), two g at once, single
+// precision four pieces of c = 4 g + j, all g at once.  (Lines of 8 pieces lie two by two on the banks.)
+template <class T, int PIECES> __device__ __forceinline__ int col_xor(int c)
 {
-    return sizeof(T) == 2 ? (c & 3) | ((c >> 3) & 3) << 2 : ((c >> 2) & 3) << 2;
+    if (sizeof(T) == 4) return ((c >> 2) & 3) << 2;
+    return PIECES == 8 ? ((c >> 1) & 1) << 1 | ((c >> 3) & 1) << 2 : (c & 3) << 1 | ((c >> 3) & 1) << 3;
 }
 
-// One operand's tile of B lines (row) or B columns (col), moved by THREADS threads.
-template <class T, bool COL, bool INTER, int B, int THREADS>
+// One operand's tile of B lines (row) or B columns (col), DEPTH bytes of c, moved by THREADS threads.
+template <class T, bool COL, bool INTER, int B, int THREADS, int DEPTH>
 struct Tile {
-    static constexpr int BYTES = B * LINE;
+    static constexpr int BYTES = B * DEPTH, LINE_C = DEPTH / (int)sizeof(T);
     static constexpr int LOADS = BYTES / 16 / THREADS;       // pieces a thread moves
-    static constexpr int PIECES = COL ? B / PIECE<T> : 8;    // pieces in a line
+    static constexpr int PIECES = COL ? B / PIECE<T> : DEPTH / 16;    // pieces in a line
     static_assert(BYTES % (16 * THREADS) == 0, "whole pieces a thread");
 
-    __device__ static int line_of(int i) { return (i * THREADS + (int)threadIdx.x) / PIECES; }
-    __device__ static int piece_of(int i)
+    // The line and the piece of it that thread `tid` moves as its i-th.
+    __device__ static int line_of(int tid, int i) { return (i * THREADS + tid) / PIECES; }
+    __device__ static int piece_of(int tid, int i)
     {
-        const int q = i * THREADS + (int)threadIdx.x, line = q / PIECES;
-        return (q % PIECES) ^ (COL ? col_xor<T>(line) : row_xor<INTER>(line));
+        const int q = i * THREADS + tid, line = q / PIECES;
+        return (q % PIECES) ^ (COL ? col_xor<T, PIECES>(line) : row_xor<INTER, PIECES>(line));
     }
-    // 64 bytes of c (half: 0 or 1) of 16x16 tile j, as mma takes them.
-    __device__ static Frag<T> read(const char *lds, int first, int j, int half)
+    // Where this lane reads tile 0 of the lines from `first` on (a multiple of the lines that the wave reads), in bytes.  The bits that the XOR takes and
+    // those that the tile's number j and the half add are different ones, so all other places follow from this one by constants.
+    __device__ static uint32_t place(int first)
     {
         const int lane = lane_id(), r = lane % 16, g = lane / 16;
         if constexpr (!COL) {
-            const int line = first + tile_line<INTER>(j, r);
-            return *reinterpret_cast<const Frag<T> *>(lds + line * LINE + (((half * 4 + g) ^ row_xor<INTER>(line)) * 16));
+            const int line = first + tile_line<INTER>(0, r);
+            return line * DEPTH + (g ^ row_xor<INTER, PIECES>(line)) * 16;
         } else if constexpr (sizeof(T) == 2) {
             // each lane names 4 columns of one c; a group of 16 lanes gets its 4 x 16 block transposed
-            const int col = first + tile_line<INTER>(j, (r % 4) * 4);
+            const int col = first + tile_line<INTER>(0, (r % 4) * 4), c = g * 8 + r / 4;
+            return c * (PIECES * 16) + ((col / 8) ^ col_xor<T, PIECES>(c)) * 16 + (col % 8) * 2;
+        } else {
+            const int col = first + tile_line<INTER>(0, r), c = g * 4;
+            return c * (PIECES * 16) + ((col / 4) ^ col_xor<T, PIECES>(c)) * 16 + (col % 4) * 4;
+        }
+    }
+    // 64 bytes of c (the half-th of DEPTH) of 16 x 16 tile j, as mma takes them.
+    __device__ static Frag<T> read(const char *lds, uint32_t place, int j, int half)
+    {
+        if constexpr (!COL) {
+            return *reinterpret_cast<const Frag<T> *>(lds + (place ^ (half * 64)) + tile_line<INTER>(j, 0) * DEPTH);
+        } else if constexpr (sizeof(T) == 2) {
+            const uint32_t at = place ^ (tile_line<INTER>(j, 0) * 2);
             s16x8 v;
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-                const int c = half * 32 + g * 8 + h * 4 + r / 4;
-                const int at = c * (PIECES * 16) + (((col / 8) ^ col_xor<T>(c)) * 16) + (col % 8) * 2;
-                const s16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4 *)(lds + at));
+                const s16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                    (__attribute__((address_space(3))) s16x4 *)(lds + at + (half * 32 + h * 4) * (PIECES * 16)));
 #pragma unroll
                 for (int i = 0; i < 4; ++i) v[h * 4 + i] = x[i];
             }
             return __builtin_bit_cast(Frag<T>, v);
         } else {
-            const int col = first + tile_line<INTER>(j, r);
+            const uint32_t at = place ^ (tile_line<INTER>(j, 0) * 4);
             f32x4 v;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int c = half * 16 + g * 4 + i;
-                v[i] = *reinterpret_cast<const float *>(lds + c * (PIECES * 16) + (((col / 4) ^ col_xor<T>(c)) * 16) + (col % 4) * 4);
-            }
+            for (int i = 0; i < 4; ++i) v[i] = *reinterpret_cast<const float *>(lds + at + (half * 16 + i) * (PIECES * 16));
             return v;
         }
     }
@@ -159,272 +179,422 @@ enum GmmMode {
     GM_EXPAND    // one R for all rows; after c, the products of h with the rows' adapters' b; rows are stored where they came from
 };
 
-__device__ __forceinline__ void group_range(const GmmArgs &a, int64_t e, int64_t &lo, int64_t &hi)
+__device__ __forceinline__ void group_range(const GmmArgs &a, int e, int &lo, int &hi)
 {
-    lo = min(max(a.ptr[e], (int64_t)0), a.rows);
-    hi = min(max(a.ptr[e + 1], lo), a.rows);
+    const int64_t l = min(max(a.ptr[e], (int64_t)0), a.rows);   // (rows are below 2^31)
+    lo = (int)l;
+    hi = (int)min(max(a.ptr[e + 1], l), a.rows);
 }
 
-// Which group and which of its tiles of `size` rows tile number `t` is; false: there are fewer.  Every wave for itself.  `used` receives the
-// tiles there are where it is false.
-__device__ __forceinline__ bool find_tile(const GmmArgs &a, int64_t t, int size, int64_t &group, int64_t &lo, int64_t &hi, int64_t &used)
+// Which group and which of its tiles of `size` rows tile number `t` is, and how many tiles there are; false: fewer than that.
+// item_of(tiles) says the number where it depends on how many there are.  Every wave for itself.
+template <class F>
+__device__ __forceinline__ bool find_tile(const GmmArgs &a, int size, F item_of, int &group, int &lo, int &hi)
 {
+    const int groups = (int)a.groups;
+    auto load = [&](int e0, int &l, int &h) -> uint32_t {   // tiles of group e0 + lane
+        l = h = 0;
+        if (e0 + lane_id() < groups) group_range(a, e0 + lane_id(), l, h);
+        return wave_inclusive_scan_u32(((uint32_t)(h - l) + (uint32_t)size - 1) / (uint32_t)size);
+    };
+    int l, h;
+    uint32_t tiles = 0, incl = 0;
+    for (int e0 = 0; e0 < groups; e0 += WAVE) {
+        incl = load(e0, l, h);
+        tiles += wave_read_lane_u32(incl, WAVE - 1);
+    }
+    const int t = item_of((int)tiles);
+    if (t < 0 || (uint32_t)t >= tiles) return false;
     uint32_t before = 0;
-    for (int64_t e0 = 0; e0 < a.groups; e0 += WAVE) {
-        const int64_t e = e0 + lane_id();
-        int64_t l = 0, h = 0;
-        if (e < a.groups) group_range(a, e, l, h);
-        const uint32_t tiles = (uint32_t)((h - l + size - 1) / size), incl = wave_inclusive_scan_u32(tiles);
-        const unsigned long long past = __ballot(before + incl > t);
+    for (int e0 = 0; e0 < groups; e0 += WAVE) {
+        if (groups > WAVE) incl = load(e0, l, h);   // (else it is at hand)
+        const unsigned long long past = __ballot(before + incl > (uint32_t)t);
         if (past) {
             const int k = __ffsll(past) - 1;
             group = e0 + k;
-            const uint32_t first = wave_read_lane_u32(before + incl - tiles, k);
-            lo = wave_first(__shfl(l, k, WAVE)) + (int64_t)((uint32_t)t - first) * size;
-            hi = wave_first(__shfl(h, k, WAVE));
+            const uint32_t first = before + (k > 0 ? wave_read_lane_u32(incl, k - 1) : 0u);
+            lo = (int)wave_read_lane_u32((uint32_t)l, k) + (int)(((uint32_t)t - first) * (uint32_t)size);
+            hi = (int)wave_read_lane_u32((uint32_t)h, k);
             return true;
         }
         before += wave_read_lane_u32(incl, WAVE - 1);
     }
-    used = before;
     return false;
 }
 
-// Work item of a workgroup: workgroups go to the 8 dies in turn, each die with its own L2, so each die gets a contiguous stretch.
-__device__ __forceinline__ int64_t by_die(int64_t block, int64_t blocks) { return (block & 7) * (blocks >> 3) + (block >> 3); }
+// Clears a stretch of columns of the rows that belong to no group; the part-th of `parts` workgroups that do so.
+template <class O>
+__device__ __forceinline__ void clear_outside(const GmmArgs &a, int64_t col, int64_t width, int64_t part, int64_t parts)
+{
+    const int64_t first = min(max(a.ptr[0], (int64_t)0), a.rows), last = min(max(a.ptr[a.groups], first), a.rows);
+    const int64_t count = (a.rows - (last - first)) * width;
+    for (int64_t i = part * blockDim.x + threadIdx.x; i < count; i += parts * blockDim.x) {
+        const int64_t row = i / width;
+        static_cast<O *>(a.out)[(row < first ? row : row - first + last) * a.ldo + col + i % width] = (O)0.0f;
+    }
+}
+
+// The number-th item of this workgroup's die: workgroups go to the 8 dies in turn, each die with its own L2, so each die gets a
+// contiguous stretch of the items.  -1: there is none; so it is for all blocks from the next multiple of 8 on where the number is blockIdx.x / 8.
+__device__ __forceinline__ int by_die(int number, int items)
+{
+    const int per = (items + 7) >> 3, item = (int)(blockIdx.x & 7) * per + number;
+    return number < per && item < items ? item : -1;
+}
 
 // m-tiles by n-tiles in bands of `band` m-tiles, so that workgroups that run together share lines of both operands.
-__device__ __forceinline__ void banded(int64_t item, int64_t mt, int64_t nt, int band, int64_t &m, int64_t &n)
+__device__ __forceinline__ void banded(int item, int mt, int nt, int band, int &m, int &n)
 {
-    const int64_t per = band * nt, b = item / per, in = item - b * per, height = min((int64_t)band, mt - b * band);
+    const int per = band * nt, b = item / per, in = item - b * per, height = min(band, mt - b * band);
     m = b * band + in % height;
     n = in / height;
 }
 
-template <class T, bool LCOL, bool RCOL, int BM, int BN, int WAVES_M, int WAVES_N, bool ASYNC, GmmMode MODE, class O = T>
-__global__ void __launch_bounds__(WAVES_M * WAVES_N * WAVE, 2) k_gmm(GmmArgs a, int64_t mt, int64_t nt)
+// Where a thread's pieces of one operand begin in memory: a base that is the same for the workgroup, and for each piece the bytes from
+// there, 32 bits where pieces go straight to LDS (the address then takes no vector instruction, see offsets_fit).
+template <class T, class TI, bool COL, bool ASYNC>
+struct Feed {
+    using Off = std::conditional_t<ASYNC, uint32_t, int64_t>;
+    const T *base;
+    int64_t ld, advance;       // elements from a line to the next, from a step to the next
+    Off off[TI::LOADS];
+    int room;                  // (col) columns from the first on
+
+    // (row) line l is row row_of(l) behind `at`
+    template <class F> __device__ __forceinline__ void lines(int tid, const T *at, int64_t ld_, F row_of)
+    {
+        base = at, ld = ld_, advance = TI::LINE_C, room = 0;
+#pragma unroll
+        for (int i = 0; i < TI::LOADS; ++i) off[i] = (Off)((row_of(TI::line_of(tid, i)) * ld + TI::piece_of(tid, i) * PIECE<T>) * (int64_t)sizeof(T));
+    }
+    // (col) columns col0 .. of `cols`, lines from c0 on; by_number: the line is given with each piece (row()).  Columns behind the end:
+    // the last piece's where pieces are whole, what comes of them is not stored
+    __device__ __forceinline__ void columns(int tid, const T *at, int64_t ld_, int64_t col0, int64_t cols, int64_t c0, bool by_number)
+    {
+        base = at + (by_number ? 0 : c0 * ld_) + col0, ld = ld_, advance = TI::LINE_C * ld_;
+        room = (int)min(cols - col0, (int64_t)1 << 30);
+#pragma unroll
+        for (int i = 0; i < TI::LOADS; ++i) {
+            const int col = ASYNC ? min(TI::piece_of(tid, i) * PIECE<T>, room - PIECE<T>) : TI::piece_of(tid, i) * PIECE<T>;
+            off[i] = (Off)(((by_number ? 0 : TI::line_of(tid, i) * ld) + col) * (int64_t)sizeof(T));
+        }
+    }
+    __device__ __forceinline__ const char *step(int t) const { return reinterpret_cast<const char *>(base + t * advance); }
+    __device__ __forceinline__ const char *row(int i, int64_t number) const { return reinterpret_cast<const char *>(base + number * ld) + off[i]; }
+    // Elements of piece i that there are where the step has `left` c (0 or less: none).
+    __device__ __forceinline__ int valid(int tid, int i, int left) const
+    {
+        if (!COL) return min(PIECE<T>, left - TI::piece_of(tid, i) * PIECE<T>);
+        return TI::line_of(tid, i) >= left ? 0 : ASYNC ? PIECE<T> : min(PIECE<T>, room - TI::piece_of(tid, i) * PIECE<T>);
+    }
+    __device__ __forceinline__ const void *numbered(int tid, int i, int left, int64_t number, int64_t rows) const
+    {
+        return valid(tid, i, left) > 0 && (uint64_t)number < (uint64_t)rows ? static_cast<const void *>(row(i, number)) : &g_zero_piece;
+    }
+};
+
+template <class T, bool LCOL, bool RCOL, int BM, int BN, int WAVES_M, int WAVES_N, bool ASYNC, int STAGES, GmmMode MODE, class O = T>
+__global__ void __launch_bounds__(WAVES_M * WAVES_N * WAVE, 2) k_gmm(GmmArgs a, int mt, int nt)
 {
     constexpr int THREADS = WAVES_M * WAVES_N * WAVE, WM = BM / WAVES_M, WN = BN / WAVES_N, TM = WM / 16, TN = WN / 16;
-    static_assert(WN % 64 == 0, "four interleaved tiles");
-    using TL = Tile<T, LCOL, false, BM, THREADS>;
-    using TR = Tile<T, RCOL, true, BN, THREADS>;
+    static_assert(RCOL || WN % 64 == 0, "four interleaved tiles");
+    constexpr int BYTES = LINE, STEP_C = BYTES / (int)sizeof(T), HALVES = BYTES / 64;
+    using TL = Tile<T, LCOL, false, BM, THREADS, BYTES>;
+    using TR = Tile<T, RCOL, !RCOL, BN, THREADS, BYTES>;
     constexpr int BUFFER = TL::BYTES + TR::BYTES;
     constexpr bool DEPTH = MODE == GM_DEPTH;
-    __shared__ __align__(16) char lds[2 * BUFFER];
+    static_assert(STAGES >= 2 && (ASYNC || STAGES == 2), "through registers: one step ahead");
+    __shared__ __align__(16) char lds[STAGES * BUFFER];
 
-    int64_t mi, ni, group = 0, lo = 0, hi = 0, c_lo = 0, c_hi = a.c;
-    int64_t item = by_die(blockIdx.x, gridDim.x), stretch = 0;
-    if constexpr (MODE == GM_EXPAND) {
-        if (item >= mt * nt) return;
-        banded(item, mt, nt, 4, mi, ni);
-        lo = mi * BM;
-        hi = a.rows;
-    } else if constexpr (DEPTH) {
-        group = item / (mt * nt);
-        if (group >= a.groups) return;
-        banded(item - group * mt * nt, mt, nt, 4, mi, ni);
-        group_range(a, group, c_lo, c_hi);
-        lo = mi * BM;
-        hi = a.m;
-    } else {
-        if constexpr (MODE == GM_SHRINK) {
-            stretch = item / (mt * nt);
-            item -= stretch * mt * nt;
-            c_lo = stretch * a.c_part;
-            if (c_lo >= a.c) return;
-            c_hi = min(c_lo + a.c_part, a.c);
-        }
-        if (item >= mt * nt) return;
-        banded(item, mt, nt, 4, mi, ni);
-        int64_t used;
-        if (!find_tile(a, mi, BM, group, lo, hi, used)) {   // no rows left: clear those of no group
-            if constexpr (MODE == GM_SHRINK) return;
-            const int64_t first = min(max(a.ptr[0], (int64_t)0), a.rows), last = min(max(a.ptr[a.groups], first), a.rows);
-            const int64_t outside = a.rows - (last - first), width = min((int64_t)BN, a.n - ni * BN);
-            for (int64_t i = (mi - used) * BM; i < outside; i += (mt - used) * BM) {
-                const int64_t count = min((int64_t)BM, outside - i) * width;
-                for (int64_t k = threadIdx.x; k < count; k += THREADS) {
-                    const int64_t row = i + k / width;
-                    static_cast<O *>(a.out)[(row < first ? row : row - first + last) * a.ldo + ni * BN + k % width] = (O)0.0f;
+    // The tile of the number-th work item of this workgroup's die.
+    struct Work { int group, m0, hi, n0, c_lo, c_hi, stretch; };
+    int tiles = 0;   // (GM_ROWS, GM_SHRINK) those that the groups make; mt is the most they may make
+    auto locate = [&](int number, Work &w) -> bool {
+        int mi, ni, lo = 0;
+        w = Work{0, 0, (int)a.rows, 0, 0, (int)a.c, 0};
+        if constexpr (MODE == GM_EXPAND) {
+            const int item = by_die(number, mt * nt);
+            if (item < 0) return false;
+            banded(item, mt, nt, 4, mi, ni);
+            lo = mi * BM;
+        } else if constexpr (DEPTH) {
+            const int item = by_die(number, mt * nt * (int)a.groups);
+            if (item < 0) return false;
+            w.group = item / (mt * nt);
+            banded(item - w.group * mt * nt, mt, nt, 4, mi, ni);
+            group_range(a, w.group, w.c_lo, w.c_hi);
+            lo = mi * BM;
+            w.hi = (int)a.m;
+        } else {
+            auto item_of = [&](int n) -> int {
+                tiles = n;
+                const int stretches = MODE == GM_SHRINK ? (int)((a.c + a.c_part - 1) / a.c_part) : 1;
+                int item = by_die(number, n * nt * stretches);
+                if (item < 0) return -1;
+                if constexpr (MODE == GM_SHRINK) {
+                    w.stretch = item / (n * nt);
+                    item -= w.stretch * n * nt;
                 }
+                banded(item, n, nt, 4, mi, ni);
+                return mi;
+            };
+            if (!find_tile(a, BM, item_of, w.group, lo, w.hi)) return false;
+            if constexpr (MODE == GM_SHRINK) {
+                w.c_lo = w.stretch * (int)a.c_part;
+                w.c_hi = (int)min(w.c_lo + a.c_part, a.c);
             }
-            return;
         }
+        w.m0 = lo;
+        w.n0 = ni * BN;
+        return true;
+    };
+    Work w;
+    if (!locate(blockIdx.x >> 3, w)) {
+        if constexpr (MODE == GM_ROWS) {   // (some have no tile: see launch_gmm)
+            const int from = (tiles * nt + 7) / 8 * 8, part = (int)blockIdx.x - from;
+            if (part >= 0) clear_outside<O>(a, 0, a.n, part, (int)gridDim.x - from);
+        }
+        return;
     }
-    const int64_t n0 = ni * BN, m0 = lo;
-    const T *lbase = static_cast<const T *>(a.l), *rbase = static_cast<const T *>(a.r) + (DEPTH ? 0 : group * a.stride);
-    O *out = static_cast<O *>(a.out) + (DEPTH ? group * a.stride : stretch * a.rows * a.ldo);
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE);
     const int wm = (wave / WAVES_N) * WM, wn = (wave % WAVES_N) * WN;
-    const int64_t depth = c_hi - c_lo, steps = (depth + STEP<T> - 1) / STEP<T>;
-
-    // Where each piece of this thread begins in memory, at step 0.  Lines behind the end are those of the last line: what
-    // comes of them is not stored.  With ragged c the line of memory is found step by step.
-    const T *lp[TL::LOADS], *rp[TR::LOADS];
-#pragma unroll
-    for (int i = 0; i < TL::LOADS; ++i) {
-        const int line = TL::line_of(i), piece = TL::piece_of(i);
-        if constexpr (!LCOL) {
-            int64_t row = min(m0 + line, hi - 1);
-            if (!DEPTH && a.index) {
-                row = a.index[row];
-                if ((uint64_t)row >= (uint64_t)a.index_rows) row = 0;   // (its result is replaced by 0)
-            }
-            lp[i] = lbase + row * a.ldl + c_lo + piece * PIECE<T>;
+    const int tid = threadIdx.x;
+    // What of x's rows this workgroup reads: those of its slots, or (GM_DEPTH) one for each c.
+    const bool numbered = DEPTH && a.index != nullptr;
+    Feed<T, TL, LCOL, ASYNC> feed_l;
+    Feed<T, TR, RCOL, ASYNC> feed_r;
+    const int depth = w.c_hi - w.c_lo, steps = (depth + STEP_C - 1) / STEP_C;
+    {
+        const T *rbase = static_cast<const T *>(a.r) + (DEPTH ? 0 : (int64_t)w.group * a.stride);
+        if constexpr (LCOL) {
+            feed_l.columns(tid, static_cast<const T *>(a.l), a.ldl, w.m0, a.m, w.c_lo, numbered && !a.index_on_r);
         } else {
-            const int64_t col = min(m0 + piece * PIECE<T>, ASYNC ? a.m - PIECE<T> : a.m);
-            lp[i] = lbase + (c_lo + line) * a.ldl + col;
+            const bool gather = !DEPTH && a.index;
+            feed_l.lines(tid, static_cast<const T *>(a.l) + (int64_t)(gather ? 0 : w.m0) * a.ldl + w.c_lo, a.ldl, [&](int line) -> int64_t {
+                const int at = min(line, w.hi - 1 - w.m0);   // (what comes of lines behind the end is not stored)
+                if (!gather) return at;
+                const int64_t row = a.index[w.m0 + at];
+                return (uint64_t)row < (uint64_t)a.index_rows ? row : 0;   // (its result is replaced by 0)
+            });
         }
-    }
-#pragma unroll
-    for (int i = 0; i < TR::LOADS; ++i) {
-        const int line = TR::line_of(i), piece = TR::piece_of(i);
-        if constexpr (!RCOL) {
-            rp[i] = rbase + min(n0 + line, a.n - 1) * a.ldr + c_lo + piece * PIECE<T>;
-        } else {
-            const int64_t col = min(n0 + piece * PIECE<T>, ASYNC ? a.n - PIECE<T> : a.n);
-            rp[i] = rbase + (c_lo + line) * a.ldr + col;
-        }
+        if constexpr (RCOL) feed_r.columns(tid, rbase, a.ldr, w.n0, a.n, w.c_lo, numbered && a.index_on_r);
+        else feed_r.lines(tid, rbase + (int64_t)w.n0 * a.ldr + w.c_lo, a.ldr, [&](int line) -> int64_t { return min(line, (int)a.n - 1 - w.n0); });
     }
 
-    // The pointer of piece i of step t, and how many of its elements there are (0 or less: none, the pointer may not be read).
-    auto piece_l = [&](int i, int64_t t, int &valid) -> const T * {
-        const int line = TL::line_of(i), piece = TL::piece_of(i);
-        if constexpr (!LCOL) {
-            valid = (int)min((int64_t)PIECE<T>, depth - t * STEP<T> - piece * PIECE<T>);
-            return lp[i] + t * STEP<T>;
-        } else {
-            const int64_t c = t * STEP<T> + line;
-            valid = c < depth ? (int)min((int64_t)PIECE<T>, a.m - (m0 + piece * PIECE<T>)) : 0;
-            if (ASYNC && c < depth) valid = PIECE<T>;
-            if (DEPTH && a.index && !a.index_on_r && c < depth) {
-                const int64_t row = a.index[c_lo + c];
-                if ((uint64_t)row >= (uint64_t)a.index_rows) { valid = 0; return lp[i]; }
-                return lp[i] + (row - c_lo - line) * a.ldl;
+    // (GM_DEPTH with row numbers: those of the step that is fetched next, loaded before the pieces of the step before it, since loads come
+    // back in order and waiting for the numbers would otherwise mean waiting for all pieces under way)
+    constexpr int NUMBERS = DEPTH ? (TL::LOADS > TR::LOADS ? TL::LOADS : TR::LOADS) : 1;
+    int32_t number[NUMBERS];
+    auto load_numbers = [&](int t) {
+        if constexpr (DEPTH) {
+            if (!numbered) return;
+            if (a.index_on_r) {
+#pragma unroll
+                for (int i = 0; i < TR::LOADS; ++i) number[i] = a.index[(int64_t)w.c_lo + min(t * STEP_C + TR::line_of(tid, i), depth - 1)];
+            } else {
+#pragma unroll
+                for (int i = 0; i < TL::LOADS; ++i) number[i] = a.index[(int64_t)w.c_lo + min(t * STEP_C + TL::line_of(tid, i), depth - 1)];
             }
-            return lp[i] + t * STEP<T> * a.ldl;
-        }
-    };
-    auto piece_r = [&](int i, int64_t t, int &valid) -> const T * {
-        const int line = TR::line_of(i), piece = TR::piece_of(i);
-        if constexpr (!RCOL) {
-            valid = (int)min((int64_t)PIECE<T>, depth - t * STEP<T> - piece * PIECE<T>);
-            return rp[i] + t * STEP<T>;
-        } else {
-            const int64_t c = t * STEP<T> + line;
-            valid = c < depth ? (int)min((int64_t)PIECE<T>, a.n - (n0 + piece * PIECE<T>)) : 0;
-            if (ASYNC && c < depth) valid = PIECE<T>;
-            if (DEPTH && a.index && a.index_on_r && c < depth) {
-                const int64_t row = a.index[c_lo + c];
-                if ((uint64_t)row >= (uint64_t)a.index_rows) { valid = 0; return rp[i]; }
-                return rp[i] + (row - c_lo - line) * a.ldr;
-            }
-            return rp[i] + t * STEP<T> * a.ldr;
         }
     };
 
     uint4 kept_l[ASYNC ? 1 : TL::LOADS], kept_r[ASYNC ? 1 : TR::LOADS];
-    auto fetch = [&](int64_t t, int buffer) {
+    auto fetch = [&](int t, int buffer) {
         char *to = lds + buffer * BUFFER;
+        const int left = min(STEP_C, depth - t * STEP_C);   // c of this step
+        if constexpr (ASYNC) {
+            int32_t now[NUMBERS];
 #pragma unroll
-        for (int i = 0; i < TL::LOADS; ++i) {
-            int valid;
-            const T *p = piece_l(i, t, valid);
-            if constexpr (ASYNC) load_to_lds(valid > 0 ? static_cast<const void *>(p) : &g_zero_piece, to + (i * THREADS + wave * WAVE) * 16);
-            else kept_l[i] = load_piece(p, valid);
-        }
+            for (int i = 0; i < NUMBERS; ++i) now[i] = number[i];
+            if constexpr (DEPTH) load_numbers(t + 1);
+            asm volatile("" ::: "memory");
+            char *to_wave = to + wave * (WAVE * 16);
+            auto move = [&](auto &feed, auto tile, char *dst, bool by_number) {
+                using TI = decltype(tile);
+                if (DEPTH && by_number) {
 #pragma unroll
-        for (int i = 0; i < TR::LOADS; ++i) {
-            int valid;
-            const T *p = piece_r(i, t, valid);
-            if constexpr (ASYNC) load_to_lds(valid > 0 ? static_cast<const void *>(p) : &g_zero_piece, to + TL::BYTES + (i * THREADS + wave * WAVE) * 16);
-            else kept_r[i] = load_piece(p, valid);
+                    for (int i = 0; i < TI::LOADS; ++i) load_to_lds(feed.numbered(tid, i, left, now[i], a.index_rows), dst + i * THREADS * 16);
+                } else if (left == STEP_C) {
+                    const char *base = feed.step(t);
+#pragma unroll
+                    for (int i = 0; i < TI::LOADS; ++i) load_to_lds(base + feed.off[i], dst + i * THREADS * 16);
+                } else {
+#pragma unroll
+                    for (int i = 0; i < TI::LOADS; ++i)
+                        load_to_lds(feed.valid(tid, i, left) > 0 ? static_cast<const void *>(feed.step(t) + feed.off[i]) : &g_zero_piece, dst + i * THREADS * 16);
+                }
+            };
+            move(feed_l, TL{}, to_wave, numbered && !a.index_on_r);
+            move(feed_r, TR{}, to_wave + TL::BYTES, numbered && a.index_on_r);
+        } else {
+            auto move = [&](auto &feed, auto tile, uint4 *dst, bool by_number) {
+                using TI = decltype(tile);
+#pragma unroll
+                for (int i = 0; i < TI::LOADS; ++i) {
+                    int valid = feed.valid(tid, i, left);
+                    const char *from = feed.step(t) + feed.off[i];
+                    if (DEPTH && by_number) {
+                        from = feed.row(i, number[i]);
+                        if ((uint64_t)(int64_t)number[i] >= (uint64_t)a.index_rows) valid = 0;
+                    }
+                    dst[i] = load_piece(reinterpret_cast<const T *>(from), valid);
+                }
+            };
+            move(feed_l, TL{}, kept_l, numbered && !a.index_on_r);
+            move(feed_r, TR{}, kept_r, numbered && a.index_on_r);
+            if constexpr (DEPTH) load_numbers(t + 1);
         }
     };
     auto stash = [&](int buffer) {
         if constexpr (!ASYNC) {
             char *to = lds + buffer * BUFFER;
 #pragma unroll
-            for (int i = 0; i < TL::LOADS; ++i) *reinterpret_cast<uint4 *>(to + (i * THREADS + threadIdx.x) * 16) = kept_l[i];
+            for (int i = 0; i < TL::LOADS; ++i) *reinterpret_cast<uint4 *>(to + (i * THREADS + tid) * 16) = kept_l[i];
 #pragma unroll
-            for (int i = 0; i < TR::LOADS; ++i) *reinterpret_cast<uint4 *>(to + TL::BYTES + (i * THREADS + threadIdx.x) * 16) = kept_r[i];
+            for (int i = 0; i < TR::LOADS; ++i) *reinterpret_cast<uint4 *>(to + TL::BYTES + (i * THREADS + tid) * 16) = kept_r[i];
         }
     };
 
+    const int lane = lane_id(), r = lane % 16, g = lane / 16;
+    const uint32_t at_l = TL::place(wm), at_r = TR::place(wn);
+    // Rows out: where the results of this lane's rows go, then the results.
+    auto store = [&](const Work &w, const f32x4 (&acc)[TM][TN]) {
+        constexpr int OP = RCOL ? 4 : PIECE<O>;   // elements of one store
+        constexpr int RUN = RCOL ? 1 : 4;         // tiles whose columns a lane has side by side
+        O *out = static_cast<O *>(a.out) + (DEPTH ? (int64_t)w.group * a.stride : (int64_t)w.stretch * a.rows * a.ldo);
+        const bool wide = a.ldo % OP == 0 && reinterpret_cast<uintptr_t>(out) % (OP * sizeof(O)) == 0;
+        int32_t x_row[TM];
+        if (!DEPTH && a.index) {
+#pragma unroll
+            for (int i = 0; i < TM; ++i) x_row[i] = a.index[min(w.m0 + wm + i * 16 + r, w.hi - 1)];
+        }
+#pragma unroll
+        for (int i = 0; i < TM; ++i) {
+            const int row = w.m0 + wm + i * 16 + r;
+            if (row >= w.hi) continue;
+            int64_t at = row;
+            bool zero = false;
+            if (!DEPTH && a.index) {
+                zero = (uint64_t)(int64_t)x_row[i] >= (uint64_t)a.index_rows;
+                if (MODE == GM_EXPAND) {
+                    if (zero) continue;
+                    at = x_row[i];
+                }
+            }
+#pragma unroll
+            for (int b = 0; b < TN / RUN; ++b) {
+                const int col = w.n0 + wn + b * RUN * 16 + g * RUN * 4;
+                O v[RUN * 4];
+#pragma unroll
+                for (int j = 0; j < RUN; ++j)
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) v[j * 4 + k] = (O)(zero ? 0.0f : acc[i][b * RUN + j][k]);
+                O *p = out + at * a.ldo + col;
+#pragma unroll
+                for (int j = 0; j < RUN * 4; j += OP) {
+                    if (wide && col + j + OP <= a.n) {
+                        Vec<O, OP> o;
+#pragma unroll
+                        for (int k = 0; k < OP; ++k) o.e[k] = v[j + k];
+                        *reinterpret_cast<Vec<O, OP> *>(p + j) = o;
+                    } else {
+#pragma unroll
+                        for (int k = 0; k < OP; ++k)
+                            if (col + j + k < a.n) p[j + k] = v[j + k];
+                    }
+                }
+            }
+        }
+    };
+
+    if (steps > 0) load_numbers(0);
     f32x4 acc[TM][TN] = {};
-    if (steps > 0) {
-        fetch(0, 0);
-        stash(0);
-    }
-    for (int64_t t = 0; t < steps; ++t) {
-        __builtin_amdgcn_s_waitcnt(0x0f70);   // vmcnt(0): this wave's part of the step is in LDS
-        __syncthreads();                      // everyone's is, and nobody reads the other buffer any more
-        const int buffer = (int)(t & 1);
-        if (t + 1 < steps) fetch(t + 1, buffer ^ 1);
+#pragma unroll
+    for (int t = 0; t < STAGES - 1; ++t)
+        if (t < steps) {
+            fetch(t, t);
+            stash(t);
+        }
+    int buffer = 0;
+    for (int t = 0; t < steps; ++t) {
+        // This wave's part of the step is in LDS (loads come back in order: all but those of later steps), and what it read of the step
+        // before has come; then everyone's is, and nobody reads the buffer of the step before any more.
+        constexpr int LATER = (STAGES - 2) * (TL::LOADS + TR::LOADS);
+        static_assert(LATER < 64, "what the counter holds");
+        if constexpr (ASYNC) {
+            asm volatile("" ::: "memory");
+            if (t + STAGES - 2 < steps) __builtin_amdgcn_s_waitcnt(0x0070 | (LATER & 15) | (LATER >> 4) << 14);
+            else __builtin_amdgcn_s_waitcnt(0x0070);
+            __builtin_amdgcn_s_barrier();
+            asm volatile("" ::: "memory");
+        } else {
+            __syncthreads();
+        }
+        const int next = buffer == 0 ? STAGES - 1 : buffer - 1;   // (that of the step before)
+        if (t + STAGES - 1 < steps) fetch(t + STAGES - 1, next);
         const char *from = lds + buffer * BUFFER;
 #pragma unroll
-        for (int half = 0; half < 2; ++half) {
+        for (int half = 0; half < HALVES; ++half) {
             Frag<T> fr[TN], fl[TM];
 #pragma unroll
-            for (int j = 0; j < TN; ++j) fr[j] = TR::read(from + TL::BYTES, wn, j, half);
+            for (int j = 0; j < TN; ++j) fr[j] = TR::read(from + TL::BYTES, at_r, j, half);
 #pragma unroll
-            for (int i = 0; i < TM; ++i) fl[i] = TL::read(from, wm, i, half);
+            for (int i = 0; i < TM; ++i) fl[i] = TL::read(from, at_l, i, half);
 #pragma unroll
             for (int i = 0; i < TM; ++i)
 #pragma unroll
                 for (int j = 0; j < TN; ++j) mma(acc[i][j], fr[j], fl[i]);
         }
-        if (t + 1 < steps) stash(buffer ^ 1);
+        if (!ASYNC && t + 1 < steps) stash(next);
+        buffer = buffer + 1 == STAGES ? 0 : buffer + 1;
     }
-
-    const int lane = lane_id(), r = lane % 16, g = lane / 16;
     if constexpr (MODE == GM_EXPAND) {
         // The adapters of the tile's rows, one after the other: 128 bytes of h and b a step, h's parts side by side and b's line again
         // for each.  A row takes only its own adapter's products (not 0 times the others', which may be infinite or NaN).
-        const int64_t end = min(m0 + BM, hi);
+        const int end = min(w.m0 + BM, w.hi);
         constexpr int PARTS = sizeof(T) == 2 ? 2 : 1;
         const int wide_h = PARTS * a.rank_up;
-        for (int64_t s = m0; s < end;) {
-            const int64_t e = wave_first(a.slot_id[s]);
+        for (int s = w.m0; s < end;) {
+            const int e = (int)wave_first(a.slot_id[s]);
             if (e < 0 || e >= a.adapters) break;   // (rows without an adapter come last)
-            const int64_t e_end = wave_first(a.adapter_ptr[e + 1]);
+            const int e_end = (int)wave_first(a.adapter_ptr[e + 1]);
             const int rank = a.ranks ? min(max(a.ranks[e], 0), a.rank) : a.rank;
-            const T *b = static_cast<const T *>(a.b) + e * a.stride_b, *h = static_cast<const T *>(a.h);
-            for (int p0 = 0; p0 < wide_h && rank > 0; p0 += STEP<T>) {
+            const T *b = static_cast<const T *>(a.b) + (int64_t)e * a.stride_b, *h = static_cast<const T *>(a.h);
+            for (int p0 = 0; p0 < wide_h && rank > 0; p0 += STEP_C) {
                 uint4 xl[TL::LOADS], xr[TR::LOADS];
 #pragma unroll
                 for (int i = 0; i < TL::LOADS; ++i) {
-                    const int p = p0 + TL::piece_of(i) * PIECE<T>;
-                    const int64_t line = min(m0 + TL::line_of(i), end - 1);
+                    const int p = p0 + TL::piece_of(tid, i) * PIECE<T>;
+                    const int64_t line = min(w.m0 + TL::line_of(tid, i), end - 1);
                     xl[i] = load_piece(h + line * wide_h + p, p < wide_h ? PIECE<T> : 0);
                 }
 #pragma unroll
                 for (int i = 0; i < TR::LOADS; ++i) {
-                    const int p = p0 + TR::piece_of(i) * PIECE<T>, q = p % a.rank_up;
-                    const int64_t line = min(n0 + TR::line_of(i), a.n - 1);
+                    const int p = p0 + TR::piece_of(tid, i) * PIECE<T>, q = p % a.rank_up;
+                    const int64_t line = min(w.n0 + TR::line_of(tid, i), (int)a.n - 1);
                     xr[i] = load_piece(b + line * a.ldb + q, p < wide_h ? rank - q : 0);
                 }
                 __syncthreads();
 #pragma unroll
-                for (int i = 0; i < TL::LOADS; ++i) *reinterpret_cast<uint4 *>(lds + (i * THREADS + threadIdx.x) * 16) = xl[i];
+                for (int i = 0; i < TL::LOADS; ++i) *reinterpret_cast<uint4 *>(lds + (i * THREADS + tid) * 16) = xl[i];
 #pragma unroll
-                for (int i = 0; i < TR::LOADS; ++i) *reinterpret_cast<uint4 *>(lds + TL::BYTES + (i * THREADS + threadIdx.x) * 16) = xr[i];
+                for (int i = 0; i < TR::LOADS; ++i) *reinterpret_cast<uint4 *>(lds + TL::BYTES + (i * THREADS + tid) * 16) = xr[i];
                 __syncthreads();
-                Frag<T> fr[2][TN];
+                Frag<T> fr[HALVES][TN];
 #pragma unroll
-                for (int half = 0; half < 2; ++half)
+                for (int half = 0; half < HALVES; ++half)
 #pragma unroll
-                    for (int j = 0; j < TN; ++j) fr[half][j] = TR::read(lds + TL::BYTES, wn, j, half);
+                    for (int j = 0; j < TN; ++j) fr[half][j] = TR::read(lds + TL::BYTES, at_r, j, half);
 #pragma unroll
                 for (int i = 0; i < TM; ++i) {
-                    const int64_t row = m0 + wm + i * 16 + r;
+                    const int row = w.m0 + wm + i * 16 + r;
                     const bool mine = row >= s && row < e_end;
                     if (!__any(mine)) continue;
                     f32x4 sum[TN] = {};
                     const float back = mine ? a.row_scale[row] : 0.0f;
 #pragma unroll
-                    for (int half = 0; half < 2; ++half) {
-                        const Frag<T> fl = TL::read(lds, wm, i, half);
+                    for (int half = 0; half < HALVES; ++half) {
+                        const Frag<T> fl = TL::read(lds, at_l, i, half);
 #pragma unroll
                         for (int j = 0; j < TN; ++j) mma(sum[j], fr[half][j], fl);
                     }
@@ -437,62 +607,45 @@ __global__ void __launch_bounds__(WAVES_M * WAVES_N * WAVE, 2) k_gmm(GmmArgs a, 
             s = e_end > s ? e_end : s + 1;
         }
     }
-
-    constexpr int OP = PIECE<O>;
-    const bool wide = a.ldo % OP == 0 && reinterpret_cast<uintptr_t>(out) % 16 == 0;
-#pragma unroll
-    for (int i = 0; i < TM; ++i) {
-        const int64_t row = m0 + wm + i * 16 + r;
-        if (row >= hi) continue;
-        bool zero = false;
-        int64_t at = row;
-        if (!DEPTH && a.index) {
-            const int64_t x_row = a.index[row];
-            zero = (uint64_t)x_row >= (uint64_t)a.index_rows;
-            if (MODE == GM_EXPAND) {
-                if (zero) continue;
-                at = x_row;
-            }
-        }
-#pragma unroll
-        for (int b = 0; b < TN / 4; ++b) {
-            const int64_t col = n0 + wn + b * 64 + g * 16;
-            O v[16];
-#pragma unroll
-            for (int j = 0; j < 4; ++j)
-#pragma unroll
-                for (int k = 0; k < 4; ++k) v[j * 4 + k] = (O)(zero ? 0.0f : acc[i][b * 4 + j][k]);
-            O *p = out + at * a.ldo + col;
-#pragma unroll
-            for (int j = 0; j < 16; j += OP) {
-                if (wide && col + j + OP <= a.n) {
-                    Vec<O, OP> o;
-#pragma unroll
-                    for (int k = 0; k < OP; ++k) o.e[k] = v[j + k];
-                    *reinterpret_cast<Vec<O, OP> *>(p + j) = o;
-                } else {
-#pragma unroll
-                    for (int k = 0; k < OP; ++k)
-                        if (col + j + k < a.n) p[j + k] = v[j + k];
-                }
-            }
-        }
-    }
+    store(w, acc);
 }
 
 inline int64_t up8(int64_t n) { return (n + 7) & ~(int64_t)7; }
 
-template <class T, bool LCOL, bool RCOL, int BM, int BN, int WAVES_M, int WAVES_N, bool ASYNC, GmmMode MODE, class O = T>
+template <class T, bool LCOL, bool RCOL, int BM, int BN, int WAVES_M, int WAVES_N, bool ASYNC, int STAGES, GmmMode MODE, class O = T>
 hipError_t launch_gmm(const GmmArgs &a, hipStream_t s)
 {
     const int64_t nt = (a.n + BN - 1) / BN;
     const int64_t mt = MODE == GM_DEPTH ? (a.m + BM - 1) / BM : MODE == GM_EXPAND ? (a.rows + BM - 1) / BM : a.rows / BM + std::min(a.groups, a.rows) + 1;
-    const int64_t blocks = up8(mt * nt * (MODE == GM_DEPTH ? a.groups : MODE == GM_SHRINK ? (a.c + a.c_part - 1) / a.c_part : 1));
+    // (GM_ROWS: the last 8 at least have no tile and clear the rows of no group)
+    const int64_t blocks = (MODE == GM_ROWS ? 8 : 0) + up8(mt * nt * (MODE == GM_DEPTH ? a.groups : MODE == GM_SHRINK ? (a.c + a.c_part - 1) / a.c_part : 1));
     constexpr int threads = WAVES_M * WAVES_N * WAVE;
     if (blocks * threads >= (1ll << 32)) return hipErrorInvalidConfiguration;
-    hipLaunchKernelGGL((k_gmm<T, LCOL, RCOL, BM, BN, WAVES_M, WAVES_N, ASYNC, MODE, O>), dim3((uint32_t)blocks), dim3(threads), 0, s, a, mt, nt);
+    hipLaunchKernelGGL((k_gmm<T, LCOL, RCOL, BM, BN, WAVES_M, WAVES_N, ASYNC, STAGES, MODE, O>), dim3((uint32_t)blocks), dim3(threads), 0, s, a, (int)mt, (int)nt);
     return hipGetLastError();
 }
+
+// The largest tile that still gives every compute unit work: 256 x 256 (one workgroup a unit) from 256 tiles on, 128 x 128 (two) from
+// 512, 64 x 128 from 256, else 64 x 64.  Eight products of 512 x 4096 by 4096 x 1024 (bfloat16; 64, 256, 512, 1024 tiles) take 117, 65, 54
+// and 73 us, 32 of 256 x 2048 by 2048 x 2048 (256, 1024, 2048, 4096 tiles) 99, 114, 132 and 166.
+// m_tiles(lines): about how many tiles of that many lines there are.
+template <class T, bool LCOL, bool RCOL, GmmMode MODE, class F> hipError_t launch_tiles(const GmmArgs &a, F m_tiles, bool aligned, hipStream_t s)
+{
+    auto tiles = [&](int64_t bm, int64_t bn) { return m_tiles(bm) * ((a.n + bn - 1) / bn); };
+    if (!aligned) {
+        if (tiles(128, 128) >= 512) return launch_gmm<T, LCOL, RCOL, 128, 128, 2, 2, false, 2, MODE>(a, s);
+        return launch_gmm<T, LCOL, RCOL, 64, 64, 4, 1, false, 2, MODE>(a, s);
+    }
+    if constexpr (sizeof(T) == 2) {
+        if (tiles(256, 256) >= 256) return launch_gmm<T, LCOL, RCOL, 256, 256, 2, 4, true, 2, MODE>(a, s);
+    }
+    if (tiles(128, 128) >= 512) return launch_gmm<T, LCOL, RCOL, 128, 128, 2, 2, true, 2, MODE>(a, s);
+    if (tiles(64, 128) >= 256) return launch_gmm<T, LCOL, RCOL, 64, 128, 2, 2, true, 3, MODE>(a, s);
+    return launch_gmm<T, LCOL, RCOL, 64, 64, 4, 1, true, 4, MODE>(a, s);
+}
+
+// Whether the places of an operand's pieces fit the 32-bit offsets of Feed: `lines` lines of `ld` elements from its base.
+bool offsets_fit(int64_t lines, int64_t ld, int size) { return lines * ld * size < (1ll << 32) - 65536; }
 
 bool pieces_aligned(const void *p, int64_t ld, int64_t stride, int size)
 {

@@ -1,18 +1,83 @@
 // Products of ragged groups of rows with their group's matrix, and the gradient of the matrices.
-#include "gmm.hpp"
+#include "few.hpp"
 
 namespace ocean {
 
 namespace {
 
+// Groups of few rows: workgroup (x, y) has columns 16 TN x .. of the y-th group that has any rows, all of its rows: 16, 32 or 64 at a time.
+constexpr int FEW_ROWS = 64;
+template <class T, bool RCOL, int TN, int WAVES, bool ALIGNED>
+__global__ void __launch_bounds__(WAVES * WAVE, 2) k_few(GmmArgs a)
+{
+    constexpr int SUMS = WAVES * FEW_ROWS * (TN * 16 + 4) * 4, RINGS = RCOL ? WAVES * FEW_RING * FEW_STAGE : 0;
+    __shared__ __align__(16) char s_lds[SUMS > RINGS ? SUMS : RINGS];
+    __shared__ int64_t s_row[FEW_ROWS];
+    int group, lo, hi, groups = 0;
+    const int64_t n0 = (int64_t)blockIdx.x * TN * 16;
+    T *out = static_cast<T *>(a.out);
+    auto item_of = [&](int n) { groups = n; return (int)blockIdx.y; };
+    if (!find_tile(a, 0x7fffffff, item_of, group, lo, hi)) {
+        clear_outside<T>(a, n0, min((int64_t)TN * 16, a.n - n0), blockIdx.y - groups, gridDim.y - groups);
+        return;
+    }
+    const T *x = static_cast<const T *>(a.l), *w = static_cast<const T *>(a.r) + (int64_t)group * a.stride;
+    for (int64_t m0 = lo; m0 < hi; m0 += FEW_ROWS) {
+        const int rows = (int)min((int64_t)FEW_ROWS, hi - m0);
+        __syncthreads();
+        if ((int)threadIdx.x < rows) {
+            const int64_t row = a.index ? a.index[m0 + threadIdx.x] : m0 + threadIdx.x;
+            s_row[threadIdx.x] = (uint64_t)row < (uint64_t)a.index_rows ? row : -1;
+        }
+        __syncthreads();
+        auto store = [&](int row, int64_t col, float v) { out[(m0 + row) * a.ldo + col] = (T)(s_row[row] < 0 ? 0.0f : v); };
+        auto tile = [&](auto tm) {
+            constexpr int TM = decltype(tm)::value;
+            if constexpr (RCOL) few_tile_col<T, TM, WAVES>(x, a.ldl, s_row, rows, w, a.ldr, n0, a.n, a.c, s_lds, store);
+            else few_tile<T, TM, TN, WAVES, ALIGNED>(x, a.ldl, s_row, rows, w, a.ldr, n0, a.n, a.c, reinterpret_cast<float *>(s_lds), store);
+        };
+        if (rows <= 16) tile(std::integral_constant<int, 1>{});
+        else if (rows <= 32) tile(std::integral_constant<int, 2>{});
+        else tile(std::integral_constant<int, 4>{});
+    }
+}
+
+template <class T, bool RCOL, int TN, int WAVES, bool ALIGNED> hipError_t launch_few(const GmmArgs &a, hipStream_t s)
+{
+    const dim3 grid((uint32_t)((a.n + TN * 16 - 1) / (TN * 16)), (uint32_t)std::min(a.groups, a.rows) + 1);
+    hipLaunchKernelGGL((k_few<T, RCOL, TN, WAVES, ALIGNED>), grid, dim3(WAVES * WAVE), 0, s, a);
+    return hipGetLastError();
+}
+
+// Groups of at most this many rows on the average go to k_few.  Weights whose lines lie along c: eight of 4096 x 1024 (bfloat16) take 24 us
+// with 32 rows each and 31 with 48 there, 26 with 64 in tiles of 64 x 64; two of 4096 x 8192 36 and 44 us, and 32.  Across c: 28, 34 and 50
+// us, and 35, 42 and 58.
+constexpr int64_t few_average(bool col) { return col ? 48 : 24; }
+
+// Columns of a workgroup.  64: wide enough that the rows, which every workgroup reads, are read half as often (32 matrices of 2048 x 2048
+// with 32 rows each: 72 us, 78 with 32 columns), if they are many or c is short; 16 and twice the waves: where 32 would
+// leave compute units without work (eight of 4096 x 1024, 8 rows: 16 us, 20 with 32 columns, 24 with 64).
+template <class T, bool RCOL> hipError_t launch_few_rows(const GmmArgs &a, int64_t groups, bool aligned, hipStream_t s)
+{
+    if constexpr (RCOL) {
+        return launch_few<T, true, 4, 4, true>(a, s);
+    } else {
+        const bool many = a.rows > 16 * groups;
+        if ((many || a.c * sizeof(T) <= 1024) && groups * ((a.n + 63) / 64) >= 256)
+            return aligned ? launch_few<T, false, 4, 4, true>(a, s) : launch_few<T, false, 4, 4, false>(a, s);
+        if (!many && groups * ((a.n + 31) / 32) < 512) return aligned ? launch_few<T, false, 1, 8, true>(a, s) : launch_few<T, false, 1, 8, false>(a, s);
+        return aligned ? launch_few<T, false, 2, 4, true>(a, s) : launch_few<T, false, 2, 4, false>(a, s);
+    }
+}
+
 template <class T, bool LCOL, bool RCOL, GmmMode MODE> hipError_t pick_tile(const GmmArgs &a, bool aligned, hipStream_t s)
 {
-    if constexpr (sizeof(T) == 2) {
-        const int64_t rows = MODE == GM_DEPTH ? a.m : a.rows / std::max<int64_t>(a.groups, 1);
-        if (aligned && rows >= 256 && a.n >= 256) return launch_gmm<T, LCOL, RCOL, 256, 256, 2, 4, true, MODE>(a, s);
+    const int64_t groups = MODE == GM_DEPTH ? a.groups : std::min(a.groups, a.rows);
+    if constexpr (MODE == GM_ROWS) {
+        if (groups > 0 && groups < 65535 && a.rows <= groups * few_average(RCOL) && (!RCOL || aligned)) return launch_few_rows<T, RCOL>(a, groups, aligned, s);
     }
-    if (aligned) return launch_gmm<T, LCOL, RCOL, 128, 128, 2, 2, true, MODE>(a, s);
-    return launch_gmm<T, LCOL, RCOL, 128, 128, 2, 2, false, MODE>(a, s);
+    return launch_tiles<T, LCOL, RCOL, MODE>(a, [&](int64_t bm) { return MODE == GM_DEPTH ? groups * ((a.m + bm - 1) / bm) : std::max(groups, a.rows / bm); },
+                                             aligned, s);
 }
 
 }  // namespace
@@ -29,8 +94,11 @@ hipError_t launch_grouped_matmul(const ocean_groups &g, int dtype, int64_t inner
     a.ptr = g.group_ptr, a.groups = g.experts, a.rows = g.rows;
     a.n = outer, a.c = inner;
     a.index = g.row_index, a.index_rows = g.x_rows;
+    if (!g.row_index) a.index_rows = g.rows;
     if (g.x_rows == 0 || inner == 0) a.c = 0, a.index_rows = 0, a.index = nullptr;
-    const bool aligned = pieces_aligned(x, ldx, 0, size) && pieces_aligned(w, ldw, stride, size) && inner % e == 0 && (!transposed || outer % e == 0);
+    // (the rows of a tile lie within 256 lines, gathered ones anywhere in x)
+    const bool aligned = pieces_aligned(x, ldx, 0, size) && pieces_aligned(w, ldw, stride, size) && inner % e == 0 && (!transposed || outer % e == 0) &&
+                         offsets_fit(g.row_index ? std::max<int64_t>(g.x_rows, 256) : 256, ldx, size) && offsets_fit(256, ldw, size);
     return with_type(dtype, [&](auto t) {
         using T = decltype(t);
         return transposed ? pick_tile<T, false, true, GM_ROWS>(a, aligned, s) : pick_tile<T, false, false, GM_ROWS>(a, aligned, s);
@@ -51,7 +119,8 @@ hipError_t launch_grouped_weight_grad(const ocean_groups &g, int dtype, int64_t 
     a.m = transposed ? inner : outer, a.n = transposed ? outer : inner;
     a.index = g.row_index, a.index_rows = g.x_rows, a.index_on_r = transposed ? 0 : 1;
     if (g.x_rows == 0) a.rows = 0;   // (nothing to add up)
-    const bool aligned = pieces_aligned(x, ldx, 0, size) && pieces_aligned(dy, lddy, 0, size) && inner % e == 0 && outer % e == 0;
+    const bool aligned = pieces_aligned(x, ldx, 0, size) && pieces_aligned(dy, lddy, 0, size) && inner % e == 0 && outer % e == 0 &&
+                         offsets_fit(256, ldx, size) && offsets_fit(256, lddy, size);
     return with_type(dtype, [&](auto t) { return pick_tile<decltype(t), true, true, GM_DEPTH>(a, aligned, s); });
 }
 

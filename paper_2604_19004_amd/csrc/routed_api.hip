@@ -19,12 +19,12 @@ int launched(hipError_t e, const char *what)
 
 bool known_type(int32_t dtype) { return dtype == OCEAN_F32 || dtype == OCEAN_BF16 || dtype == OCEAN_F16; }
 bool aligned(const void *p, int size) { return reinterpret_cast<uintptr_t>(p) % size == 0; }
-constexpr int64_t MAX_DIM = 1ll << 31;   // rows and widths are below this
+constexpr int64_t MAX_DIM = (1ll << 31) - 4096;   // rows and widths are below this: tiles count in 32 bits
 
 // Null where the matrix is fine: base there (if it has elements), aligned to its type, rows apart.
 const char *matrix_fault(const void *p, int64_t rows, int64_t width, int64_t ld, int dtype)
 {
-    if (rows < 0 || rows >= MAX_DIM || width < 0 || width >= MAX_DIM) return "a matrix's size is negative or 2^31 or more";
+    if (rows < 0 || rows >= MAX_DIM || width < 0 || width >= MAX_DIM) return "a matrix's size is negative or not below 2^31 - 4096";
     if (ld < width || ld >= (1ll << 40)) return "a row stride is less than the row's width";
     if (rows > 0 && width > 0 && !p) return "a matrix is null";
     if (!aligned(p, type_size(dtype))) return "a matrix is not aligned to its type";
