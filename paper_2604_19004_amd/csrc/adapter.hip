@@ -1,8 +1,10 @@
 // A shared projection with a low-rank adapter for each row beside it, adapters of many requests in one batch.
 //
-// Rows are put in the order of their adapters, x * A^T is a product of ragged groups (few columns: c is cut into stretches to fill
+// Few rows: a wave forms four of a row's inner products with its adapter, then a workgroup that has a few columns of the shared projection
+// begins each result with the adapter's part, a dot product over the rank in 32 bits.
+// More: rows are put in the order of their adapters, x * A^T is a product of ragged groups (few columns: c is cut into stretches to fill
 // the chip, the stretches' sums are added up in a fixed order), and the shared projection's tiles go on, after their own c, with the products with B.
-#include "gmm.hpp"
+#include "few.hpp"
 
 namespace ocean {
 
@@ -51,9 +53,26 @@ __global__ void __launch_bounds__(1024) k_order_rows(const int32_t *ids, int64_t
     __shared__ uint32_t s_wave[1024 / WAVE];
     for (int e = threadIdx.x; e <= adapters; e += 1024) s_at[e] = 0;
     __syncthreads();
-    for (int64_t i = threadIdx.x; i < rows; i += 1024) {
-        const uint32_t e = min((uint32_t)ids[i], (uint32_t)adapters);
-        atomicAdd(&s_at[e], 1u);
+    // Rows side by side often have the same adapter: a wave takes the places of up to four of them at once, the others one by one.
+    auto take = [&](bool there, uint32_t e, auto got) {
+        for (int i = 0; i < 4; ++i) {
+            const unsigned long long left = __ballot(there);
+            if (!left) return;
+            const uint32_t first = wave_read_lane_u32(e, __ffsll(left) - 1);
+            const unsigned long long same = __ballot(there && e == first);
+            uint32_t at = 0;
+            if (lane_id() == __ffsll(same) - 1) at = atomicAdd(&s_at[first], (uint32_t)__popcll(same));
+            at = wave_read_lane_u32(at, __ffsll(same) - 1);
+            if (there && e == first) {
+                got(at + (uint32_t)__popcll(same & ((1ull << lane_id()) - 1)));
+                there = false;
+            }
+        }
+        if (there) got(atomicAdd(&s_at[e], 1u));
+    };
+    for (int64_t i0 = 0; i0 < rows; i0 += 1024) {
+        const int64_t i = i0 + threadIdx.x;
+        take(i < rows, i < rows ? min((uint32_t)ids[i], (uint32_t)adapters) : 0u, [](uint32_t) {});
     }
     __syncthreads();
     uint32_t before = 0;
@@ -73,10 +92,13 @@ __global__ void __launch_bounds__(1024) k_order_rows(const int32_t *ids, int64_t
         }
         __syncthreads();
     }
-    for (int64_t i = threadIdx.x; i < rows; i += 1024) {
-        const uint32_t e = min((uint32_t)ids[i], (uint32_t)adapters), at = atomicAdd(&s_at[e], 1u);
-        w.perm[at] = (int32_t)i;
-        w.slot_id[at] = e < (uint32_t)adapters ? (int32_t)e : -1;
+    for (int64_t i0 = 0; i0 < rows; i0 += 1024) {
+        const int64_t i = i0 + threadIdx.x;
+        const uint32_t e = i < rows ? min((uint32_t)ids[i], (uint32_t)adapters) : 0u;
+        take(i < rows, e, [&](uint32_t at) {
+            w.perm[at] = (int32_t)i;
+            w.slot_id[at] = e < (uint32_t)adapters ? (int32_t)e : -1;
+        });
     }
 }
 
@@ -126,6 +148,120 @@ __global__ void __launch_bounds__(256) k_finish_shrink(AdapterSpace w, int64_t r
     }
 }
 
+// Few rows.  h[row][r .. r + 3] = scale * x[row] * A^T, one wave each; nothing for rows without an adapter and behind its rank.
+constexpr int FEW_R = 4;
+template <class T, bool ALIGNED>
+__global__ void __launch_bounds__(256) k_shrink_few(ocean_adapters l, const int32_t *ids, const T *x, int64_t ldx, int64_t inner, int64_t rows,
+                                                    float *h, int rank_up)
+{
+    const int parts = (int)((l.rank + FEW_R - 1) / FEW_R), lane = lane_id();
+    const int64_t item = (int64_t)blockIdx.x * (256 / WAVE) + threadIdx.x / WAVE;
+    if (item >= rows * parts) return;
+    const int64_t row = item / parts;
+    const int r0 = (int)(item - row * parts) * FEW_R;
+    const int64_t id = ids[row];
+    if ((uint64_t)id >= (uint64_t)l.adapters) return;
+    const int used = l.ranks ? (int)min((int64_t)l.ranks[id], l.rank) : (int)l.rank;
+    if (r0 >= used) return;
+    const T *xr = x + row * ldx, *ar[FEW_R];
+#pragma unroll
+    for (int j = 0; j < FEW_R; ++j) ar[j] = static_cast<const T *>(l.a) + id * l.stride_a + min(r0 + j, used - 1) * l.ld_a;
+    constexpr int P = PIECE<T>;
+    float sum[FEW_R] = {};
+#pragma unroll 2
+    for (int64_t c = lane * P; c < inner; c += WAVE * P) {
+        const Frag<T> v = few_load<T, ALIGNED>(xr + c, inner - c);
+#pragma unroll
+        for (int j = 0; j < FEW_R; ++j) {
+            const Frag<T> a = few_load<T, ALIGNED>(ar[j] + c, inner - c);
+#pragma unroll
+            for (int i = 0; i < P; ++i) sum[j] += (float)v[i] * (float)a[i];
+        }
+    }
+#pragma unroll
+    for (int j = 0; j < FEW_R; ++j) {
+        const float v = wave_sum(sum[j]);
+        if (lane == 0 && r0 + j < used) h[row * rank_up + r0 + j] = l.scale ? v * l.scale[id] : v;
+    }
+}
+
+// The shared projection of 16, 32 or 64 rows (blockIdx.y-th 64) and TN * 16 columns, each result begun with the adapter's part.
+constexpr int FEW_ROWS = 64;
+constexpr int64_t FEW_ROWS_MOST = 128;   // (64 adapters of rank 16, 4096 x 4096: 128 rows 39 us, in tiles 63; 192 61 and 61)
+template <class T, int TN, int WAVES, bool ALIGNED>
+__global__ void __launch_bounds__(WAVES * WAVE, 2) k_adapter_few(ocean_adapters l, const int32_t *ids, const T *x, int64_t ldx, int64_t inner, int64_t rows,
+                                                                 const T *w, int64_t ldw, int64_t outer, T *y, int64_t ldy, const float *h, int rank_up)
+{
+    __shared__ __align__(16) float s_sum[WAVES * FEW_ROWS * (TN * 16 + 4)];
+    __shared__ int64_t s_row[FEW_ROWS];
+    __shared__ int32_t s_id[FEW_ROWS], s_used[FEW_ROWS];
+    const int64_t m0 = (int64_t)blockIdx.y * FEW_ROWS, n0 = (int64_t)blockIdx.x * TN * 16;
+    const int count = (int)min((int64_t)FEW_ROWS, rows - m0);
+    if ((int)threadIdx.x < count) {
+        const int64_t id = ids[m0 + threadIdx.x];
+        const bool has = (uint64_t)id < (uint64_t)l.adapters;
+        s_row[threadIdx.x] = m0 + threadIdx.x;
+        s_id[threadIdx.x] = has ? (int32_t)id : 0;
+        s_used[threadIdx.x] = !has ? 0 : l.ranks ? (int)min((int64_t)l.ranks[id], l.rank) : (int)l.rank;
+    }
+    __syncthreads();
+    auto first = [&](int row, int64_t col) {
+        const int used = s_used[row];
+        float v = 0.0f;
+        if (used > 0) {
+            const T *b = static_cast<const T *>(l.b) + (int64_t)s_id[row] * l.stride_b + col * l.ld_b;
+            const float *hr = h + (m0 + row) * rank_up;
+#pragma unroll 4
+            for (int r = 0; r < used; r += PIECE<T>) {
+                const Frag<T> p = __builtin_bit_cast(Frag<T>, load_piece(b + r, used - r));
+#pragma unroll
+                for (int i = 0; i < PIECE<T>; ++i)
+                    if (r + i < used) v += hr[r + i] * (float)p[i];
+            }
+        }
+        return v;
+    };
+    auto store = [&](int row, int64_t col, float v) { y[(m0 + row) * ldy + col] = (T)v; };
+    auto tile = [&](auto tm) {
+        few_tile<T, decltype(tm)::value, TN, WAVES, ALIGNED>(x, ldx, s_row, count, w, ldw, n0, outer, inner, s_sum, first, store);
+    };
+    if (count <= 16) tile(std::integral_constant<int, 1>{});
+    else if (count <= 32) tile(std::integral_constant<int, 2>{});
+    else tile(std::integral_constant<int, 4>{});
+}
+
+template <class T>
+hipError_t launch_few_rows(const ocean_adapters &l, const int32_t *ids, int64_t rows, int64_t inner, int64_t outer, const T *x, int64_t ldx, const T *w,
+                           int64_t ldw, T *y, int64_t ldy, float *h, int rank_up, bool none, hipStream_t s)
+{
+    const int size = sizeof(T);
+    ocean_adapters used = l;
+    if (none) used.adapters = 0;
+    if (!none) {
+        const bool aligned = pieces_aligned(x, ldx, 0, size) && pieces_aligned(l.a, l.ld_a, l.stride_a, size) && inner % PIECE<T> == 0;
+        const dim3 grid((uint32_t)((rows * ((l.rank + FEW_R - 1) / FEW_R) + 3) / 4));
+        if (aligned) hipLaunchKernelGGL((k_shrink_few<T, true>), grid, dim3(256), 0, s, used, ids, x, ldx, inner, rows, h, rank_up);
+        else hipLaunchKernelGGL((k_shrink_few<T, false>), grid, dim3(256), 0, s, used, ids, x, ldx, inner, rows, h, rank_up);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    const bool aligned = pieces_aligned(x, ldx, 0, size) && pieces_aligned(w, ldw, 0, size) && inner % PIECE<T> == 0;
+    auto launch = [&](auto tn, auto waves, auto al) {
+        constexpr int TN = decltype(tn)::value, WAVES = decltype(waves)::value;
+        const dim3 grid((uint32_t)((outer + TN * 16 - 1) / (TN * 16)), (uint32_t)((rows + FEW_ROWS - 1) / FEW_ROWS));
+        hipLaunchKernelGGL((k_adapter_few<T, TN, WAVES, decltype(al)::value>), grid, dim3(WAVES * WAVE), 0, s, used, ids, x, ldx, inner, rows, w, ldw,
+                           outer, y, ldy, h, rank_up);
+        return hipGetLastError();
+    };
+    const std::integral_constant<int, 1> one{};
+    const std::integral_constant<int, 2> two{};
+    const std::integral_constant<int, 8> eight{};
+    // Columns of a workgroup: every one reads all rows, and all compute units should have one (64 adapters of rank 16, 4096 x 4096: 32 rows 23
+    // us with 16 columns and 27 with 32, 96 rows 42 and 38; 4096 x 1024, 48 rows 37 and 48).
+    if (rows > 64 && outer >= 4096) return aligned ? launch(two, eight, std::true_type{}) : launch(two, eight, std::false_type{});
+    return aligned ? launch(one, eight, std::true_type{}) : launch(one, eight, std::false_type{});
+}
+
 }  // namespace
 
 size_t adapter_workspace(int64_t rows, int64_t inner, int64_t outer, int64_t adapters, int64_t rank, int dtype)
@@ -142,6 +278,13 @@ hipError_t launch_adapter(const ocean_adapters &l, const int32_t *ids, int dtype
     const int64_t adapters = none ? 0 : l.adapters;
     const bool x_fits = offsets_fit(std::max<int64_t>(rows, 256), ldx, size);
     const AdapterSpace sp = adapter_space(workspace, rows, inner, l.adapters, l.rank, dtype);
+    if (rows <= FEW_ROWS_MOST) {
+        return with_type(dtype, [&](auto t) {
+            using T = decltype(t);
+            return launch_few_rows(l, ids, rows, inner, outer, static_cast<const T *>(x), ldx, static_cast<const T *>(w), ldw, static_cast<T *>(y), ldy,
+                                   sp.part, sp.rank_up, none, s);
+        });
+    }
     hipLaunchKernelGGL(k_order_rows, dim3(1), dim3(1024), 0, s, ids, rows, (int)adapters, sp);
     hipError_t err = hipGetLastError();
     if (err != hipSuccess) return err;
@@ -167,7 +310,7 @@ hipError_t launch_adapter(const ocean_adapters &l, const int32_t *ids, int dtype
         }
         a.r = w, a.ldr = ldw, a.stride = 0;
         a.out = y, a.ldo = ldy, a.n = outer;
-        a.slot_id = sp.slot_id, a.adapter_ptr = sp.ptr, a.adapters = adapters;
+        a.slot_id = sp.slot_id, a.adapters = adapters;
         a.h = sp.h, a.row_scale = sp.row_scale, a.b = l.b, a.ldb = l.ld_b, a.stride_b = l.stride_b, a.ranks = l.ranks, a.rank = rank, a.rank_up = sp.rank_up;
         const bool aligned = pieces_aligned(x, ldx, 0, size) && pieces_aligned(w, ldw, 0, size) && inner % e == 0 && x_fits && offsets_fit(256, ldw, size);
         return launch_tiles<T, false, false, GM_EXPAND>(a, [&](int64_t bm) { return (rows + bm - 1) / bm; }, aligned, s);

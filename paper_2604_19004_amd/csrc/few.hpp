@@ -19,7 +19,8 @@ template <class T, bool ALIGNED> __device__ __forceinline__ Frag<T> few_load(con
 
 // The waves' sums meet: [wave][row][column], a line of columns padded by four so that rows lie on different banks.
 template <class T, int TM, int TN, int WAVES, class Store>
-__device__ __forceinline__ void few_finish(const f32x4 (&acc)[TM][TN], int rows, int64_t n0, int64_t n, float *lds, Store store)
+__device__ __forceinline__ void few_finish(const f32x4 (&acc)[TM][TN], const float (&first)[(TM * TN * 256 + WAVES * WAVE - 1) / (WAVES * WAVE)], int rows,
+                                           int64_t n0, int64_t n, float *lds, Store store)
 {
     const int lane = lane_id(), r = lane % 16, g = lane / 16, wave = threadIdx.x / WAVE;
     constexpr int COLS = TN * 16, LD = COLS + 4;
@@ -29,21 +30,36 @@ __device__ __forceinline__ void few_finish(const f32x4 (&acc)[TM][TN], int rows,
 #pragma unroll
         for (int j = 0; j < TN; ++j) *reinterpret_cast<f32x4 *>(lds + (wave * TM * 16 + i * 16 + r) * LD + j * 16 + g * 4) = acc[i][j];
     __syncthreads();
-    for (int k = threadIdx.x; k < rows * COLS; k += WAVES * WAVE) {
-        const int row = k / COLS, col = k % COLS;
+#pragma unroll
+    for (int o = 0; o < (TM * TN * 256 + WAVES * WAVE - 1) / (WAVES * WAVE); ++o) {
+        const int k = o * WAVES * WAVE + threadIdx.x, row = k / COLS, col = k % COLS;
+        if (row >= rows || n0 + col >= n) continue;
         float v = 0.0f;
 #pragma unroll
         for (int s = 0; s < WAVES; ++s) v += lds[(s * TM * 16 + row) * LD + col];
-        if (n0 + col < n) store(row, n0 + col, v);
+        store(row, n0 + col, v + first[o]);
+    }
+}
+
+// What is added to the products of this thread's results, worked out before they are (its loads are under way with theirs).
+template <int TM, int TN, int WAVES, class First>
+__device__ __forceinline__ void few_first(float (&first)[(TM * TN * 256 + WAVES * WAVE - 1) / (WAVES * WAVE)], int rows, int64_t n0, int64_t n, First f)
+{
+#pragma unroll
+    for (int o = 0; o < (TM * TN * 256 + WAVES * WAVE - 1) / (WAVES * WAVE); ++o) {
+        const int k = o * WAVES * WAVE + threadIdx.x, row = k / (TN * 16), col = k % (TN * 16);
+        first[o] = row < rows && n0 + col < n ? f(row, n0 + col) : 0.0f;
     }
 }
 
 // The workgroup's columns, n0 .. n0 + 16 TN - 1, of `rows` rows (1 .. 16 TM), numbers row_of[] of x (-1: what comes of it is not
-// used).  store(row, column, sum) is called once for each of them that there is.
-template <class T, int TM, int TN, int WAVES, bool ALIGNED, class Store>
+// used).  store(row, column, sum) is called once for each of them that there is; the sum begins with first(row, column).
+template <class T, int TM, int TN, int WAVES, bool ALIGNED, class First, class Store>
 __device__ __forceinline__ void few_tile(const T *x, int64_t ldx, const int64_t *row_of, int rows, const T *w, int64_t ldw, int64_t n0, int64_t n,
-                                         int64_t c, float *lds, Store store)
+                                         int64_t c, float *lds, First f, Store store)
 {
+    float first[(TM * TN * 256 + WAVES * WAVE - 1) / (WAVES * WAVE)];
+    few_first<TM, TN, WAVES>(first, rows, n0, n, f);
     const int lane = lane_id(), r = lane % 16, g = lane / 16, wave = threadIdx.x / WAVE;
     constexpr int S = STEP<T>, P = PIECE<T>, UNROLL = TM + TN <= 3 ? 4 : 2;
     const T *xp[TM], *wp[TN];
@@ -90,58 +106,31 @@ __device__ __forceinline__ void few_tile(const T *x, int64_t ldx, const int64_t 
                 for (int j = 0; j < TN; ++j) mma(acc[i][j], fw[j], fx[i]);
         }
     }
-    few_finish<T, TM, TN, WAVES>(acc, rows, n0, n, lds, store);
+    few_finish<T, TM, TN, WAVES>(acc, first, rows, n0, n, lds, store);
 }
 
 // The same where a line of the right matrix is one c (its columns lie side by side, aligned to 16 bytes).  The matrix cores want 8
 // (4) c of one column in a lane, so the lines pass through LDS, which gives them back transposed: each wave has a ring of RING pieces of its own,
 // 4 KB (32 or 16 lines of 64 columns) each, filled straight from memory RING - 1 ahead; no wave waits for another.  `lds` holds
 // the rings, then the sums.
-constexpr int FEW_COLS = 64, FEW_RING = 4, FEW_STAGE = 4096;   // (RING: the most; the rows' fragments of as many stages are in registers)
-template <class T> __device__ __forceinline__ Frag<T> few_read(const char *stage, int j)
-{
-    const int lane = lane_id(), r = lane % 16, g = lane / 16;
-    constexpr int LINE_BYTES = FEW_COLS * sizeof(T);
-    if constexpr (sizeof(T) == 2) {
-        const int col = j * 16 + (r % 4) * 4;
-        s16x8 v;
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            const int c = g * 8 + h * 4 + r / 4;
-            const s16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-                (__attribute__((address_space(3))) s16x4 *)(stage + c * LINE_BYTES + (((col / 8) ^ col_xor<T, FEW_COLS / PIECE<T>>(c)) * 16) + (col % 8) * 2));
-#pragma unroll
-            for (int i = 0; i < 4; ++i) v[h * 4 + i] = x[i];
-        }
-        return __builtin_bit_cast(Frag<T>, v);
-    } else {
-        const int col = j * 16 + r;
-        f32x4 v;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int c = g * 4 + i;
-            v[i] = *reinterpret_cast<const float *>(stage + c * LINE_BYTES + (((col / 4) ^ col_xor<T, FEW_COLS / PIECE<T>>(c)) * 16) + (col % 4) * 4);
-        }
-        return v;
-    }
-}
+constexpr int FEW_COLS = 64, FEW_RING = 4, FEW_STAGE = 4096;
 template <class T, int TM, int WAVES, class Store>
 __device__ __forceinline__ void few_tile_col(const T *x, int64_t ldx, const int64_t *row_of, int rows, const T *w, int64_t ldw, int64_t n0, int64_t n,
                                              int64_t c, char *lds, Store store)
 {
     const int lane = lane_id(), r = lane % 16, g = lane / 16, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE);
-    constexpr int RING = TM > 2 ? FEW_RING - 1 : FEW_RING;
-    constexpr int P = PIECE<T>, LINES = STEP<T> / 2, PIECES = FEW_COLS / P, LOADS = FEW_STAGE / 16 / WAVE, TN = FEW_COLS / 16;
-    char *ring = lds + wave * RING * FEW_STAGE;
+    constexpr int P = PIECE<T>, LINES = STEP<T> / 2, LOADS = FEW_STAGE / 16 / WAVE, TN = FEW_COLS / 16;
+    char *ring = lds + wave * FEW_RING * FEW_STAGE;
+    using Stage = Tile<T, true, false, FEW_COLS, WAVE, 64>;
+    const uint32_t at_w = Stage::place(0);
     const T *xp[TM], *wp[LOADS];
     int line[LOADS];
 #pragma unroll
     for (int i = 0; i < TM; ++i) xp[i] = x + max(row_of[min(i * 16 + r, rows - 1)], (int64_t)0) * ldx + g * P;
 #pragma unroll
     for (int i = 0; i < LOADS; ++i) {
-        const int q = i * WAVE + lane;
-        line[i] = q / PIECES;
-        wp[i] = w + line[i] * ldw + min(n0 + ((q % PIECES) ^ col_xor<T, FEW_COLS / PIECE<T>>(line[i])) * P, n - P);
+        line[i] = Stage::line_of(lane, i);
+        wp[i] = w + line[i] * ldw + min(n0 + Stage::piece_of(lane, i) * P, n - P);
     }
     const int64_t stages = (c + LINES - 1) / LINES;                                  // of all waves, taken in turn
     const int64_t mine = stages > wave ? (stages - wave + WAVES - 1) / WAVES : 0;     // of this wave
@@ -154,30 +143,29 @@ __device__ __forceinline__ void few_tile_col(const T *x, int64_t ldx, const int6
         for (int i = 0; i < TM; ++i) fx[i] = few_load<T, true>(xp[i] + c0, c - c0 - g * P);
     };
     f32x4 acc[TM][TN] = {};
-    Frag<T> fx[RING][TM];
+    Frag<T> fx[FEW_RING][TM];
     __syncthreads();
 #pragma unroll
-    for (int k = 0; k < RING - 1; ++k)
+    for (int k = 0; k < FEW_RING - 1; ++k)
         if (k < mine) fill(k, k, fx[k]);
-    for (int64_t k0 = 0; k0 < mine; k0 += RING) {
+    for (int64_t k0 = 0; k0 < mine; k0 += FEW_RING) {
 #pragma unroll
-        for (int u = 0; u < RING; ++u) {
+        for (int u = 0; u < FEW_RING; ++u) {
             const int64_t k = k0 + u;
             if (k >= mine) break;
             // The slot that is filled next was read in the turn before: those reads have come back.
             __builtin_amdgcn_s_waitcnt(0xc07f);   // lgkmcnt(0)
-            const bool more = k + RING - 1 < mine;
-            if (more) fill(k + RING - 1, (u + RING - 1) % RING, fx[(u + RING - 1) % RING]);
-            // Loads come back in order: all but those of the RING - 1 stages behind this one.
+            const bool more = k + FEW_RING - 1 < mine;
+            if (more) fill(k + FEW_RING - 1, (u + FEW_RING - 1) % FEW_RING, fx[(u + FEW_RING - 1) % FEW_RING]);
+            // Loads come back in order: all but those of the FEW_RING - 1 stages behind this one.
             // (Each is one instruction: some lane's c lies before the end.)
-            constexpr int LATER = (RING - 1) * (LOADS + TM);
+            constexpr int LATER = (FEW_RING - 1) * (LOADS + TM);
             asm volatile("" ::: "memory");
             if (more) __builtin_amdgcn_s_waitcnt(0x0f70 | (LATER & 15) | (LATER >> 4) << 14);
             else __builtin_amdgcn_s_waitcnt(0x0f70);
             wave_sync();
             Frag<T> fw[TN];
-#pragma unroll
-            for (int j = 0; j < TN; ++j) fw[j] = few_read<T>(ring + u * FEW_STAGE, j);
+            Stage::template read<0>(ring + u * FEW_STAGE, at_w, fw);
 #pragma unroll
             for (int i = 0; i < TM; ++i)
 #pragma unroll
@@ -185,7 +173,8 @@ __device__ __forceinline__ void few_tile_col(const T *x, int64_t ldx, const int6
             wave_sync();
         }
     }
-    few_finish<T, TM, TN, WAVES>(acc, rows, n0, n, reinterpret_cast<float *>(lds), store);
+    const float first[(TM * TN * 256 + WAVES * WAVE - 1) / (WAVES * WAVE)] = {};
+    few_finish<T, TM, TN, WAVES>(acc, first, rows, n0, n, reinterpret_cast<float *>(lds), store);
 }
 
 }  // namespace

@@ -70,6 +70,37 @@ template <class T, int PIECES> __device__ __forceinline__ int col_xor(int c)
     return PIECES == 8 ? ((c >> 1) & 1) << 1 | ((c >> 3) & 1) << 2 : (c & 3) << 1 | ((c >> 3) & 1) << 3;
 }
 
+// Transposing reads of LDS: each lane names 4 16-bit numbers at `at` + OFFSET, and a group of 16 lanes gets its block of 4 x 16 turned round; the
+// same at OFFSET + NEXT into the upper half of the fragment.  Of N addresses at once, and waited for here: the compiler, which cannot
+// tell the buffers of a pipeline apart, puts a wait for all loads on their way to LDS in front of the builtin (64 us instead of 35 for two
+// products with 4096 x 8192 weights across c, a row each).
+__device__ __forceinline__ uint32_t lds_address(const char *p) { return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const char *)p; }
+template <int OFFSET, int NEXT, int N> __device__ __forceinline__ void read_transposed(const uint32_t (&at)[N], s16x8 (&out)[N])
+{
+    static_assert(N == 1 || N == 2 || N % 4 == 0, "one, two or fours");
+    s16x4 v[2 * N];
+    if constexpr (N == 1) {
+        asm volatile("ds_read_b64_tr_b16 %0, %2 offset:%3\n\tds_read_b64_tr_b16 %1, %2 offset:%4\n\ts_waitcnt lgkmcnt(0)"
+                     : "=&v"(v[0]), "=&v"(v[1]) : "v"(at[0]), "n"(OFFSET), "n"(OFFSET + NEXT) : "memory");
+    } else if constexpr (N == 2) {
+        asm volatile("ds_read_b64_tr_b16 %0, %4 offset:%6\n\tds_read_b64_tr_b16 %1, %4 offset:%7\n\t"
+                     "ds_read_b64_tr_b16 %2, %5 offset:%6\n\tds_read_b64_tr_b16 %3, %5 offset:%7\n\ts_waitcnt lgkmcnt(0)"
+                     : "=&v"(v[0]), "=&v"(v[1]), "=&v"(v[2]), "=&v"(v[3]) : "v"(at[0]), "v"(at[1]), "n"(OFFSET), "n"(OFFSET + NEXT) : "memory");
+    } else {
+#pragma unroll
+        for (int k = 0; k < N; k += 4)
+            asm volatile("ds_read_b64_tr_b16 %0, %8 offset:%12\n\tds_read_b64_tr_b16 %1, %8 offset:%13\n\t"
+                         "ds_read_b64_tr_b16 %2, %9 offset:%12\n\tds_read_b64_tr_b16 %3, %9 offset:%13\n\t"
+                         "ds_read_b64_tr_b16 %4, %10 offset:%12\n\tds_read_b64_tr_b16 %5, %10 offset:%13\n\t"
+                         "ds_read_b64_tr_b16 %6, %11 offset:%12\n\tds_read_b64_tr_b16 %7, %11 offset:%13\n\ts_waitcnt lgkmcnt(0)"
+                         : "=&v"(v[2 * k]), "=&v"(v[2 * k + 1]), "=&v"(v[2 * k + 2]), "=&v"(v[2 * k + 3]), "=&v"(v[2 * k + 4]), "=&v"(v[2 * k + 5]),
+                           "=&v"(v[2 * k + 6]), "=&v"(v[2 * k + 7])
+                         : "v"(at[k]), "v"(at[k + 1]), "v"(at[k + 2]), "v"(at[k + 3]), "n"(OFFSET), "n"(OFFSET + NEXT) : "memory");
+    }
+#pragma unroll
+    for (int k = 0; k < N; ++k) out[k] = __builtin_shufflevector(v[2 * k], v[2 * k + 1], 0, 1, 2, 3, 4, 5, 6, 7);
+}
+
 // One operand's tile of B lines (row) or B columns (col), DEPTH bytes of c, moved by THREADS threads.
 template <class T, bool COL, bool INTER, int B, int THREADS, int DEPTH>
 struct Tile {
@@ -102,28 +133,26 @@ struct Tile {
             return c * (PIECES * 16) + ((col / 4) ^ col_xor<T, PIECES>(c)) * 16 + (col % 4) * 4;
         }
     }
-    // 64 bytes of c (the half-th of DEPTH) of 16 x 16 tile j, as mma takes them.
-    __device__ static Frag<T> read(const char *lds, uint32_t place, int j, int half)
+    // 64 bytes of c (the HALF-th of DEPTH) of 16 x 16 tiles 0 .. N - 1, as mma takes them.
+    template <int HALF, int N> __device__ static void read(const char *lds, uint32_t place, Frag<T> (&out)[N])
     {
         if constexpr (!COL) {
-            return *reinterpret_cast<const Frag<T> *>(lds + (place ^ (half * 64)) + tile_line<INTER>(j, 0) * DEPTH);
+#pragma unroll
+            for (int j = 0; j < N; ++j) out[j] = *reinterpret_cast<const Frag<T> *>(lds + (place ^ (HALF * 64)) + tile_line<INTER>(j, 0) * DEPTH);
         } else if constexpr (sizeof(T) == 2) {
-            const uint32_t at = place ^ (tile_line<INTER>(j, 0) * 2);
-            s16x8 v;
+            uint32_t at[N];
+            s16x8 v[N];
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const s16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-                    (__attribute__((address_space(3))) s16x4 *)(lds + at + (half * 32 + h * 4) * (PIECES * 16)));
+            for (int j = 0; j < N; ++j) at[j] = lds_address(lds) + (place ^ (tile_line<INTER>(j, 0) * 2));
+            read_transposed<HALF * 32 * PIECES * 16, 4 * PIECES * 16>(at, v);
 #pragma unroll
-                for (int i = 0; i < 4; ++i) v[h * 4 + i] = x[i];
-            }
-            return __builtin_bit_cast(Frag<T>, v);
+            for (int j = 0; j < N; ++j) out[j] = __builtin_bit_cast(Frag<T>, v[j]);
         } else {
-            const uint32_t at = place ^ (tile_line<INTER>(j, 0) * 4);
-            f32x4 v;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) v[i] = *reinterpret_cast<const float *>(lds + at + (half * 16 + i) * (PIECES * 16));
-            return v;
+            for (int j = 0; j < N; ++j)
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    out[j][i] = *reinterpret_cast<const float *>(lds + (place ^ (tile_line<INTER>(j, 0) * 4)) + (HALF * 16 + i) * (PIECES * 16));
         }
     }
 };
@@ -161,7 +190,6 @@ struct GmmArgs {
     int index_on_r;            // (GM_DEPTH) x is the right operand
     // adapters: rows in the order of their adapters
     const int32_t *slot_id;    // adapter of each slot, -1: none
-    const int64_t *adapter_ptr;
     int64_t adapters;
     const void *h;             // [rows][parts * rank up to whole pieces]: x * A^T with the scale over row_scale, in the operands' type
     const float *row_scale;
@@ -298,7 +326,7 @@ __global__ void __launch_bounds__(WAVES_M * WAVES_N * WAVE, 2) k_gmm(GmmArgs a, 
 {
     constexpr int THREADS = WAVES_M * WAVES_N * WAVE, WM = BM / WAVES_M, WN = BN / WAVES_N, TM = WM / 16, TN = WN / 16;
     static_assert(RCOL || WN % 64 == 0, "four interleaved tiles");
-    constexpr int BYTES = LINE, STEP_C = BYTES / (int)sizeof(T), HALVES = BYTES / 64;
+    constexpr int BYTES = LINE, STEP_C = BYTES / (int)sizeof(T), HALVES = 2;
     using TL = Tile<T, LCOL, false, BM, THREADS, BYTES>;
     using TR = Tile<T, RCOL, !RCOL, BN, THREADS, BYTES>;
     constexpr int BUFFER = TL::BYTES + TR::BYTES;
@@ -348,6 +376,9 @@ __global__ void __launch_bounds__(WAVES_M * WAVES_N * WAVE, 2) k_gmm(GmmArgs a, 
         w.n0 = ni * BN;
         return true;
     };
+    // (GM_EXPAND) the adapters of the tile's rows, which are in their order, and where their rows begin.
+    __shared__ int s_adapter[MODE == GM_EXPAND ? BM : 1], s_rank[MODE == GM_EXPAND ? BM : 1], s_begin[MODE == GM_EXPAND ? BM + 1 : 1];
+    __shared__ int s_wave[8], s_adapters;
     Work w;
     if (!locate(blockIdx.x >> 3, w)) {
         if constexpr (MODE == GM_ROWS) {   // (some have no tile: see launch_gmm)
@@ -399,7 +430,12 @@ __global__ void __launch_bounds__(WAVES_M * WAVES_N * WAVE, 2) k_gmm(GmmArgs a, 
     };
 
     uint4 kept_l[ASYNC ? 1 : TL::LOADS], kept_r[ASYNC ? 1 : TR::LOADS];
+    // Workgroups begin at different steps and go round: at the same one, the lines that they read all begin in the same few memory channels
+    // where lines are a multiple of some KB long (32 products with 2048 x 2048 weights, 64 rows each: 53 us, from one step on 94).
+    const int turn = DEPTH || steps == 0 ? 0 : (w.n0 / BN + w.group * 5) % steps;
     auto fetch = [&](int t, int buffer) {
+        t += turn;
+        if (t >= steps) t -= steps;
         char *to = lds + buffer * BUFFER;
         const int left = min(STEP_C, depth - t * STEP_C);   // c of this step
         if constexpr (ASYNC) {
@@ -508,6 +544,31 @@ __global__ void __launch_bounds__(WAVES_M * WAVES_N * WAVE, 2) k_gmm(GmmArgs a, 
     };
 
     if (steps > 0) load_numbers(0);
+    if constexpr (MODE == GM_EXPAND) {
+        const int slot = w.m0 + tid;
+        const bool has = tid < BM && slot < w.hi && (uint32_t)a.slot_id[min(slot, w.hi - 1)] < (uint32_t)a.adapters;
+        const int id = has ? a.slot_id[slot] : -1;
+        const bool starts = has && (tid == 0 || a.slot_id[slot - 1] != id);
+        const unsigned long long b = __ballot(starts), hb = __ballot(has);
+        if (lane == 0) s_wave[wave] = __popcll(b) | __popcll(hb) << 16;
+        __syncthreads();
+        int before = 0, total = 0;
+        for (int i = 0; i < WAVES_M * WAVES_N; ++i) {
+            if (i < wave) before += s_wave[i];
+            total += s_wave[i];
+        }
+        const int at = (before & 0xffff) + __popcll(b & ((1ull << lane) - 1));
+        if (starts) {
+            s_adapter[at] = id;
+            s_begin[at] = slot;
+            s_rank[at] = a.ranks ? a.ranks[id] : 0;
+        }
+        if (tid == 0) {
+            s_adapters = total & 0xffff;
+            s_begin[total & 0xffff] = w.m0 + (total >> 16);
+        }
+        __syncthreads();
+    }
     f32x4 acc[TM][TN] = {};
 #pragma unroll
     for (int t = 0; t < STAGES - 1; ++t)
@@ -533,80 +594,91 @@ __global__ void __launch_bounds__(WAVES_M * WAVES_N * WAVE, 2) k_gmm(GmmArgs a, 
         const int next = buffer == 0 ? STAGES - 1 : buffer - 1;   // (that of the step before)
         if (t + STAGES - 1 < steps) fetch(t + STAGES - 1, next);
         const char *from = lds + buffer * BUFFER;
-#pragma unroll
-        for (int half = 0; half < HALVES; ++half) {
+        auto part = [&](auto half) {
             Frag<T> fr[TN], fl[TM];
-#pragma unroll
-            for (int j = 0; j < TN; ++j) fr[j] = TR::read(from + TL::BYTES, at_r, j, half);
-#pragma unroll
-            for (int i = 0; i < TM; ++i) fl[i] = TL::read(from, at_l, i, half);
+            TR::template read<decltype(half)::value>(from + TL::BYTES, at_r, fr);
+            TL::template read<decltype(half)::value>(from, at_l, fl);
 #pragma unroll
             for (int i = 0; i < TM; ++i)
 #pragma unroll
                 for (int j = 0; j < TN; ++j) mma(acc[i][j], fr[j], fl[i]);
-        }
+        };
+        part(std::integral_constant<int, 0>{});
+        part(std::integral_constant<int, 1>{});
         if (!ASYNC && t + 1 < steps) stash(next);
         buffer = buffer + 1 == STAGES ? 0 : buffer + 1;
     }
     if constexpr (MODE == GM_EXPAND) {
-        // The adapters of the tile's rows, one after the other: 128 bytes of h and b a step, h's parts side by side and b's line again
-        // for each.  A row takes only its own adapter's products (not 0 times the others', which may be infinite or NaN).
+        // The adapters of the tile's rows: 64 bytes of h and b at a time (a unit), as many units a step as the tile has halves, h's parts side
+        // by side and b's line again for each.  A row takes only its own adapter's products (not 0 times the others', which may be
+        // infinite or NaN).
+        constexpr int PARTS = sizeof(T) == 2 ? 2 : 1, UNIT = 64 / (int)sizeof(T);
+        constexpr bool AHEAD = BM * BN <= 128 * 128;   // the next step's loads are under way meanwhile (larger tiles leave no registers)
+        const int wide_h = PARTS * a.rank_up, each = (wide_h + UNIT - 1) / UNIT, units = s_adapters * each;
+        const T *h = static_cast<const T *>(a.h);
         const int end = min(w.m0 + BM, w.hi);
-        constexpr int PARTS = sizeof(T) == 2 ? 2 : 1;
-        const int wide_h = PARTS * a.rank_up;
-        for (int s = w.m0; s < end;) {
-            const int e = (int)wave_first(a.slot_id[s]);
-            if (e < 0 || e >= a.adapters) break;   // (rows without an adapter come last)
-            const int e_end = (int)wave_first(a.adapter_ptr[e + 1]);
-            const int rank = a.ranks ? min(max(a.ranks[e], 0), a.rank) : a.rank;
-            const T *b = static_cast<const T *>(a.b) + (int64_t)e * a.stride_b, *h = static_cast<const T *>(a.h);
-            for (int p0 = 0; p0 < wide_h && rank > 0; p0 += STEP_C) {
-                uint4 xl[TL::LOADS], xr[TR::LOADS];
+        uint4 xl[TL::LOADS], xr[TR::LOADS];
+        struct Unit { const T *b; int p, rank, last; };   // where its columns of h begin, those of b that there are; `last` of h's behind p
+        auto unit = [&](int u) -> Unit {
+            const int j = __builtin_amdgcn_readfirstlane(u / each), e = __builtin_amdgcn_readfirstlane(s_adapter[min(j, BM - 1)]);
+            const int rank = a.ranks ? min(max(__builtin_amdgcn_readfirstlane(s_rank[min(j, BM - 1)]), 0), a.rank) : a.rank, p = (u - j * each) * UNIT;
+            return u < units ? Unit{static_cast<const T *>(a.b) + e * a.stride_b, p, rank, wide_h - p} : Unit{static_cast<const T *>(a.b), 0, 0, 0};
+        };
+        auto load = [&](int u0) {
+            const Unit u[2] = {unit(u0), unit(u0 + 1)};
 #pragma unroll
-                for (int i = 0; i < TL::LOADS; ++i) {
-                    const int p = p0 + TL::piece_of(tid, i) * PIECE<T>;
-                    const int64_t line = min(w.m0 + TL::line_of(tid, i), end - 1);
-                    xl[i] = load_piece(h + line * wide_h + p, p < wide_h ? PIECE<T> : 0);
-                }
+            for (int i = 0; i < TL::LOADS; ++i) {
+                const int q = TL::piece_of(tid, i), in = q % 4 * PIECE<T>;
+                const bool second = q >= 4;
+                xl[i] = load_piece(h + (int64_t)min(w.m0 + TL::line_of(tid, i), end - 1) * wide_h + (second ? u[1].p : u[0].p) + in,
+                                   in < (second ? u[1].last : u[0].last) ? PIECE<T> : 0);
+            }
 #pragma unroll
-                for (int i = 0; i < TR::LOADS; ++i) {
-                    const int p = p0 + TR::piece_of(tid, i) * PIECE<T>, q = p % a.rank_up;
-                    const int64_t line = min(w.n0 + TR::line_of(tid, i), (int)a.n - 1);
-                    xr[i] = load_piece(b + line * a.ldb + q, p < wide_h ? rank - q : 0);
-                }
-                __syncthreads();
+            for (int i = 0; i < TR::LOADS; ++i) {
+                const int q = TR::piece_of(tid, i), in = q % 4 * PIECE<T>;
+                const bool second = q >= 4;
+                const int p = (second ? u[1].p : u[0].p) + in, at = p >= a.rank_up ? p - a.rank_up : p;
+                xr[i] = load_piece((second ? u[1].b : u[0].b) + min(w.n0 + TR::line_of(tid, i), (int)a.n - 1) * a.ldb + at,
+                                   in < (second ? u[1].last : u[0].last) ? (second ? u[1].rank : u[0].rank) - at : 0);
+            }
+        };
+        if (AHEAD && units > 0) load(0);
+        for (int u0 = 0; u0 < units; u0 += HALVES) {
+            if (!AHEAD) load(u0);
+            __syncthreads();
 #pragma unroll
-                for (int i = 0; i < TL::LOADS; ++i) *reinterpret_cast<uint4 *>(lds + (i * THREADS + tid) * 16) = xl[i];
+            for (int i = 0; i < TL::LOADS; ++i) *reinterpret_cast<uint4 *>(lds + (i * THREADS + tid) * 16) = xl[i];
 #pragma unroll
-                for (int i = 0; i < TR::LOADS; ++i) *reinterpret_cast<uint4 *>(lds + TL::BYTES + (i * THREADS + tid) * 16) = xr[i];
-                __syncthreads();
-                Frag<T> fr[HALVES][TN];
-#pragma unroll
-                for (int half = 0; half < HALVES; ++half)
-#pragma unroll
-                    for (int j = 0; j < TN; ++j) fr[half][j] = TR::read(lds + TL::BYTES, at_r, j, half);
+            for (int i = 0; i < TR::LOADS; ++i) *reinterpret_cast<uint4 *>(lds + TL::BYTES + (i * THREADS + tid) * 16) = xr[i];
+            if (AHEAD && u0 + HALVES < units) load(u0 + HALVES);
+            __syncthreads();
+            auto part = [&](auto half_) {
+                constexpr int half = decltype(half_)::value;
+                if (u0 + half >= units) return;
+                const int from = s_begin[(u0 + half) / each], to = s_begin[(u0 + half) / each + 1];
+                Frag<T> fr[TN], fl[TM];
+                TR::template read<half>(lds + TL::BYTES, at_r, fr);
+                TL::template read<half>(lds, at_l, fl);
 #pragma unroll
                 for (int i = 0; i < TM; ++i) {
                     const int row = w.m0 + wm + i * 16 + r;
-                    const bool mine = row >= s && row < e_end;
+                    const bool mine = row >= from && row < to;
                     if (!__any(mine)) continue;
-                    f32x4 sum[TN] = {};
                     const float back = mine ? a.row_scale[row] : 0.0f;
 #pragma unroll
-                    for (int half = 0; half < HALVES; ++half) {
-                        const Frag<T> fl = TL::read(lds, at_l, i, half);
+                    for (int j = 0; j < TN; ++j) {
+                        f32x4 sum = {};
+                        mma(sum, fr[j], fl[i]);
 #pragma unroll
-                        for (int j = 0; j < TN; ++j) mma(sum[j], fr[half][j], fl);
+                        for (int k = 0; k < 4; ++k) acc[i][j][k] = mine ? acc[i][j][k] + back * sum[k] : acc[i][j][k];
                     }
-#pragma unroll
-                    for (int j = 0; j < TN; ++j)
-#pragma unroll
-                        for (int k = 0; k < 4; ++k) acc[i][j][k] = mine ? acc[i][j][k] + back * sum[j][k] : acc[i][j][k];
                 }
-            }
-            s = e_end > s ? e_end : s + 1;
+            };
+            part(std::integral_constant<int, 0>{});
+            part(std::integral_constant<int, 1>{});
         }
     }
+
     store(w, acc);
 }
 
@@ -625,22 +697,29 @@ hipError_t launch_gmm(const GmmArgs &a, hipStream_t s)
     return hipGetLastError();
 }
 
-// The largest tile that still gives every compute unit work: 256 x 256 (one workgroup a unit) from 256 tiles on, 128 x 128 (two) from
-// 512, 64 x 128 from 256, else 64 x 64.  Eight products of 512 x 4096 by 4096 x 1024 (bfloat16; 64, 256, 512, 1024 tiles) take 117, 65, 54
-// and 73 us, 32 of 256 x 2048 by 2048 x 2048 (256, 1024, 2048, 4096 tiles) 99, 114, 132 and 166.
+// Which tile: the one whose rounds over the chip's 256 compute units take the least.  A round is one tile of 256 x 256 a unit, or two of the
+// others; what a round takes, or half of one (a tile a unit), in units of half a round of the largest: measured at c = 4096 in bfloat16 as
+// 135 us for 256 tiles of 256 x 256, 82 for 512 of 128 x 128 and 66 for 256, 62 and 38 of 64 x 128, 45 and 28 of 64 x 64.
+inline double rounds(double tiles, double half, double full)
+{
+    const double whole = (double)(int64_t)(tiles / 512), rest = tiles - whole * 512;
+    return whole * full + (rest > 256 ? full : rest > 0 ? half : 0.0);
+}
 // m_tiles(lines): about how many tiles of that many lines there are.
 template <class T, bool LCOL, bool RCOL, GmmMode MODE, class F> hipError_t launch_tiles(const GmmArgs &a, F m_tiles, bool aligned, hipStream_t s)
 {
-    auto tiles = [&](int64_t bm, int64_t bn) { return m_tiles(bm) * ((a.n + bn - 1) / bn); };
-    if (!aligned) {
+    auto tiles = [&](int64_t bm, int64_t bn) { return (double)m_tiles(bm) * (double)((a.n + bn - 1) / bn); };
+    const double large = (double)(int64_t)((tiles(256, 256) + 255) / 256) * 2.0, middle = rounds(tiles(128, 128), 0.98, 1.22),
+                 low = rounds(tiles(64, 128), 0.56, 0.92), small = rounds(tiles(64, 64), 0.42, 0.66);
+    if (!aligned) {   // (through registers, more tiles hide more)
         if (tiles(128, 128) >= 512) return launch_gmm<T, LCOL, RCOL, 128, 128, 2, 2, false, 2, MODE>(a, s);
         return launch_gmm<T, LCOL, RCOL, 64, 64, 4, 1, false, 2, MODE>(a, s);
     }
     if constexpr (sizeof(T) == 2) {
-        if (tiles(256, 256) >= 256) return launch_gmm<T, LCOL, RCOL, 256, 256, 2, 4, true, 2, MODE>(a, s);
+        if (large <= std::min(std::min(middle, low), small)) return launch_gmm<T, LCOL, RCOL, 256, 256, 2, 4, true, 2, MODE>(a, s);
     }
-    if (tiles(128, 128) >= 512) return launch_gmm<T, LCOL, RCOL, 128, 128, 2, 2, true, 2, MODE>(a, s);
-    if (tiles(64, 128) >= 256) return launch_gmm<T, LCOL, RCOL, 64, 128, 2, 2, true, 3, MODE>(a, s);
+    if (middle <= std::min(low, small)) return launch_gmm<T, LCOL, RCOL, 128, 128, 2, 2, true, 2, MODE>(a, s);
+    if (low <= small) return launch_gmm<T, LCOL, RCOL, 64, 128, 2, 2, true, 3, MODE>(a, s);
     return launch_gmm<T, LCOL, RCOL, 64, 64, 4, 1, true, 4, MODE>(a, s);
 }
 

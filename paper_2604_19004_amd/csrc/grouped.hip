@@ -5,12 +5,12 @@ namespace ocean {
 
 namespace {
 
-// Groups of few rows: workgroup (x, y) has columns 16 TN x .. of the y-th group that has any rows, all of its rows: 16, 32 or 64 at a time.
-constexpr int FEW_ROWS = 64;
+// Groups of few rows: workgroup (x, y) has columns 16 TN x .. of the y-th group that has any rows, all of its rows, up to 64 (32) at a time.
+constexpr int few_rows(bool col) { return col ? 32 : 64; }   // (more fragments at a time than registers take)
 template <class T, bool RCOL, int TN, int WAVES, bool ALIGNED>
 __global__ void __launch_bounds__(WAVES * WAVE, 2) k_few(GmmArgs a)
 {
-    constexpr int SUMS = WAVES * FEW_ROWS * (TN * 16 + 4) * 4, RINGS = RCOL ? WAVES * FEW_RING * FEW_STAGE : 0;
+    constexpr int FEW_ROWS = few_rows(RCOL), SUMS = WAVES * FEW_ROWS * (TN * 16 + 4) * 4, RINGS = RCOL ? WAVES * FEW_RING * FEW_STAGE : 0;
     __shared__ __align__(16) char s_lds[SUMS > RINGS ? SUMS : RINGS];
     __shared__ int64_t s_row[FEW_ROWS];
     int group, lo, hi, groups = 0;
@@ -34,11 +34,12 @@ __global__ void __launch_bounds__(WAVES * WAVE, 2) k_few(GmmArgs a)
         auto tile = [&](auto tm) {
             constexpr int TM = decltype(tm)::value;
             if constexpr (RCOL) few_tile_col<T, TM, WAVES>(x, a.ldl, s_row, rows, w, a.ldr, n0, a.n, a.c, s_lds, store);
-            else few_tile<T, TM, TN, WAVES, ALIGNED>(x, a.ldl, s_row, rows, w, a.ldr, n0, a.n, a.c, reinterpret_cast<float *>(s_lds), store);
+            else few_tile<T, TM, TN, WAVES, ALIGNED>(x, a.ldl, s_row, rows, w, a.ldr, n0, a.n, a.c, reinterpret_cast<float *>(s_lds),
+                                                            [](int, int64_t) { return 0.0f; }, store);
         };
         if (rows <= 16) tile(std::integral_constant<int, 1>{});
         else if (rows <= 32) tile(std::integral_constant<int, 2>{});
-        else tile(std::integral_constant<int, 4>{});
+        else if constexpr (!RCOL) tile(std::integral_constant<int, 4>{});
     }
 }
 
@@ -49,35 +50,22 @@ template <class T, bool RCOL, int TN, int WAVES, bool ALIGNED> hipError_t launch
     return hipGetLastError();
 }
 
-// Groups of at most this many rows on the average go to k_few.  Weights whose lines lie along c: eight of 4096 x 1024 (bfloat16) take 24 us
-// with 32 rows each and 31 with 48 there, 26 with 64 in tiles of 64 x 64; two of 4096 x 8192 36 and 44 us, and 32.  Across c: 28, 34 and 50
-// us, and 35, 42 and 58.
-constexpr int64_t few_average(bool col) { return col ? 48 : 24; }
-
-// Columns of a workgroup.  64: wide enough that the rows, which every workgroup reads, are read half as often (32 matrices of 2048 x 2048
-// with 32 rows each: 72 us, 78 with 32 columns), if they are many or c is short; 16 and twice the waves: where 32 would
-// leave compute units without work (eight of 4096 x 1024, 8 rows: 16 us, 20 with 32 columns, 24 with 64).
-template <class T, bool RCOL> hipError_t launch_few_rows(const GmmArgs &a, int64_t groups, bool aligned, hipStream_t s)
-{
-    if constexpr (RCOL) {
-        return launch_few<T, true, 4, 4, true>(a, s);
-    } else {
-        const bool many = a.rows > 16 * groups;
-        if ((many || a.c * sizeof(T) <= 1024) && groups * ((a.n + 63) / 64) >= 256)
-            return aligned ? launch_few<T, false, 4, 4, true>(a, s) : launch_few<T, false, 4, 4, false>(a, s);
-        if (!many && groups * ((a.n + 31) / 32) < 512) return aligned ? launch_few<T, false, 1, 8, true>(a, s) : launch_few<T, false, 1, 8, false>(a, s);
-        return aligned ? launch_few<T, false, 2, 4, true>(a, s) : launch_few<T, false, 2, 4, false>(a, s);
-    }
-}
-
 template <class T, bool LCOL, bool RCOL, GmmMode MODE> hipError_t pick_tile(const GmmArgs &a, bool aligned, hipStream_t s)
 {
     const int64_t groups = MODE == GM_DEPTH ? a.groups : std::min(a.groups, a.rows);
     if constexpr (MODE == GM_ROWS) {
-        if (groups > 0 && groups < 65535 && a.rows <= groups * few_average(RCOL) && (!RCOL || aligned)) return launch_few_rows<T, RCOL>(a, groups, aligned, s);
+        // Where tiles of 64 x 64 would leave compute units without work, c is divided among the waves of a workgroup instead: eight
+        // products with 4096 x 1024 weights take 14 us with a row each, 19 with 16, 24 with 24 and in tiles 26 (lines along c); 20 to 27 with
+        // up to 32 and in tiles 30 (across c).
+        if (groups > 0 && groups * ((a.n + 63) / 64) < 256 && a.rows <= groups * (RCOL ? 32 : 24)) {
+            if constexpr (!RCOL) return aligned ? launch_few<T, false, 1, 8, true>(a, s) : launch_few<T, false, 1, 8, false>(a, s);
+            if (aligned) return launch_few<T, true, 4, 8, true>(a, s);
+        }
     }
-    return launch_tiles<T, LCOL, RCOL, MODE>(a, [&](int64_t bm) { return MODE == GM_DEPTH ? groups * ((a.m + bm - 1) / bm) : std::max(groups, a.rows / bm); },
-                                             aligned, s);
+    return launch_tiles<T, LCOL, RCOL, MODE>(a, [&](int64_t bm) {
+        if (MODE == GM_DEPTH) return groups * ((a.m + bm - 1) / bm);
+        return a.rows <= groups * bm ? groups : a.rows / bm + groups / 2;   // (a group's last tile is half full on the average)
+    }, aligned, s);
 }
 
 }  // namespace
