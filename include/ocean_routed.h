@@ -49,7 +49,8 @@ typedef struct ocean_routing {
  * A logit that is NaN, -inf or the lowest finite value of its type is masked: it is never taken (a row of
  * such logits stays empty).  +inf counts as the largest finite value.  Weights: the softmax of the row's logits, over the
  * entries taken (normalize != 0) or over all that are not masked (0).  1 <= k <= min(experts, OCEAN_ROUTE_MAX_K), experts <=
- * OCEAN_ROUTE_MAX_EXPERTS, tokens * k < 2^31.  workspace: ocean_route_workspace bytes, aligned to 256, needed until the kernels have run.
+ * OCEAN_ROUTE_MAX_EXPERTS, tokens * k < 2^31.  workspace: ocean_route_workspace bytes, aligned to 256, needed until the kernels have run (0
+ * bytes, and NULL will do, for few tokens).
  */
 size_t ocean_route_workspace(int64_t tokens, int64_t experts, int32_t k);
 int ocean_route(const void *logits, int32_t dtype, int64_t ld, int32_t normalize, const ocean_routing *out, void *workspace,

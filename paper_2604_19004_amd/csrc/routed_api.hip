@@ -83,7 +83,8 @@ int ocean_route(const void *logits, int32_t dtype, int64_t ld, int32_t normalize
     if (!known_type(dtype)) return bad("dtype must be OCEAN_F32, OCEAN_BF16 or OCEAN_F16");
     REFUSE(routing_fault(out, true, true));
     REFUSE(matrix_fault(logits, out->tokens, out->experts, ld, dtype));
-    if (!workspace || !aligned(workspace, 256) || workspace_bytes < route_workspace(out->tokens, out->experts, out->k))
+    const size_t need = route_workspace(out->tokens, out->experts, out->k);
+    if (need > 0 && (!workspace || !aligned(workspace, 256) || workspace_bytes < need))
         return bad("workspace is null, not aligned to 256 bytes or smaller than ocean_route_workspace");
     return launched(launch_route(logits, dtype, ld, normalize != 0, *out, workspace, static_cast<hipStream_t>(stream)), "ocean_route");
 }

@@ -74,7 +74,7 @@ def load():
     return lib
 
 
-@dataclass
+@dataclass(frozen=True)
 class Routing:
     """A routing matrix in CSR (row_ptr int64 [tokens+1], col_idx int32, val float32 or None) and in the order of its columns
     (expert_ptr int64 [experts+1], token int32, slot int32).  The four entry arrays have tokens * k places; those behind the last
@@ -89,25 +89,44 @@ class Routing:
     token: "object"
     slot: "object"
 
+    def __post_init__(self):
+        """The lists are contiguous, of their types, of their sizes and on one device."""
+        import torch
+        n, device = self.tokens * self.k, self.row_ptr.device
+        for name, dtype, size in (("row_ptr", torch.int64, self.tokens + 1), ("col_idx", torch.int32, n), ("val", torch.float32, n),
+                                  ("expert_ptr", torch.int64, self.experts + 1), ("token", torch.int32, n), ("slot", torch.int32, n)):
+            t = getattr(self, name)
+            if t is not None or name != "val":
+                _vector(t, name, dtype, size, device)
+        self._hold(device, self.val is not None)
+
+    def _hold(self, device, weighted):
+        """The C structs, with val and without, for as long as the lists are held."""
+        lists = [_ptr(t) for t in (self.row_ptr, self.col_idx, self.val if weighted else None, self.expert_ptr, self.token, self.slot)]
+        c = ocean_routing(self.tokens, self.experts, self.k, 0, *lists)
+        lists[2] = None
+        self.__dict__.update(_device=device, _structs=(ocean_routing(self.tokens, self.experts, self.k, 0, *lists), c))
+
+    @classmethod
+    def _made(cls, *fields):
+        """One whose lists this module has just made."""
+        r = object.__new__(cls)
+        r.__dict__.update(zip(cls.__dataclass_fields__, fields))
+        r._hold(r.row_ptr.device, True)
+        return r
+
     def csr(self) -> DeviceCSR:
         """The matrix as an operand of binding.spgemm; reads the number of its entries back."""
         n = int(self.row_ptr[-1])
         return DeviceCSR(self.tokens, self.experts, self.row_ptr, self.col_idx[:n], self.val[:n], [self])
 
     def _struct(self, weighted=True):
-        return ocean_routing(self.tokens, self.experts, self.k, 0, *(_ptr(t) for t in (
-            self.row_ptr, self.col_idx, self.val if weighted else None, self.expert_ptr, self.token, self.slot)))
+        return self._structs[bool(weighted)]
 
-    def _check(self, device):
-        """The lists are contiguous, of their types, of their sizes and on `device`."""
-        import torch
-        n = self.tokens * self.k
-        for name, dtype, size in (("row_ptr", torch.int64, self.tokens + 1), ("col_idx", torch.int32, n), ("val", torch.float32, n),
-                                  ("expert_ptr", torch.int64, self.experts + 1), ("token", torch.int32, n), ("slot", torch.int32, n)):
-            t = getattr(self, name)
-            if t is not None or name != "val":
-                _vector(t, name, dtype, size, device)
-        return [t for t in (self.row_ptr, self.col_idx, self.val, self.expert_ptr, self.token, self.slot) if t is not None]
+    def _lists(self, device):
+        if device != self._device:
+            raise ValueError(f"the routing is on {self._device}, not {device}")
+        return self.row_ptr, self.col_idx, self.val, self.expert_ptr, self.token, self.slot
 
 
 # ---------------------------------------------------------------- arguments
@@ -149,30 +168,26 @@ def _matrix(t, name, rows=None, width=None, like=None):
     return max(t.stride(0), 1)
 
 
-class _Call:
-    """One call's device and stream: tensors made inside belong to the stream; tensors that the call reads and that another stream
-    made are kept until it is done with them."""
+_HERE = nullcontext()
+_raw_stream = None
 
-    def __init__(self, device, stream, *tensors):
-        torch = _b._torch()
-        if device.type != "cuda":
-            raise ValueError(f"tensors must be on a GPU, not {device}")
-        current = torch.cuda.current_stream(device)
-        self.stream = current if stream is None else stream
-        self.ptr = int(self.stream.cuda_stream)
-        other = self.stream != current
-        self.scope = torch.cuda.stream(self.stream) if other else _b._on(device)
-        if other:
-            for t in tensors:
-                if t is not None:
-                    t.record_stream(self.stream)
 
-    def __enter__(self):
-        self.scope.__enter__()
-        return self.ptr
-
-    def __exit__(self, *e):
-        return self.scope.__exit__(*e)
+def _at(device, stream, *tensors):
+    """(the stream's pointer, the context in which it is current on `device`): tensors made inside belong to it, and those that the call
+    uses and another stream made are kept until it is done with them."""
+    global _raw_stream
+    torch = _b._torch()
+    if device.type != "cuda":
+        raise ValueError(f"tensors must be on a GPU, not {device}")
+    if stream is None:
+        if _raw_stream is None:   # (a fifth of the time of current_stream(), where torch has it)
+            _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda i: torch.cuda.current_stream(i).cuda_stream)
+        return _raw_stream(device.index), _HERE if device.index == torch.cuda.current_device() else torch.cuda.device(device)
+    if stream != torch.cuda.current_stream(device):
+        for t in tensors:
+            if t is not None:
+                t.record_stream(stream)
+    return int(stream.cuda_stream), torch.cuda.stream(stream)
 
 
 def _output(out, shape, like, name="out"):
@@ -196,15 +211,15 @@ def route(logits, k: int, *, normalize: bool = True, stream=None) -> Routing:
     if not 1 <= k <= min(E, MAX_K) or E > MAX_EXPERTS:
         raise ValueError(f"k must be 1 to min(experts, {MAX_K}) and experts at most {MAX_EXPERTS}, not {k} of {E}")
     dev = logits.device
-    with _Call(dev, stream, logits) as s:
+    s, here = _at(dev, stream, logits)
+    with here:
         n = T * k
-        r = Routing(T, E, k, torch.empty(T + 1, dtype=torch.int64, device=dev), torch.empty(n, dtype=torch.int32, device=dev),
-                    torch.empty(n, dtype=torch.float32, device=dev), torch.empty(E + 1, dtype=torch.int64, device=dev),
-                    torch.empty(n, dtype=torch.int32, device=dev), torch.empty(n, dtype=torch.int32, device=dev))
+        row_ptr, expert_ptr = torch.empty(T + E + 2, dtype=torch.int64, device=dev).split((T + 1, E + 1))
+        val, col_idx, token, slot = torch.empty((4, n), dtype=torch.int32, device=dev).unbind(0)
+        r = Routing._made(T, E, k, row_ptr, col_idx, val.view(torch.float32), expert_ptr, token, slot)
         nbytes = lib.ocean_route_workspace(T, E, k)
-        space = torch.empty(nbytes, dtype=torch.uint8, device=dev)
-        c = r._struct()
-        _b._check(lib.ocean_route(_ptr(logits), code, ld, int(normalize), C.byref(c), space.data_ptr(), nbytes, s))
+        space = torch.empty(nbytes, dtype=torch.uint8, device=dev) if nbytes else None
+        _b._check(lib.ocean_route(_ptr(logits), code, ld, int(normalize), C.byref(r._struct()), _ptr(space), nbytes, s))
     return r
 
 
@@ -213,15 +228,15 @@ def route_backward(routing: Routing, dval, logits, *, normalize: bool = True, ou
     import torch
     lib = load()
     ld = _matrix(logits, "logits", routing.tokens, routing.experts)
-    lists = routing._check(logits.device)
+    lists = routing._lists(logits.device)
     if routing.val is None:
         raise ValueError("the routing has no weights")
     _vector(dval, "dval", torch.float32, routing.tokens * routing.k, logits.device)
-    with _Call(logits.device, stream, logits, dval, out, *lists) as s:
+    s, here = _at(logits.device, stream, logits, dval, out, *lists)
+    with here:
         out = _output(out, logits.shape, logits)
         ldo = _matrix(out, "out", like=logits)
-        c = routing._struct()
-        _b._check(lib.ocean_route_backward(C.byref(c), _ptr(dval), _ptr(logits), _code(logits.dtype), ld, int(normalize), _ptr(out), ldo, s))
+        _b._check(lib.ocean_route_backward(C.byref(routing._struct()), _ptr(dval), _ptr(logits), _code(logits.dtype), ld, int(normalize), _ptr(out), ldo, s))
     return out
 
 
@@ -229,12 +244,12 @@ def combine(y, routing: Routing, *, weighted: bool = True, out=None, stream=None
     """out[t] = sum of val[p] * y[slot[p]] over the entries p of row t (weighted=False, or a routing without val: of y[slot[p]])."""
     lib = load()
     ldy = _matrix(y, "y", routing.tokens * routing.k)
-    lists = routing._check(y.device)
-    with _Call(y.device, stream, y, out, *lists) as s:
+    lists = routing._lists(y.device)
+    s, here = _at(y.device, stream, y, out, *lists)
+    with here:
         out = _output(out, (routing.tokens, y.shape[1]), y)
         ldo = _matrix(out, "out", like=y)
-        c = routing._struct(weighted)
-        _b._check(lib.ocean_combine(C.byref(c), _ptr(y), _code(y.dtype), y.shape[1], ldy, _ptr(out), ldo, s))
+        _b._check(lib.ocean_combine(C.byref(routing._struct(weighted)), _ptr(y), _code(y.dtype), y.shape[1], ldy, _ptr(out), ldo, s))
     return out
 
 
@@ -245,12 +260,12 @@ def combine_backward(dout, y, routing: Routing, *, weighted: bool = True, stream
     ldo = _matrix(dout, "dout", routing.tokens)
     width, n = dout.shape[1], routing.tokens * routing.k
     ldy = _matrix(y, "y", n, width, like=dout) if y is not None else width
-    lists = routing._check(dout.device)
-    with _Call(dout.device, stream, dout, y, *lists) as s:
+    lists = routing._lists(dout.device)
+    s, here = _at(dout.device, stream, dout, y, *lists)
+    with here:
         dy = dout.new_empty((n, width))
         dval = torch.empty(n, dtype=torch.float32, device=dout.device) if y is not None else None
-        c = routing._struct(weighted)
-        _b._check(lib.ocean_combine_backward(C.byref(c), _ptr(dout), ldo, _ptr(y), ldy, _code(dout.dtype), width, _ptr(dy), max(width, 1),
+        _b._check(lib.ocean_combine_backward(C.byref(routing._struct(weighted)), _ptr(dout), ldo, _ptr(y), ldy, _code(dout.dtype), width, _ptr(dy), max(width, 1),
                                              _ptr(dval), s))
     return dy, dval
 
@@ -293,7 +308,8 @@ def grouped_matmul(x, w, expert_ptr, *, rows=None, transposed: bool = False, out
     outer, inner = (w.shape[2], w.shape[1]) if transposed else (w.shape[1], w.shape[2])
     if w.shape[0] != g.experts or inner != x.shape[1]:
         raise ValueError(f"w is {tuple(w.shape)}{' (transposed)' if transposed else ''}: not {g.experts} matrices for rows of {x.shape[1]}")
-    with _Call(x.device, stream, x, w, expert_ptr, rows, out) as s:
+    s, here = _at(x.device, stream, x, w, expert_ptr, rows, out)
+    with here:
         out = _output(out, (g.rows, outer), x)
         ldo = _matrix(out, "out", like=x)
         _b._check(lib.ocean_grouped_matmul(C.byref(g), code, inner, outer, _ptr(x), ldx, _ptr(w), ldw, stride, int(transposed), _ptr(out), ldo, s))
@@ -309,7 +325,8 @@ def grouped_weight_grad(dy, x, expert_ptr, *, rows=None, transposed: bool = Fals
     g = _groups(x, expert_ptr, rows)
     ldd = _matrix(dy, "dy", g.rows, like=x)
     inner, outer = x.shape[1], dy.shape[1]
-    with _Call(x.device, stream, x, dy, expert_ptr, rows, out) as s:
+    s, here = _at(x.device, stream, x, dy, expert_ptr, rows, out)
+    with here:
         out = _output(out, (g.experts, inner, outer) if transposed else (g.experts, outer, inner), x)
         ldo, stride = _matrices(out, "out", like=x)
         _b._check(lib.ocean_grouped_weight_grad(C.byref(g), code, inner, outer, _ptr(dy), ldd, _ptr(x), ldx, _ptr(out), ldo, stride, int(transposed), s))
@@ -340,7 +357,8 @@ def adapter_matmul(x, w, a, b, ids, *, ranks=None, scale=None, out=None, stream=
         _vector(ranks, "ranks", torch.int32, adapters, dev)
     if scale is not None:
         _vector(scale, "scale", torch.float32, adapters, dev)
-    with _Call(dev, stream, x, w, a, b, ids, ranks, scale, out) as s:
+    s, here = _at(dev, stream, x, w, a, b, ids, ranks, scale, out)
+    with here:
         out = _output(out, (rows, outer), x)
         ldo = _matrix(out, "out", like=x)
         nbytes = lib.ocean_adapter_workspace(rows, inner, outer, adapters, rank, code)

@@ -96,6 +96,16 @@ def test_gradient_of_the_logits_against_differences(rt, normalize):
         assert np.all(np.abs(diff - got[:, e]) <= 12 * h * h / 6 + 12 * 1.1e-5 / h)
 
 
+def test_one_block_and_several(rt):
+    """Up to 64 tokens take another way than more: their matrix is the same as that of the same rows among more."""
+    import torch
+    for T, E, k in ((64, 40, 3), (64, 300, 9), (63, 700, 20)):
+        x = _logits(T, E, torch.float32, E, "masked").cuda()
+        few, many = rt.route(x, k, normalize=False), rt.route(torch.cat([x, x]), k, normalize=False)
+        n = int(few.row_ptr[-1])
+        assert torch.equal(few.row_ptr, many.row_ptr[:T + 1]) and torch.equal(few.col_idx[:n], many.col_idx[:n]) and torch.equal(few.val[:n], many.val[:n])
+
+
 def test_strided_logits_streams_and_out(rt):
     import torch
     base = torch.randn(70, 40, device="cuda")
@@ -236,8 +246,10 @@ def test_refusals(rt):
             call()
     import ctypes
     from paper_2604_19004_amd import binding
-    lib, c = rt.load(), r._struct()
-    need = lib.ocean_route_workspace(8, 6, 2)
+    x = torch.randn(200, 6, device="cuda")   # (few tokens need no workspace)
+    lib, c, few = rt.load(), rt.route(x, 2)._struct(), r._struct()
+    assert lib.ocean_route_workspace(8, 6, 2) == 0
+    need = lib.ocean_route_workspace(200, 6, 2)
     space = torch.empty(need + 256, dtype=torch.uint8, device="cuda")
     at = space.data_ptr()
     for rc, word in ((lambda: lib.ocean_route(x.data_ptr(), 0, 6, 1, ctypes.byref(c), at, need, None), "dtype"),
@@ -249,6 +261,6 @@ def test_refusals(rt):
                      (lambda: lib.ocean_route(None, 1, 6, 1, ctypes.byref(c), at, need, None), "null"),
                      (lambda: lib.ocean_combine(None, y.data_ptr(), 1, 32, 32, y.data_ptr(), 32, None), "routing is null")):
         assert rc() == 1 and word in lib.ocean_last_error().decode()
-    c.k = 7
-    assert lib.ocean_combine(ctypes.byref(c), y.data_ptr(), 1, 32, 32, y.data_ptr(), 32, None) == 1
+    few.k = 7
+    assert lib.ocean_combine(ctypes.byref(few), y.data_ptr(), 1, 32, 32, y.data_ptr(), 32, None) == 1
     assert lib.ocean_route_workspace(-1, 6, 2) == 0
