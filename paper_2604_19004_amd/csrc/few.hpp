@@ -109,12 +109,12 @@ __device__ __forceinline__ void few_tile(const T *x, int64_t ldx, const int64_t 
     few_finish<T, TM, TN, WAVES>(acc, first, rows, n0, n, lds, store);
 }
 
-// The same where a line of the right matrix is one c (its columns lie side by side, aligned to 16 bytes).  The matrix cores want 8
+// The same where a line of the right matrix is one c (its columns lie side by side).  The matrix cores want 8
 // (4) c of one column in a lane, so the lines pass through LDS, which gives them back transposed: each wave has a ring of RING pieces of its own,
-// 4 KB (32 or 16 lines of 64 columns) each, filled straight from memory RING - 1 ahead; no wave waits for another.  `lds` holds
+// 4 KB (32 or 16 lines of 64 columns) each, filled FEW_RING - 1 ahead, straight from memory or (unaligned) through registers; no wave waits for another.  `lds` holds
 // the rings, then the sums.
 constexpr int FEW_COLS = 64, FEW_RING = 4, FEW_STAGE = 4096;
-template <class T, int TM, int WAVES, class Store>
+template <class T, int TM, int WAVES, bool ALIGNED, class Store>
 __device__ __forceinline__ void few_tile_col(const T *x, int64_t ldx, const int64_t *row_of, int rows, const T *w, int64_t ldw, int64_t n0, int64_t n,
                                              int64_t c, char *lds, Store store)
 {
@@ -124,30 +124,35 @@ __device__ __forceinline__ void few_tile_col(const T *x, int64_t ldx, const int6
     using Stage = Tile<T, true, false, FEW_COLS, WAVE, 64>;
     const uint32_t at_w = Stage::place(0);
     const T *xp[TM], *wp[LOADS];
-    int line[LOADS];
+    int line[LOADS], room[LOADS];   // (columns of a piece that there are)
+    uint4 kept[FEW_RING][ALIGNED ? 1 : LOADS];
 #pragma unroll
     for (int i = 0; i < TM; ++i) xp[i] = x + max(row_of[min(i * 16 + r, rows - 1)], (int64_t)0) * ldx + g * P;
 #pragma unroll
     for (int i = 0; i < LOADS; ++i) {
+        const int64_t col = n0 + Stage::piece_of(lane, i) * P;
         line[i] = Stage::line_of(lane, i);
-        wp[i] = w + line[i] * ldw + min(n0 + Stage::piece_of(lane, i) * P, n - P);
+        wp[i] = w + line[i] * ldw + (ALIGNED ? min(col, n - P) : col);
+        room[i] = (int)max(min(n - col, (int64_t)P), (int64_t)0);
     }
     const int64_t stages = (c + LINES - 1) / LINES;                                  // of all waves, taken in turn
     const int64_t mine = stages > wave ? (stages - wave + WAVES - 1) / WAVES : 0;     // of this wave
-    auto fill = [&](int64_t k, int slot, Frag<T> (&fx)[TM]) {
+    auto fill = [&](int64_t k, int slot, Frag<T> (&fx)[TM], uint4 (&kept_now)[ALIGNED ? 1 : LOADS]) {
         const int64_t c0 = (wave + k * WAVES) * LINES;
 #pragma unroll
-        for (int i = 0; i < LOADS; ++i)
-            load_to_lds(c0 + line[i] < c ? static_cast<const void *>(wp[i] + c0 * ldw) : &g_zero_piece, ring + slot * FEW_STAGE + i * WAVE * 16);
+        for (int i = 0; i < LOADS; ++i) {
+            if constexpr (!ALIGNED) kept_now[i] = load_piece(wp[i] + c0 * ldw, c0 + line[i] < c ? room[i] : 0);
+            else load_to_lds(c0 + line[i] < c ? static_cast<const void *>(wp[i] + c0 * ldw) : &g_zero_piece, ring + slot * FEW_STAGE + i * WAVE * 16);
+        }
 #pragma unroll
-        for (int i = 0; i < TM; ++i) fx[i] = few_load<T, true>(xp[i] + c0, c - c0 - g * P);
+        for (int i = 0; i < TM; ++i) fx[i] = few_load<T, ALIGNED>(xp[i] + c0, c - c0 - g * P);
     };
     f32x4 acc[TM][TN] = {};
     Frag<T> fx[FEW_RING][TM];
     __syncthreads();
 #pragma unroll
     for (int k = 0; k < FEW_RING - 1; ++k)
-        if (k < mine) fill(k, k, fx[k]);
+        if (k < mine) fill(k, k, fx[k], kept[k]);
     for (int64_t k0 = 0; k0 < mine; k0 += FEW_RING) {
 #pragma unroll
         for (int u = 0; u < FEW_RING; ++u) {
@@ -156,13 +161,19 @@ __device__ __forceinline__ void few_tile_col(const T *x, int64_t ldx, const int6
             // The slot that is filled next was read in the turn before: those reads have come back.
             __builtin_amdgcn_s_waitcnt(0xc07f);   // lgkmcnt(0)
             const bool more = k + FEW_RING - 1 < mine;
-            if (more) fill(k + FEW_RING - 1, (u + FEW_RING - 1) % FEW_RING, fx[(u + FEW_RING - 1) % FEW_RING]);
+            if (more) fill(k + FEW_RING - 1, (u + FEW_RING - 1) % FEW_RING, fx[(u + FEW_RING - 1) % FEW_RING], kept[(u + FEW_RING - 1) % FEW_RING]);
             // Loads come back in order: all but those of the FEW_RING - 1 stages behind this one.
             // (Each is one instruction: some lane's c lies before the end.)
-            constexpr int LATER = (FEW_RING - 1) * (LOADS + TM);
-            asm volatile("" ::: "memory");
-            if (more) __builtin_amdgcn_s_waitcnt(0x0f70 | (LATER & 15) | (LATER >> 4) << 14);
-            else __builtin_amdgcn_s_waitcnt(0x0f70);
+            [[maybe_unused]] constexpr int LATER = (FEW_RING - 1) * (LOADS + TM);
+            if constexpr (!ALIGNED) {
+#pragma unroll
+                for (int i = 0; i < LOADS; ++i) *reinterpret_cast<uint4 *>(ring + u * FEW_STAGE + (i * WAVE + lane) * 16) = kept[u][i];
+                __builtin_amdgcn_s_waitcnt(0xc07f);   // lgkmcnt(0)
+            } else {
+                asm volatile("" ::: "memory");
+                if (more) __builtin_amdgcn_s_waitcnt(0x0f70 | (LATER & 15) | (LATER >> 4) << 14);
+                else __builtin_amdgcn_s_waitcnt(0x0f70);
+            }
             wave_sync();
             Frag<T> fw[TN];
             Stage::template read<0>(ring + u * FEW_STAGE, at_w, fw);

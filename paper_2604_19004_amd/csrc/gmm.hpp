@@ -162,11 +162,16 @@ __device__ __forceinline__ void load_to_lds(const void *src, char *lds)
 {
     __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)src, (__attribute__((address_space(3))) void *)lds, 16, 0, 0);
 }
+// A piece from any address of the element type.
+template <class T> __device__ __forceinline__ uint4 load_any(const char *p)
+{
+    typedef uint32_t any_u32x4 __attribute__((ext_vector_type(4), aligned(2)));
+    return __builtin_bit_cast(uint4, (u32x4)*reinterpret_cast<const any_u32x4 *>(p));
+}
 // Up to a piece from any address of the element type; what lies behind `valid` elements is not read and 0.
 template <class T> __device__ __forceinline__ uint4 load_piece(const T *p, int valid)
 {
-    typedef uint32_t any_u32x4 __attribute__((ext_vector_type(4), aligned(2)));
-    if (valid >= PIECE<T>) return __builtin_bit_cast(uint4, (u32x4)*reinterpret_cast<const any_u32x4 *>(p));
+    if (valid >= PIECE<T>) return load_any<T>(reinterpret_cast<const char *>(p));
     Vec<T, PIECE<T>> e = {};
 #pragma unroll
     for (int i = 0; i < PIECE<T>; ++i)
@@ -315,6 +320,8 @@ struct Feed {
         if (!COL) return min(PIECE<T>, left - TI::piece_of(tid, i) * PIECE<T>);
         return TI::line_of(tid, i) >= left ? 0 : ASYNC ? PIECE<T> : min(PIECE<T>, room - TI::piece_of(tid, i) * PIECE<T>);
     }
+    // Whether all pieces of a step with `left` c are whole.
+    __device__ __forceinline__ bool whole(int left) const { return left == TI::LINE_C && (!COL || room >= TI::PIECES * PIECE<T>); }
     __device__ __forceinline__ const void *numbered(int tid, int i, int left, int64_t number, int64_t rows) const
     {
         return valid(tid, i, left) > 0 && (uint64_t)number < (uint64_t)rows ? static_cast<const void *>(row(i, number)) : &g_zero_piece;
@@ -465,6 +472,12 @@ __global__ void __launch_bounds__(WAVES_M * WAVES_N * WAVE, 2) k_gmm(GmmArgs a, 
         } else {
             auto move = [&](auto &feed, auto tile, uint4 *dst, bool by_number) {
                 using TI = decltype(tile);
+                if (!(DEPTH && by_number) && feed.whole(left)) {   // (the same for all: no lane looks at its pieces' ends)
+                    const char *base = feed.step(t);
+#pragma unroll
+                    for (int i = 0; i < TI::LOADS; ++i) dst[i] = load_any<T>(base + feed.off[i]);
+                    return;
+                }
 #pragma unroll
                 for (int i = 0; i < TI::LOADS; ++i) {
                     int valid = feed.valid(tid, i, left);
@@ -570,29 +583,7 @@ __global__ void __launch_bounds__(WAVES_M * WAVES_N * WAVE, 2) k_gmm(GmmArgs a, 
         __syncthreads();
     }
     f32x4 acc[TM][TN] = {};
-#pragma unroll
-    for (int t = 0; t < STAGES - 1; ++t)
-        if (t < steps) {
-            fetch(t, t);
-            stash(t);
-        }
-    int buffer = 0;
-    for (int t = 0; t < steps; ++t) {
-        // This wave's part of the step is in LDS (loads come back in order: all but those of later steps), and what it read of the step
-        // before has come; then everyone's is, and nobody reads the buffer of the step before any more.
-        constexpr int LATER = (STAGES - 2) * (TL::LOADS + TR::LOADS);
-        static_assert(LATER < 64, "what the counter holds");
-        if constexpr (ASYNC) {
-            asm volatile("" ::: "memory");
-            if (t + STAGES - 2 < steps) __builtin_amdgcn_s_waitcnt(0x0070 | (LATER & 15) | (LATER >> 4) << 14);
-            else __builtin_amdgcn_s_waitcnt(0x0070);
-            __builtin_amdgcn_s_barrier();
-            asm volatile("" ::: "memory");
-        } else {
-            __syncthreads();
-        }
-        const int next = buffer == 0 ? STAGES - 1 : buffer - 1;   // (that of the step before)
-        if (t + STAGES - 1 < steps) fetch(t + STAGES - 1, next);
+    auto multiply = [&](int buffer) {
         const char *from = lds + buffer * BUFFER;
         auto part = [&](auto half) {
             Frag<T> fr[TN], fl[TM];
@@ -605,9 +596,43 @@ __global__ void __launch_bounds__(WAVES_M * WAVES_N * WAVE, 2) k_gmm(GmmArgs a, 
         };
         part(std::integral_constant<int, 0>{});
         part(std::integral_constant<int, 1>{});
-        if (!ASYNC && t + 1 < steps) stash(next);
-        buffer = buffer + 1 == STAGES ? 0 : buffer + 1;
+    };
+    if constexpr (ASYNC) {
+#pragma unroll
+        for (int t = 0; t < STAGES - 1; ++t)
+            if (t < steps) fetch(t, t);
+        int buffer = 0;
+        for (int t = 0; t < steps; ++t) {
+            // This wave's part of the step is in LDS (loads come back in order: all but those of later steps), and what it read of the
+            // step before has come; then everyone's is, and nobody reads the buffer of the step before any more.
+            constexpr int LATER = (STAGES - 2) * (TL::LOADS + TR::LOADS);
+            static_assert(LATER < 64, "what the counter holds");
+            asm volatile("" ::: "memory");
+            if (t + STAGES - 2 < steps) __builtin_amdgcn_s_waitcnt(0x0070 | (LATER & 15) | (LATER >> 4) << 14);
+            else __builtin_amdgcn_s_waitcnt(0x0070);
+            __builtin_amdgcn_s_barrier();
+            asm volatile("" ::: "memory");
+            if (t + STAGES - 1 < steps) fetch(t + STAGES - 1, buffer == 0 ? STAGES - 1 : buffer - 1);   // (in place of the step before)
+            multiply(buffer);
+            buffer = buffer + 1 == STAGES ? 0 : buffer + 1;
+        }
+    } else {
+        // Through registers, one step ahead (two were no faster).
+        if (steps > 0) {
+            fetch(0, 0);
+            stash(0);
+        }
+        for (int t = 0; t < steps; ++t) {
+            asm volatile("" ::: "memory");
+            __builtin_amdgcn_s_waitcnt(0xc07f);   // lgkmcnt(0): what this wave wrote is in LDS, what it read has come
+            __builtin_amdgcn_s_barrier();
+            asm volatile("" ::: "memory");
+            if (t + 1 < steps) fetch(t + 1, 0);
+            multiply(t & 1);
+            if (t + 1 < steps) stash((t + 1) & 1);
+        }
     }
+
     if constexpr (MODE == GM_EXPAND) {
         // The adapters of the tile's rows: 64 bytes of h and b at a time (a unit), as many units a step as the tile has halves, h's parts side
         // by side and b's line again for each.  A row takes only its own adapter's products (not 0 times the others', which may be
@@ -711,8 +736,8 @@ template <class T, bool LCOL, bool RCOL, GmmMode MODE, class F> hipError_t launc
     auto tiles = [&](int64_t bm, int64_t bn) { return (double)m_tiles(bm) * (double)((a.n + bn - 1) / bn); };
     const double large = (double)(int64_t)((tiles(256, 256) + 255) / 256) * 2.0, middle = rounds(tiles(128, 128), 0.98, 1.22),
                  low = rounds(tiles(64, 128), 0.56, 0.92), small = rounds(tiles(64, 64), 0.42, 0.66);
-    if (!aligned) {   // (through registers, more tiles hide more)
-        if (tiles(128, 128) >= 512) return launch_gmm<T, LCOL, RCOL, 128, 128, 2, 2, false, 2, MODE>(a, s);
+    if (!aligned) {   // (through registers: 8356 rows of 4517 by four 832 x 4517, 462 tiles of 128 x 128, 171 us and 204 in those of 64 x 64)
+        if (tiles(128, 128) >= 256) return launch_gmm<T, LCOL, RCOL, 128, 128, 2, 2, false, 2, MODE>(a, s);
         return launch_gmm<T, LCOL, RCOL, 64, 64, 4, 1, false, 2, MODE>(a, s);
     }
     if constexpr (sizeof(T) == 2) {

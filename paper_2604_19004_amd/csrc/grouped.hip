@@ -33,7 +33,7 @@ __global__ void __launch_bounds__(WAVES * WAVE, 2) k_few(GmmArgs a)
         auto store = [&](int row, int64_t col, float v) { out[(m0 + row) * a.ldo + col] = (T)(s_row[row] < 0 ? 0.0f : v); };
         auto tile = [&](auto tm) {
             constexpr int TM = decltype(tm)::value;
-            if constexpr (RCOL) few_tile_col<T, TM, WAVES>(x, a.ldl, s_row, rows, w, a.ldr, n0, a.n, a.c, s_lds, store);
+            if constexpr (RCOL) few_tile_col<T, TM, WAVES, ALIGNED>(x, a.ldl, s_row, rows, w, a.ldr, n0, a.n, a.c, s_lds, store);
             else few_tile<T, TM, TN, WAVES, ALIGNED>(x, a.ldl, s_row, rows, w, a.ldr, n0, a.n, a.c, reinterpret_cast<float *>(s_lds),
                                                             [](int, int64_t) { return 0.0f; }, store);
         };
@@ -59,7 +59,7 @@ template <class T, bool LCOL, bool RCOL, GmmMode MODE> hipError_t pick_tile(cons
         // up to 32 and in tiles 30 (across c).
         if (groups > 0 && groups * ((a.n + 63) / 64) < 256 && a.rows <= groups * (RCOL ? 32 : 24)) {
             if constexpr (!RCOL) return aligned ? launch_few<T, false, 1, 8, true>(a, s) : launch_few<T, false, 1, 8, false>(a, s);
-            if (aligned) return launch_few<T, true, 4, 8, true>(a, s);
+            else return aligned ? launch_few<T, true, 4, 8, true>(a, s) : launch_few<T, true, 4, 8, false>(a, s);
         }
     }
     return launch_tiles<T, LCOL, RCOL, MODE>(a, [&](int64_t bm) {
