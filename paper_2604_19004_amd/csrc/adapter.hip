@@ -185,7 +185,7 @@ __global__ void __launch_bounds__(256) k_shrink_few(ocean_adapters l, const int3
     }
 }
 
-// The shared projection of 16, 32 or 64 rows (blockIdx.y-th 64) and TN * 16 columns, each result begun with the adapter's part.
+// The shared projection of 16, 32, 48 or 64 rows (blockIdx.y-th 64) and TN * 16 columns, each result begun with the adapter's part.
 constexpr int FEW_ROWS = 64;
 constexpr int64_t FEW_ROWS_MOST = 128;   // (64 adapters of rank 16, 4096 x 4096: 128 rows 39 us, in tiles 63; 192 61 and 61)
 template <class T, int TN, int WAVES, bool ALIGNED>
@@ -227,6 +227,7 @@ __global__ void __launch_bounds__(WAVES * WAVE, 2) k_adapter_few(ocean_adapters 
     };
     if (count <= 16) tile(std::integral_constant<int, 1>{});
     else if (count <= 32) tile(std::integral_constant<int, 2>{});
+    else if (count <= 48) tile(std::integral_constant<int, 3>{});
     else tile(std::integral_constant<int, 4>{});
 }
 
