@@ -85,11 +85,7 @@ __device__ __forceinline__ void few_tile(const T *x, int64_t ldx, const int64_t 
 #pragma unroll
         for (int u = 0; u < UNROLL; ++u)
 #pragma unroll
-            for (int h = 0; h < 2; ++h)
-#pragma unroll
-                for (int i = 0; i < TM; ++i)
-#pragma unroll
-                    for (int j = 0; j < TN; ++j) mma(acc[i][j], fw[u][h][j], fx[u][h][i]);
+            for (int h = 0; h < 2; ++h) mma<T>(acc, fw[u][h], fx[u][h]);
     }
     for (; t * S < c; t += WAVES) {
 #pragma unroll
@@ -100,10 +96,7 @@ __device__ __forceinline__ void few_tile(const T *x, int64_t ldx, const int64_t 
             for (int j = 0; j < TN; ++j) fw[j] = few_load<T, ALIGNED>(wp[j] + at, valid);
 #pragma unroll
             for (int i = 0; i < TM; ++i) fx[i] = few_load<T, ALIGNED>(xp[i] + at, valid);
-#pragma unroll
-            for (int i = 0; i < TM; ++i)
-#pragma unroll
-                for (int j = 0; j < TN; ++j) mma(acc[i][j], fw[j], fx[i]);
+            mma<T>(acc, fw, fx);
         }
     }
     few_finish<T, TM, TN, WAVES>(acc, first, rows, n0, n, lds, store);
@@ -177,10 +170,7 @@ __device__ __forceinline__ void few_tile_col(const T *x, int64_t ldx, const int6
             wave_sync();
             Frag<T> fw[TN];
             Stage::template read<0>(ring + u * FEW_STAGE, at_w, fw);
-#pragma unroll
-            for (int i = 0; i < TM; ++i)
-#pragma unroll
-                for (int j = 0; j < TN; ++j) mma(acc[i][j], fw[j], fx[u][i]);
+            mma<T>(acc, fw, fx[u]);
             wave_sync();
         }
     }

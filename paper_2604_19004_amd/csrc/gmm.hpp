@@ -31,20 +31,27 @@ template <class T> constexpr int PIECE = 16 / (int)sizeof(T);    // elements of 
 
 __device__ const uint4 g_zero_piece = {0u, 0u, 0u, 0u};     // what stands for pieces behind the end of c
 
-// acc += A * B for 64 bytes of c of 16 lines each: a lane has 16 bytes of line lane % 16, piece lane / 16.
-__device__ __forceinline__ void mma(f32x4 &acc, bf16x8 a, bf16x8 b) { acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, acc, 0, 0, 0); }
-__device__ __forceinline__ void mma(f32x4 &acc, f16x8 a, f16x8 b) { acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, acc, 0, 0, 0); }
-// (single precision: c in another order, the same one for both operands)
-__device__ __forceinline__ void mma(f32x4 &acc, f32x4 a, f32x4 b)
-{
-#pragma unroll
-    for (int j = 0; j < 4; ++j) acc = __builtin_amdgcn_mfma_f32_16x16x4f32(a[j], b[j], acc, 0, 0, 0);
-}
+// acc += A * B for 64 bytes of c of 16 lines each: a lane has 16 bytes of line lane % 16, piece lane / 16.  In as many parts as the type
+// takes matrix instructions (single precision: c in another order, the same one for both operands), so that a caller can put other
+// products between two of the same sum.
+template <class T> constexpr int MMA_PARTS = sizeof(T) == 4 ? 4 : 1;
+__device__ __forceinline__ void mma_part(f32x4 &acc, bf16x8 a, bf16x8 b, int) { acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, acc, 0, 0, 0); }
+__device__ __forceinline__ void mma_part(f32x4 &acc, f16x8 a, f16x8 b, int) { acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, acc, 0, 0, 0); }
+__device__ __forceinline__ void mma_part(f32x4 &acc, f32x4 a, f32x4 b, int p) { acc = __builtin_amdgcn_mfma_f32_16x16x4f32(a[p], b[p], acc, 0, 0, 0); }
 template <class T> struct FragOf;
 template <> struct FragOf<float> { using type = f32x4; };
 template <> struct FragOf<bf16_t> { using type = bf16x8; };
 template <> struct FragOf<f16_t> { using type = f16x8; };
 template <class T> using Frag = typename FragOf<T>::type;
+template <class T, int M, int N> __device__ __forceinline__ void mma(f32x4 (&acc)[M][N], const Frag<T> (&columns)[N], const Frag<T> (&rows)[M])
+{
+#pragma unroll
+    for (int p = 0; p < MMA_PARTS<T>; ++p)
+#pragma unroll
+        for (int i = 0; i < M; ++i)
+#pragma unroll
+            for (int j = 0; j < N; ++j) mma_part(acc[i][j], columns[j], rows[i], p);
+}
 
 // Which line of an operand lane r (0 .. 15) of 16 x 16 tile j reads: in order, or four tiles interleaved in fours.
 template <bool INTER> __device__ __forceinline__ int tile_line(int j, int r)
@@ -589,10 +596,7 @@ __global__ void __launch_bounds__(WAVES_M * WAVES_N * WAVE, 2) k_gmm(GmmArgs a, 
             Frag<T> fr[TN], fl[TM];
             TR::template read<decltype(half)::value>(from + TL::BYTES, at_r, fr);
             TL::template read<decltype(half)::value>(from, at_l, fl);
-#pragma unroll
-            for (int i = 0; i < TM; ++i)
-#pragma unroll
-                for (int j = 0; j < TN; ++j) mma(acc[i][j], fr[j], fl[i]);
+            mma<T>(acc, fr, fl);
         };
         part(std::integral_constant<int, 0>{});
         part(std::integral_constant<int, 1>{});
@@ -693,7 +697,8 @@ __global__ void __launch_bounds__(WAVES_M * WAVES_N * WAVE, 2) k_gmm(GmmArgs a, 
 #pragma unroll
                     for (int j = 0; j < TN; ++j) {
                         f32x4 sum = {};
-                        mma(sum, fr[j], fl[i]);
+#pragma unroll
+                        for (int p = 0; p < MMA_PARTS<T>; ++p) mma_part(sum, fr[j], fl[i], p);
 #pragma unroll
                         for (int k = 0; k < 4; ++k) acc[i][j][k] = mine ? acc[i][j][k] + back * sum[k] : acc[i][j][k];
                     }
