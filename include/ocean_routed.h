@@ -76,6 +76,13 @@ int ocean_combine_backward(const ocean_routing *r, const void *dout, int64_t ld_
                            int64_t width, void *dy, int64_t ld_dy, float *dval, ocean_stream_t stream);
 
 /*
+ * Sizes: rows and widths below 2^31 - 4096, experts of a grouped product at most OCEAN_GROUPS_MAX (each workgroup finds its group by
+ * going through their offsets).  Straight loads to LDS address 4 GB from a matrix's first row that a workgroup
+ * needs: gathered rows of an x larger than that go through registers, which is slower and otherwise the same.
+ */
+#define OCEAN_GROUPS_MAX 16384
+
+/*
  * Products of ragged groups of rows with their group's matrix.  Group e has rows group_ptr[e] .. group_ptr[e+1]-1 of `rows`
  * rows (group_ptr: experts + 1 ascending offsets; values outside 0 .. rows are limited to it).  With row_index, row s of the left matrix
  * is row row_index[s] of x (an index outside 0 .. x_rows-1 stands for a row of zeros); NULL: row s itself, and x_rows = rows.

@@ -84,7 +84,7 @@ template <class T, int PIECES> __device__ __forceinline__ int col_xor(int c)
 __device__ __forceinline__ uint32_t lds_address(const char *p) { return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const char *)p; }
 template <int OFFSET, int NEXT, int N> __device__ __forceinline__ void read_transposed(const uint32_t (&at)[N], s16x8 (&out)[N])
 {
-    static_assert(N == 1 || N == 2 || N % 4 == 0, "one, two or fours");
+    static_assert(N == 1 || N == 2 || N % 4 == 0, "one, two, fours or eights");
     s16x4 v[2 * N];
     if constexpr (N == 1) {
         asm volatile("ds_read_b64_tr_b16 %0, %2 offset:%3\n\tds_read_b64_tr_b16 %1, %2 offset:%4\n\ts_waitcnt lgkmcnt(0)"
@@ -93,16 +93,30 @@ template <int OFFSET, int NEXT, int N> __device__ __forceinline__ void read_tran
         asm volatile("ds_read_b64_tr_b16 %0, %4 offset:%6\n\tds_read_b64_tr_b16 %1, %4 offset:%7\n\t"
                      "ds_read_b64_tr_b16 %2, %5 offset:%6\n\tds_read_b64_tr_b16 %3, %5 offset:%7\n\ts_waitcnt lgkmcnt(0)"
                      : "=&v"(v[0]), "=&v"(v[1]), "=&v"(v[2]), "=&v"(v[3]) : "v"(at[0]), "v"(at[1]), "n"(OFFSET), "n"(OFFSET + NEXT) : "memory");
+    } else if constexpr (N % 8 == 0) {
+#pragma unroll
+        for (int k = 0; k < 2 * N; k += 16)
+            asm volatile("ds_read_b64_tr_b16 %0, %16 offset:%24\n\tds_read_b64_tr_b16 %1, %16 offset:%25\n\t"
+                         "ds_read_b64_tr_b16 %2, %17 offset:%24\n\tds_read_b64_tr_b16 %3, %17 offset:%25\n\t"
+                         "ds_read_b64_tr_b16 %4, %18 offset:%24\n\tds_read_b64_tr_b16 %5, %18 offset:%25\n\t"
+                         "ds_read_b64_tr_b16 %6, %19 offset:%24\n\tds_read_b64_tr_b16 %7, %19 offset:%25\n\t"
+                         "ds_read_b64_tr_b16 %8, %20 offset:%24\n\tds_read_b64_tr_b16 %9, %20 offset:%25\n\t"
+                         "ds_read_b64_tr_b16 %10, %21 offset:%24\n\tds_read_b64_tr_b16 %11, %21 offset:%25\n\t"
+                         "ds_read_b64_tr_b16 %12, %22 offset:%24\n\tds_read_b64_tr_b16 %13, %22 offset:%25\n\t"
+                         "ds_read_b64_tr_b16 %14, %23 offset:%24\n\tds_read_b64_tr_b16 %15, %23 offset:%25\n\t"
+                         "s_waitcnt lgkmcnt(0)"
+                         : "=&v"(v[k + 0]), "=&v"(v[k + 1]), "=&v"(v[k + 2]), "=&v"(v[k + 3]), "=&v"(v[k + 4]), "=&v"(v[k + 5]), "=&v"(v[k + 6]), "=&v"(v[k + 7]), "=&v"(v[k + 8]), "=&v"(v[k + 9]), "=&v"(v[k + 10]), "=&v"(v[k + 11]), "=&v"(v[k + 12]), "=&v"(v[k + 13]), "=&v"(v[k + 14]), "=&v"(v[k + 15])
+                         : "v"(at[k / 2 + 0]), "v"(at[k / 2 + 1]), "v"(at[k / 2 + 2]), "v"(at[k / 2 + 3]), "v"(at[k / 2 + 4]), "v"(at[k / 2 + 5]), "v"(at[k / 2 + 6]), "v"(at[k / 2 + 7]), "n"(OFFSET), "n"(OFFSET + NEXT) : "memory");
     } else {
 #pragma unroll
-        for (int k = 0; k < N; k += 4)
+        for (int k = 0; k < 2 * N; k += 8)
             asm volatile("ds_read_b64_tr_b16 %0, %8 offset:%12\n\tds_read_b64_tr_b16 %1, %8 offset:%13\n\t"
                          "ds_read_b64_tr_b16 %2, %9 offset:%12\n\tds_read_b64_tr_b16 %3, %9 offset:%13\n\t"
                          "ds_read_b64_tr_b16 %4, %10 offset:%12\n\tds_read_b64_tr_b16 %5, %10 offset:%13\n\t"
-                         "ds_read_b64_tr_b16 %6, %11 offset:%12\n\tds_read_b64_tr_b16 %7, %11 offset:%13\n\ts_waitcnt lgkmcnt(0)"
-                         : "=&v"(v[2 * k]), "=&v"(v[2 * k + 1]), "=&v"(v[2 * k + 2]), "=&v"(v[2 * k + 3]), "=&v"(v[2 * k + 4]), "=&v"(v[2 * k + 5]),
-                           "=&v"(v[2 * k + 6]), "=&v"(v[2 * k + 7])
-                         : "v"(at[k]), "v"(at[k + 1]), "v"(at[k + 2]), "v"(at[k + 3]), "n"(OFFSET), "n"(OFFSET + NEXT) : "memory");
+                         "ds_read_b64_tr_b16 %6, %11 offset:%12\n\tds_read_b64_tr_b16 %7, %11 offset:%13\n\t"
+                         "s_waitcnt lgkmcnt(0)"
+                         : "=&v"(v[k + 0]), "=&v"(v[k + 1]), "=&v"(v[k + 2]), "=&v"(v[k + 3]), "=&v"(v[k + 4]), "=&v"(v[k + 5]), "=&v"(v[k + 6]), "=&v"(v[k + 7])
+                         : "v"(at[k / 2 + 0]), "v"(at[k / 2 + 1]), "v"(at[k / 2 + 2]), "v"(at[k / 2 + 3]), "n"(OFFSET), "n"(OFFSET + NEXT) : "memory");
     }
 #pragma unroll
     for (int k = 0; k < N; ++k) out[k] = __builtin_shufflevector(v[2 * k], v[2 * k + 1], 0, 1, 2, 3, 4, 5, 6, 7);
@@ -360,10 +374,12 @@ __global__ void __launch_bounds__(WAVES_M * WAVES_N * WAVE, 2) k_gmm(GmmArgs a, 
             banded(item, mt, nt, 4, mi, ni);
             lo = mi * BM;
         } else if constexpr (DEPTH) {
-            const int item = by_die(number, mt * nt * (int)a.groups);
-            if (item < 0) return false;
-            w.group = item / (mt * nt);
-            banded(item - w.group * mt * nt, mt, nt, 4, mi, ni);
+            // (each die has a stretch of every group's tiles, another one of each: a group's tiles take as long as it is deep)
+            const int per = (mt * nt + 7) >> 3;
+            w.group = number / per;
+            const int item = (((int)blockIdx.x + w.group) & 7) * per + number - w.group * per;
+            if (w.group >= a.groups || item >= mt * nt) return false;
+            banded(item, mt, nt, 4, mi, ni);
             group_range(a, w.group, w.c_lo, w.c_hi);
             lo = mi * BM;
             w.hi = (int)a.m;
@@ -720,7 +736,7 @@ hipError_t launch_gmm(const GmmArgs &a, hipStream_t s)
     const int64_t nt = (a.n + BN - 1) / BN;
     const int64_t mt = MODE == GM_DEPTH ? (a.m + BM - 1) / BM : MODE == GM_EXPAND ? (a.rows + BM - 1) / BM : a.rows / BM + std::min(a.groups, a.rows) + 1;
     // (GM_ROWS: the last 8 at least have no tile and clear the rows of no group)
-    const int64_t blocks = (MODE == GM_ROWS ? 8 : 0) + up8(mt * nt * (MODE == GM_DEPTH ? a.groups : MODE == GM_SHRINK ? (a.c + a.c_part - 1) / a.c_part : 1));
+    const int64_t blocks = (MODE == GM_ROWS ? 8 : 0) + (MODE == GM_DEPTH ? up8(mt * nt) * a.groups : up8(mt * nt * (MODE == GM_SHRINK ? (a.c + a.c_part - 1) / a.c_part : 1)));
     constexpr int threads = WAVES_M * WAVES_N * WAVE;
     if (blocks * threads >= (1ll << 32)) return hipErrorInvalidConfiguration;
     hipLaunchKernelGGL((k_gmm<T, LCOL, RCOL, BM, BN, WAVES_M, WAVES_N, ASYNC, STAGES, MODE, O>), dim3((uint32_t)blocks), dim3(threads), 0, s, a, (int)mt, (int)nt);

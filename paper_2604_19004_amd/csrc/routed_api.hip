@@ -46,8 +46,8 @@ const char *routing_fault(const ocean_routing *r, bool need_val, bool need_all)
 const char *groups_fault(const ocean_groups *g)
 {
     if (!g) return "the groups are null";
-    if (g->rows < 0 || g->rows >= MAX_DIM || g->experts < 0 || g->experts > (1 << 20) || g->x_rows < 0 || g->x_rows >= MAX_DIM)
-        return "rows, experts or x_rows out of range";
+    if (g->rows < 0 || g->rows >= MAX_DIM || g->experts < 0 || g->experts > OCEAN_GROUPS_MAX || g->x_rows < 0 || g->x_rows >= MAX_DIM)
+        return "rows, experts (OCEAN_GROUPS_MAX) or x_rows out of range";
     if (!g->group_ptr) return "group_ptr is null";
     if (!g->row_index && g->rows > 0 && g->x_rows != g->rows) return "without row_index, x_rows must be rows";
     return nullptr;
