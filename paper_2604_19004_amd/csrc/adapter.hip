@@ -187,7 +187,12 @@ __global__ void __launch_bounds__(256) k_shrink_few(ocean_adapters l, const int3
 
 // The shared projection of 16, 32, 48 or 64 rows (blockIdx.y-th 64) and TN * 16 columns, each result begun with the adapter's part.
 constexpr int FEW_ROWS = 64;
-constexpr int64_t FEW_ROWS_MOST = 128;   // (64 adapters of rank 16, 4096 x 4096: 128 rows 39 us, in tiles 63; 192 61 and 61)
+// Few rows: up to 128 (64 adapters of rank 16, 4096 x 4096: 39 us, in tiles 63; 192 rows 61 and 61), more while there are workgroups for one round
+// only and the adapters' rows, which each row reads for itself, are not many (4096 x 1024, rank 64: 256 rows 45 us, in tiles 57).
+inline bool few_enough(int64_t rows, int64_t outer, int64_t rank)
+{
+    return rows <= 128 || (rows * rank <= 20480 && (outer + 15) / 16 * ((rows + FEW_ROWS - 1) / FEW_ROWS) <= 320);
+}
 template <class T, int TN, int WAVES, bool ALIGNED>
 __global__ void __launch_bounds__(WAVES * WAVE, 2) k_adapter_few(ocean_adapters l, const int32_t *ids, const T *x, int64_t ldx, int64_t inner, int64_t rows,
                                                                  const T *w, int64_t ldw, int64_t outer, T *y, int64_t ldy, const float *h, int rank_up)
@@ -279,7 +284,7 @@ hipError_t launch_adapter(const ocean_adapters &l, const int32_t *ids, int dtype
     const int64_t adapters = none ? 0 : l.adapters;
     const bool x_fits = offsets_fit(std::max<int64_t>(rows, 256), ldx, size);
     const AdapterSpace sp = adapter_space(workspace, rows, inner, l.adapters, l.rank, dtype);
-    if (rows <= FEW_ROWS_MOST) {
+    if (few_enough(rows, outer, l.rank)) {
         return with_type(dtype, [&](auto t) {
             using T = decltype(t);
             return launch_few_rows(l, ids, rows, inner, outer, static_cast<const T *>(x), ldx, static_cast<const T *>(w), ldw, static_cast<T *>(y), ldy,

@@ -296,7 +296,8 @@ __device__ __forceinline__ int by_die(int number, int items)
     return number < per && item < items ? item : -1;
 }
 
-// m-tiles by n-tiles in bands of `band` m-tiles, so that workgroups that run together share lines of both operands.
+// m-tiles by n-tiles in bands of `band` m-tiles, so that workgroups that run together share lines of both operands (32568 rows of 4096 by eight
+// 8192 x 4096 2.24 ms in bands of 2, 2.12 in those of 4, 2.10 in those of 8).
 __device__ __forceinline__ void banded(int item, int mt, int nt, int band, int &m, int &n)
 {
     const int per = band * nt, b = item / per, in = item - b * per, height = min(band, mt - b * band);
@@ -371,7 +372,7 @@ __global__ void __launch_bounds__(WAVES_M * WAVES_N * WAVE, 2) k_gmm(GmmArgs a, 
         if constexpr (MODE == GM_EXPAND) {
             const int item = by_die(number, mt * nt);
             if (item < 0) return false;
-            banded(item, mt, nt, 4, mi, ni);
+            banded(item, mt, nt, 8, mi, ni);
             lo = mi * BM;
         } else if constexpr (DEPTH) {
             // (each die has a stretch of every group's tiles, another one of each: a group's tiles take as long as it is deep)
@@ -379,7 +380,7 @@ __global__ void __launch_bounds__(WAVES_M * WAVES_N * WAVE, 2) k_gmm(GmmArgs a, 
             w.group = number / per;
             const int item = (((int)blockIdx.x + w.group) & 7) * per + number - w.group * per;
             if (w.group >= a.groups || item >= mt * nt) return false;
-            banded(item, mt, nt, 4, mi, ni);
+            banded(item, mt, nt, 8, mi, ni);
             group_range(a, w.group, w.c_lo, w.c_hi);
             lo = mi * BM;
             w.hi = (int)a.m;
@@ -393,7 +394,7 @@ __global__ void __launch_bounds__(WAVES_M * WAVES_N * WAVE, 2) k_gmm(GmmArgs a, 
                     w.stretch = item / (n * nt);
                     item -= w.stretch * n * nt;
                 }
-                banded(item, n, nt, 4, mi, ni);
+                banded(item, n, nt, 8, mi, ni);
                 return mi;
             };
             if (!find_tile(a, BM, item_of, w.group, lo, w.hi)) return false;
