@@ -25,7 +25,8 @@ constexpr int64_t MAX_DIM = (1ll << 31) - 4096;   // rows and widths are below t
 const char *matrix_fault(const void *p, int64_t rows, int64_t width, int64_t ld, int dtype)
 {
     if (rows < 0 || rows >= MAX_DIM || width < 0 || width >= MAX_DIM) return "a matrix's size is negative or not below 2^31 - 4096";
-    if (ld < width || ld >= (1ll << 40)) return "a row stride is less than the row's width";
+    if (ld < width) return "a row stride is less than the row's width";
+    if (ld >= (1ll << 40) || (rows > 1 && ld > (1ll << 46) / rows)) return "a matrix spans more than 2^46 elements";
     if (rows > 0 && width > 0 && !p) return "a matrix is null";
     if (!aligned(p, type_size(dtype))) return "a matrix is not aligned to its type";
     return nullptr;

@@ -3,7 +3,7 @@
 A routing matrix (tokens x experts, k entries a row) is made from logits, applied to the rows that the experts gave, and
 differentiated; the ragged groups of rows that it forms are multiplied with their experts' weights; and rows that each name a
 low-rank adapter are projected with it.  Every step runs in the HIP library, on the current stream or the one given; outputs and
-workspaces are torch tensors of that stream, nothing synchronises, and calls can be captured into a graph.  There is no CPU fallback.
+workspaces are torch tensors of that stream, nothing synchronises, and calls can be captured into a graph.  An `out` may not overlap what is read.  There is no CPU fallback.
 
 A training step of an experts' block, for x [T, D], w1 [E, F, D], w2 [E, D, F]:
 

@@ -81,3 +81,18 @@ def test_calls_on_the_cpu_raise(rt):
         rt.route(x, 2)
     with pytest.raises((RuntimeError, ValueError)):
         rt.grouped_matmul(x, torch.zeros(2, 8, 8), torch.zeros(3, dtype=torch.int64))
+
+
+def test_refusals_of_sizes(rt):
+    lib = rt.load()
+    b = ctypes.byref
+    many = rt.ocean_groups(10, 16385, 0x1000, None, 10)
+    two = rt.ocean_groups(10, 2, 0x1000, None, 10)
+    for rc, word in ((lambda: lib.ocean_grouped_matmul(b(many), 1, 4, 4, 0x1000, 4, 0x1000, 4, 16, 0, 0x1000, 4, None), "OCEAN_GROUPS_MAX"),
+                     (lambda: lib.ocean_grouped_matmul(b(two), 1, 4, 4, 0x1000, 3, 0x1000, 4, 16, 0, 0x1000, 4, None), "row stride"),
+                     (lambda: lib.ocean_grouped_matmul(b(two), 1, 4, 4, 0x1000, 1 << 45, 0x1000, 4, 16, 0, 0x1000, 4, None), "2^46"),
+                     (lambda: lib.ocean_grouped_matmul(b(two), 1, 4, 4, 0x1002, 4, 0x1000, 4, 16, 0, 0x1000, 4, None), "aligned"),
+                     (lambda: lib.ocean_grouped_matmul(b(two), 1, 4, 4, 0x1000, 4, 0x1000, 4, -16, 0, 0x1000, 4, None), "stride"),
+                     (lambda: lib.ocean_grouped_weight_grad(b(two), 1, 4, 4, 0x1000, 4, 0x1000, 4, 0x1000, 4, 15, 0, None), "overlap"),
+                     (lambda: lib.ocean_grouped_weight_grad(b(two), 1, 4, 4, 0x1000, 4, 0x1000, 4, 0x1000, 1 << 39, 16, 0, None), "overlap")):
+        assert rc() == 1 and word in lib.ocean_last_error().decode(), word
