@@ -46,7 +46,7 @@ AdapterSpace adapter_space(void *at, int64_t rows, int64_t inner, int64_t adapte
 }
 
 // Slots of every adapter.  The order of an adapter's rows is that of arrival and may change from call to call: no result depends on
-// it, since a row's sums do not depend on its place in a tile.
+// it, since a row's sums do not depend on its place in a tile.  One workgroup (6000 rows 8 us of the 290 that all of it takes).
 __global__ void __launch_bounds__(1024) k_order_rows(const int32_t *ids, int64_t rows, int adapters, AdapterSpace w)
 {
     __shared__ uint32_t s_at[OCEAN_ADAPTER_MAX + 1];
@@ -148,7 +148,8 @@ __global__ void __launch_bounds__(256) k_finish_shrink(AdapterSpace w, int64_t r
     }
 }
 
-// Few rows.  h[row][r .. r + 3] = scale * x[row] * A^T, one wave each; nothing for rows without an adapter and behind its rank.
+// Few rows.  h[row][r .. r + 3] = scale * x[row] * A^T, one wave each; nothing for rows without an adapter and behind its rank.  Bound by the wave's
+// own chain of loads (48 rows, rank 16, c = 4096 in bfloat16: 5 us).
 constexpr int FEW_R = 4;
 template <class T, bool ALIGNED>
 __global__ void __launch_bounds__(256) k_shrink_few(ocean_adapters l, const int32_t *ids, const T *x, int64_t ldx, int64_t inner, int64_t rows,
@@ -185,7 +186,8 @@ __global__ void __launch_bounds__(256) k_shrink_few(ocean_adapters l, const int3
     }
 }
 
-// The shared projection of 16, 32, 48 or 64 rows (blockIdx.y-th 64) and TN * 16 columns, each result begun with the adapter's part.
+// The shared projection of 16, 32, 48 or 64 rows (blockIdx.y-th 64) and TN * 16 columns, each result begun with the adapter's part.  Up to 16 rows it
+// is bound by W's bytes (4096 x 4096 in bfloat16: 9 us), with more by the rows, which every workgroup reads from the L2 (48: 19 us, 17 without adapters).
 constexpr int FEW_ROWS = 64;
 // Few rows: up to 128 (64 adapters of rank 16, 4096 x 4096: 39 us, in tiles 63; 192 rows 61 and 61), more while there are workgroups for one round
 // only and the adapters' rows, which each row reads for itself, are not many (4096 x 1024, rank 64: 256 rows 45 us, in tiles 57).

@@ -76,7 +76,7 @@ template <int G> __device__ __forceinline__ float lanes_sum(float v)
 
 // Takes the largest logits of the block's rows.  G lanes share a row, lane l has columns l, l + G, ...: the largest key, then the lowest
 // column that holds it, k times.  Bound by instructions, some thirty a turn whatever G is: four rows in 16 lanes each take a third of the
-// time of a row a wave (32768 rows of 100, 8 taken: 14 us instead of 40; a large copy's rate would be 5).  A row's softmax is relative to
+// time of a row a wave (32768 rows of 100, 8 taken: 17 us instead of 40; at the rate of a large copy the bytes would take 3).  A row's softmax is relative to
 // its largest logit.  The bits of s_mask (expert: which of the 64 rows took it) give the entries' rank among the block's of the same
 // column without an order of arrival.
 template <class T, int G, int NV, class Put>
@@ -156,7 +156,7 @@ __global__ void __launch_bounds__(1024) k_route_pick(const T *logits, int64_t ld
     }
 }
 
-// A single block: all in one launch, and no workspace.
+// A single block: all in one launch, and no workspace (64 rows of 64 in bfloat16, 4 taken: 5 us, the chain of loads, turns and scans).
 template <class T, int G, int NV>
 __global__ void __launch_bounds__(1024) k_route_one(const T *logits, int64_t ld, int tokens, int experts, int k, int normalize, ocean_routing r)
 {
@@ -212,7 +212,7 @@ __global__ void __launch_bounds__(1024) k_route_one(const T *logits, int64_t ld,
     }
 }
 
-// Entries of earlier blocks, per expert (one workgroup each), and the expert's entries.
+// Entries of earlier blocks, per expert (one workgroup each), and the expert's entries (512 blocks, 100 experts: 4 us, a launch and one scan).
 __global__ void __launch_bounds__(PLACE_TPB) k_route_scan(uint32_t *count, uint32_t *total, int64_t blocks)
 {
     __shared__ uint32_t s_wave[PLACE_TPB / WAVE];
@@ -235,7 +235,7 @@ __global__ void __launch_bounds__(PLACE_TPB) k_route_scan(uint32_t *count, uint3
     if (threadIdx.x == 0) total[blockIdx.x] = before;
 }
 
-// Entries go to their places in both orders.
+// Entries go to their places in both orders (32768 rows of 100, 8 taken: 6 us, 5 MB of entries).
 __global__ void __launch_bounds__(PLACE_TPB) k_route_place(RouteSpace w, int64_t blocks, int tokens, int experts, int k, ocean_routing r)
 {
     __shared__ uint32_t s_base[OCEAN_ROUTE_MAX_EXPERTS];   // slot of the block's first entry of each expert
@@ -291,7 +291,8 @@ __global__ void __launch_bounds__(PLACE_TPB) k_route_place(RouteSpace w, int64_t
 }
 
 // Gradient of a row's logits, G lanes a row.  Weights over the entries taken: dl_c = w_c (g_c - m) with m = sum w g;
-// over all: p_e ([e taken] g_e - m).
+// over all: p_e ([e taken] g_e - m).  The row's gradient is put together in LDS, where an entry finds its column; in single precision, 32768
+// rows of 100, 8 taken, over all: 13 us, 6 of them instructions (the softmax again) and 5 the bytes at the rate of a large copy.
 template <class T, int G, int NV>
 __global__ void __launch_bounds__(256) k_route_backward(ocean_routing r, const float *dval, const T *logits, int64_t ld, int normalize,
                                                         T *dlogits, int64_t ldd)
