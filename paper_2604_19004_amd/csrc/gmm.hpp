@@ -200,11 +200,12 @@ template <class T> __device__ __forceinline__ uint4 load_piece(const T *p, int v
     return __builtin_bit_cast(uint4, e);
 }
 
-// A piece to any address of the element type.
-template <class T> __device__ __forceinline__ void store_any(T *p, const Vec<T, PIECE<T>> &v)
+// A piece to any address of the element type; past the cache or not.
+template <bool PAST, class T> __device__ __forceinline__ void store_any(T *p, const Vec<T, PIECE<T>> &v)
 {
     typedef uint32_t any_u32x4 __attribute__((ext_vector_type(4), aligned(2)));
-    *reinterpret_cast<any_u32x4 *>(p) = __builtin_bit_cast(u32x4, v);
+    if constexpr (PAST) __builtin_nontemporal_store((any_u32x4)__builtin_bit_cast(u32x4, v), reinterpret_cast<any_u32x4 *>(p));
+    else *reinterpret_cast<any_u32x4 *>(p) = __builtin_bit_cast(u32x4, v);
 }
 
 namespace {
@@ -545,6 +546,9 @@ __global__ void __launch_bounds__(WAVES_M * WAVES_N * WAVE, 2) k_gmm(GmmArgs a, 
     auto store = [&](const f32x4 (&acc)[TM][TN]) {
         constexpr int RUN = RCOL ? 1 : 4;         // tiles whose columns a lane has side by side
         constexpr int E = PIECE<O>, ROW = WN * (int)sizeof(O), PIECES = ROW / 16, ROWS = WAVE / PIECES;
+        // (256 of the largest tiles are as much as the dies' caches hold: past them, so that the operands' lines stay; 32768 rows, 32 groups, 2048 x 1400,
+        // both gradients 461 us, else 500)
+        constexpr bool PAST = BM * BN >= 256 * 256;
         static_assert(BM * BN * sizeof(O) <= sizeof(lds) && PIECES >= 8, "room for the results");
         char *mine = lds + wave * (WM * ROW);
         auto place = [&](int row, int col) { return mine + row * ROW + ((col / E ^ (row & 7)) * 16 + col % E * (int)sizeof(O)); };
@@ -578,7 +582,7 @@ __global__ void __launch_bounds__(WAVES_M * WAVES_N * WAVE, 2) k_gmm(GmmArgs a, 
             if constexpr (MODE == GM_EXPAND) at = a.index[slot];
             O *p = out + at * a.ldo + col;
             if (valid == E) {
-                store_any(p, o);
+                store_any<PAST>(p, o);
             } else {
 #pragma unroll
                 for (int k = 0; k < E; ++k)
@@ -751,20 +755,33 @@ hipError_t launch_gmm(const GmmArgs &a, hipStream_t s)
     return hipGetLastError();
 }
 
-// Which tile: the one whose rounds over the chip's 256 compute units take the least.  A round is one tile of 256 x 256 a unit, or two of the
-// others; what a round takes, or half of one (a tile a unit), in units of half a round of the largest: measured at c = 4096 in bfloat16 as
-// 135 us for 256 tiles of 256 x 256, 82 for 512 of 128 x 128 and 66 for 256, 62 and 38 of 64 x 128, 45 and 28 of 64 x 64.
+// Which tile: the one whose rounds over the chip's 256 compute units take the least.  A round is one tile of 256 x 256 or 128 x 256 a unit, or two
+// of the others; what a round takes, or half of one (a tile a unit), in units of half a round of the largest: measured at c = 4096 in bfloat16 as
+// 117 us for 256 tiles of 256 x 256, 68 of 128 x 256, 66 for 512 of 128 x 128 and 52 for 256, 40 and 32 of 64 x 128, 29 and 26 of 64 x 64.
 inline double rounds(double tiles, double half, double full)
 {
     const double whole = (double)(int64_t)(tiles / 512), rest = tiles - whole * 512;
     return whole * full + (rest > 256 ? full : rest > 0 ? half : 0.0);
 }
+// (a last round of few tiles is shorter, the others' power goes to them: 1152 tiles 228 us, a round of 256 57)
+inline double large_rounds(double tiles)
+{
+    const double whole = (double)(int64_t)(tiles / 256), rest = tiles - whole * 256;
+    return whole * 2.0 + (rest > 0 ? 1.5 + rest / 512 : 0.0);
+}
 // m_tiles(lines): about how many tiles of that many lines there are.
 template <class T, bool LCOL, bool RCOL, GmmMode MODE, class F> hipError_t launch_tiles(const GmmArgs &a, F m_tiles, bool aligned, hipStream_t s)
 {
     auto tiles = [&](int64_t bm, int64_t bn) { return (double)m_tiles(bm) * (double)((a.n + bn - 1) / bn); };
-    const double large = (double)(int64_t)((tiles(256, 256) + 255) / 256) * 2.0, middle = rounds(tiles(128, 128), 0.98, 1.22),
-                 low = rounds(tiles(64, 128), 0.56, 0.92), small = rounds(tiles(64, 64), 0.42, 0.66);
+    // (adapters: 128 x 256 instead of 128 x 128, since each of a tile's columns goes through the adapters of its rows: 6000 rows of 4096, 4096 columns, rank
+    // 64, 245 us and 271)
+    constexpr bool WIDE = MODE == GM_EXPAND && sizeof(T) == 2;
+    // (gradients of weights in a single round wait for the deepest group: 8 uneven groups, 32768 rows, 2048 x 1024, in 256 tiles of 256 x 256 264
+    // us, in 1024 of 128 x 128 170; with even ones some 130 and 165)
+    const double alone = MODE == GM_DEPTH && a.groups > 1 && tiles(256, 256) <= 256 ? 1.6 : 1.0;
+    const double large = large_rounds(tiles(256, 256)) * alone,
+                 middle = WIDE ? (double)(int64_t)((tiles(128, 256) + 255) / 256) * 1.16 : rounds(tiles(128, 128), 0.89, 1.13),
+                 low = rounds(tiles(64, 128), 0.55, 0.69), small = rounds(tiles(64, 64), 0.44, 0.50);
     if (!aligned) {   // (through registers: 8356 rows of 4517 by four 832 x 4517, 462 tiles of 128 x 128, 171 us and 204 in those of 64 x 64)
         if (tiles(128, 128) >= 256) return launch_gmm<T, LCOL, RCOL, 128, 128, 2, 2, false, 2, MODE>(a, s);
         return launch_gmm<T, LCOL, RCOL, 64, 64, 4, 1, false, 2, MODE>(a, s);
@@ -774,7 +791,10 @@ template <class T, bool LCOL, bool RCOL, GmmMode MODE, class F> hipError_t launc
         constexpr int DOWN = MODE == GM_DEPTH ? 4 : 2;
         if (large <= std::min(std::min(middle, low), small)) return launch_gmm<T, LCOL, RCOL, 256, 256, DOWN, 8 / DOWN, true, 2, MODE>(a, s);
     }
-    if (middle <= std::min(low, small)) return launch_gmm<T, LCOL, RCOL, 128, 128, 2, 2, true, 2, MODE>(a, s);
+    if (middle <= std::min(low, small)) {
+        if constexpr (WIDE) return launch_gmm<T, LCOL, RCOL, 128, 256, 2, 4, true, 3, MODE>(a, s);
+        else return launch_gmm<T, LCOL, RCOL, 128, 128, 2, 2, true, 2, MODE>(a, s);
+    }
     if (low <= small) return launch_gmm<T, LCOL, RCOL, 64, 128, 2, 2, true, 3, MODE>(a, s);
     return launch_gmm<T, LCOL, RCOL, 64, 64, 4, 1, true, 4, MODE>(a, s);
 }
