@@ -618,6 +618,21 @@ __global__ void __launch_bounds__(WAVES_M * WAVES_N * WAVE, 2) k_gmm(GmmArgs a, 
         __syncthreads();
     }
     f32x4 acc[TM][TN] = {};
+    // Single precision: the sums of eight steps (256 c) are put aside, so that the roundings of a long sum grow with the root of a 256th of its terms (c =
+    // 4096: a quarter of those of one running sum).  Results of 16 bits are rounded far above them.
+    constexpr bool ASIDE = sizeof(T) == 4;
+    f32x4 sums[ASIDE ? TM : 1][ASIDE ? TN : 1] = {};
+    auto put_aside = [&] {
+        if constexpr (ASIDE) {
+#pragma unroll
+            for (int i = 0; i < TM; ++i)
+#pragma unroll
+                for (int j = 0; j < TN; ++j) {
+                    sums[i][j] += acc[i][j];
+                    acc[i][j] = f32x4{};
+                }
+        }
+    };
     auto multiply = [&](int buffer) {
         const char *from = lds + buffer * BUFFER;
         auto part = [&](auto half) {
@@ -646,6 +661,7 @@ __global__ void __launch_bounds__(WAVES_M * WAVES_N * WAVE, 2) k_gmm(GmmArgs a, 
             asm volatile("" ::: "memory");
             if (t + STAGES - 1 < steps) fetch(t + STAGES - 1, buffer == 0 ? STAGES - 1 : buffer - 1);   // (in place of the step before)
             multiply(buffer);
+            if (ASIDE && t % 8 == 7) put_aside();
             buffer = buffer + 1 == STAGES ? 0 : buffer + 1;
         }
     } else {
@@ -661,8 +677,15 @@ __global__ void __launch_bounds__(WAVES_M * WAVES_N * WAVE, 2) k_gmm(GmmArgs a, 
             asm volatile("" ::: "memory");
             if (t + 1 < steps) fetch(t + 1, 0);
             multiply(t & 1);
+            if (ASIDE && t % 8 == 7) put_aside();
             if (t + 1 < steps) stash((t + 1) & 1);
         }
+    }
+    if constexpr (ASIDE) {
+#pragma unroll
+        for (int i = 0; i < TM; ++i)
+#pragma unroll
+            for (int j = 0; j < TN; ++j) acc[i][j] += sums[i][j];
     }
 
     if constexpr (MODE == GM_EXPAND) {

@@ -278,3 +278,19 @@ def test_refusals(rt):
                      (lambda: product(rt.ocean_groups(10, 2, ptr.data_ptr(), None, 9)), "x_rows"),
                      (lambda: lib.ocean_grouped_weight_grad(ctypes.byref(g), 1, 16, 8, at[2], 8, at[0], 16, at[1], 16, 100, 0, None), "overlap")):
         assert rc() == 1 and word in lib.ocean_last_error().decode()
+
+
+def test_long_sums_in_single_precision(rt):
+    """The sums of 256 products are put aside.  With numbers of either sign a sum of n terms, rounded at each of them by at most 2^-24 of what it has
+    come to, is off by 2^-24 sqrt(n / 2) of its size, taken over many results: 256 terms each, then c / 256 of these."""
+    import torch
+    g = torch.Generator(device="cuda").manual_seed(6)
+    for c in (4096, 8192, 8191):
+        x, w = torch.randn(400, c, device="cuda", generator=g), torch.randn(2, 200, c, device="cuda", generator=g)
+        dy, z = torch.randn(c, 136, device="cuda", generator=g), torch.randn(c, 200, device="cuda", generator=g)
+        ptr, one = torch.tensor([0, 150, 400], device="cuda"), torch.tensor([0, c], device="cuda")
+        want = torch.cat([x[:150].double() @ w[0].double().T, x[150:].double() @ w[1].double().T])
+        dw = dy.double().T @ z.double()
+        for got, ref in ((rt.grouped_matmul(x, w, ptr), want), (rt.grouped_matmul(x, w.transpose(1, 2).contiguous(), ptr, transposed=True), want),
+                         (rt.grouped_weight_grad(dy, z, one)[0], dw)):
+            assert float((got.double() - ref).norm() / ref.norm()) <= 2.0 ** -24 * (128 + c / 512) ** 0.5
