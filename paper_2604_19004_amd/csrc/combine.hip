@@ -64,20 +64,21 @@ __global__ void __launch_bounds__(256) k_combine(ocean_routing r, const T *y, in
     }
 }
 
-// One wave a token: the row of dout goes to the rows of its entries, and its products with the rows that the experts gave are
-// summed up across the lanes.  Rows that no entry names are cleared.  Bound by the bytes: 16384 rows of 2048 in bfloat16, four entries each,
-// 132 us or 4.5 TB/s (a large copy has 4.9).
+// `split` waves a token, each with every split-th of its entries: the row of dout goes to the entries' rows, and its products with the rows that the
+// experts gave are summed up across the lanes.  Rows that no entry names are cleared.  Bound by the bytes: 16384 rows of 2048 in bfloat16, four entries
+// each, 125 us or 4.8 TB/s (a large copy has 4.9).
 template <class T, int V>
 __global__ void __launch_bounds__(256) k_combine_backward(ocean_routing r, const T *dout, int64_t ldo, const T *y, int64_t ldy, int64_t width,
-                                                          T *dy, int64_t lddy, float *dval)
+                                                          T *dy, int64_t lddy, float *dval, int split)
 {
     const int lane = lane_id();
     const int64_t wave = (int64_t)blockIdx.x * (256 / WAVE) + threadIdx.x / WAVE, waves = (int64_t)gridDim.x * (256 / WAVE), cap = r.tokens * r.k;
     const int64_t n = min(max(r.row_ptr[r.tokens], (int64_t)0), cap);
-    for (int64_t t = wave; t < r.tokens; t += waves) {
+    for (int64_t item = wave; item < r.tokens * split; item += waves) {
+        const int64_t t = item / split;
         int64_t lo, hi;
         row_range(r, t, lo, hi);
-        for (int64_t p = lo; p < hi; ++p) {
+        for (int64_t p = lo + (item - t * split); p < hi; p += split) {
             const int64_t slot = r.slot[p];
             const bool there = (uint64_t)slot < (uint64_t)cap;
             const float w = r.val ? r.val[p] : 1.0f;
@@ -133,8 +134,11 @@ hipError_t launch_combine_backward(const ocean_routing &r, const void *dout, int
         using T = decltype(e);
         return with_vector<T>(vector_width(sizeof(T), width, {{dout, ldo}, {dval ? y : nullptr, ldy}, {dy, lddy}}), [&](auto v) {
             constexpr int V = decltype(v)::value;
-            hipLaunchKernelGGL((k_combine_backward<T, V>), dim3((uint32_t)std::min((r.tokens + 3) / 4, (int64_t)1 << 20)), dim3(256), 0, s, r,
-                               static_cast<const T *>(dout), ldo, static_cast<const T *>(y), ldy, width, static_cast<T *>(dy), lddy, dval);
+            // A wave an entry (16384 rows of 2048 in bfloat16, four entries each, 125 us and with a wave a row 133; 2019 of 6464 in single precision, seven
+            // each, 164 and 271), but not where many rows are only written (without dval, 32768 of 1024, eight each, 169 and 131; 16384 of 2048 75 and 89).
+            const int split = dval || r.tokens * r.k <= 65536 ? r.k : 1;
+            hipLaunchKernelGGL((k_combine_backward<T, V>), dim3((uint32_t)std::min((r.tokens * split + 3) / 4, (int64_t)1 << 20)), dim3(256), 0, s, r,
+                               static_cast<const T *>(dout), ldo, static_cast<const T *>(y), ldy, width, static_cast<T *>(dy), lddy, dval, split);
             return hipGetLastError();
         });
     });
