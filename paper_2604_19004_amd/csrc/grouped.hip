@@ -64,7 +64,7 @@ template <class T, bool LCOL, bool RCOL, GmmMode MODE> hipError_t pick_tile(cons
     }
     return launch_tiles<T, LCOL, RCOL, MODE>(a, [&](int64_t bm) {
         if (MODE == GM_DEPTH) return groups * ((a.m + bm - 1) / bm);
-        return a.rows <= groups * bm ? groups : a.rows / bm + groups / 2;   // (a group's last tile is half full on the average)
+        return std::max(groups, a.rows / bm + groups / 2);   // (a group's last tile is half full on the average)
     }, aligned, s);
 }
 
