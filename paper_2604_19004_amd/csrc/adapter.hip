@@ -46,7 +46,7 @@ AdapterSpace adapter_space(void *at, int64_t rows, int64_t inner, int64_t adapte
 }
 
 // Slots of every adapter.  The order of an adapter's rows is that of arrival and may change from call to call: no result depends on
-// it, since a row's sums do not depend on its place in a tile.  One workgroup (6000 rows 8 us of the 290 that all of it takes).
+// it, since a row's sums do not depend on its place in a tile.  One workgroup (6000 rows 8 us of the 255 that all of it takes).
 __global__ void __launch_bounds__(1024) k_order_rows(const int32_t *ids, int64_t rows, int adapters, AdapterSpace w)
 {
     __shared__ uint32_t s_at[OCEAN_ADAPTER_MAX + 1];

@@ -305,7 +305,7 @@ __device__ __forceinline__ int by_die(int number, int items)
 }
 
 // m-tiles by n-tiles in bands of `band` m-tiles, so that workgroups that run together share lines of both operands (32568 rows of 4096 by eight
-// 8192 x 4096 2.24 ms in bands of 2, 2.12 in those of 4, 2.10 in those of 8).
+// 8192 x 4096 2.24 ms in bands of 2, 2.12 in those of 4, 2.10 in those of 8, when results still left in half lines).
 __device__ __forceinline__ void banded(int item, int mt, int nt, int band, int &m, int &n)
 {
     const int per = band * nt, b = item / per, in = item - b * per, height = min(band, mt - b * band);
@@ -359,7 +359,7 @@ struct Feed {
 };
 
 // One workgroup a tile, STAGES steps of both operands in LDS.  Large tiles are bound by the matrix cores, and those by what the card may draw: 32568 rows
-// of 4096 by eight 8192 x 4096 in bfloat16 take 2.02 ms, 1080 TFLOP/s (with zeros for numbers 1300; a library's largest product 1320), no bank conflict
+// of 4096 by eight 8192 x 4096 in bfloat16 take 1.9 to 2.0 ms, 1100 TFLOP/s (with zeros for numbers 1300; a library's largest product 1320), no bank conflict
 // counted.  Small ones are bound by the weights' bytes: two rows by two 8192 x 4096, 27 us or 5.1 TB/s.
 template <class T, bool LCOL, bool RCOL, int BM, int BN, int WAVES_M, int WAVES_N, bool ASYNC, int STAGES, GmmMode MODE, class O = T>
 __global__ void __launch_bounds__(WAVES_M * WAVES_N * WAVE, 2) k_gmm(GmmArgs a, int mt, int nt)
