@@ -189,8 +189,8 @@ __global__ void __launch_bounds__(256) k_shrink_few(ocean_adapters l, const int3
 // The shared projection of 16, 32, 48 or 64 rows (blockIdx.y-th 64) and TN * 16 columns, each result begun with the adapter's part.  Up to 16 rows it
 // is bound by W's bytes (4096 x 4096 in bfloat16: 9 us), with more by the rows, which every workgroup reads from the L2 (48: 19 us, 17 without adapters).
 constexpr int FEW_ROWS = 64;
-// Few rows: up to 128 (64 adapters of rank 16, 4096 x 4096: 39 us, in tiles 63; 192 rows 61 and 61), more while there are workgroups for one round
-// only and the adapters' rows, which each row reads for itself, are not many (4096 x 1024, rank 64: 256 rows 45 us, in tiles 57).
+// Few rows: up to 128 (64 adapters of rank 16, 4096 x 4096: 37 us, in tiles 64; 192 rows 61 and 61), more while there are workgroups for one round
+// only and the adapters' rows, which each row reads for itself, are not many (4096 x 1024, rank 64: 256 rows 45 us, in tiles 55).
 inline bool few_enough(int64_t rows, int64_t outer, int64_t rank)
 {
     return rows <= 128 || (rows * rank <= 20480 && (outer + 15) / 16 * ((rows + FEW_ROWS - 1) / FEW_ROWS) <= 320);

@@ -7,7 +7,7 @@
 // place in LDS is fixed by its number, so the XOR is applied to the source), otherwise through registers by unaligned loads.
 //
 // A 16 x 16 result tile of v_mfma_16x16 has its columns' operand first, so that a lane holds 4 columns of one row; the lines of R that
-// four such tiles read are interleaved in fours, so that a lane holds 16 consecutive columns and writes 32 or 64 bytes side by side (not in a col tile:
+// four such tiles read are interleaved in fours, so that a lane holds 16 consecutive columns, whole pieces of a result's line (not in a col tile:
 // the transposing read would use half of each piece).
 #pragma once
 
@@ -805,7 +805,7 @@ template <class T, bool LCOL, bool RCOL, GmmMode MODE, class F> hipError_t launc
     const double large = large_rounds(tiles(256, 256)) * alone,
                  middle = WIDE ? (double)(int64_t)((tiles(128, 256) + 255) / 256) * 1.16 : rounds(tiles(128, 128), 0.89, 1.13),
                  low = rounds(tiles(64, 128), 0.55, 0.69), small = rounds(tiles(64, 64), 0.44, 0.50);
-    if (!aligned) {   // (through registers: 8356 rows of 4517 by four 832 x 4517, 462 tiles of 128 x 128, 171 us and 204 in those of 64 x 64)
+    if (!aligned) {   // (through registers: 8356 rows of 4517 by four 832 x 4517, 462 tiles of 128 x 128, 121 us and 169 in those of 64 x 64)
         if (tiles(128, 128) >= 256) return launch_gmm<T, LCOL, RCOL, 128, 128, 2, 2, false, 2, MODE>(a, s);
         return launch_gmm<T, LCOL, RCOL, 64, 64, 4, 1, false, 2, MODE>(a, s);
     }

@@ -55,8 +55,8 @@ template <class T, bool LCOL, bool RCOL, GmmMode MODE> hipError_t pick_tile(cons
     const int64_t groups = MODE == GM_DEPTH ? a.groups : std::min(a.groups, a.rows);
     if constexpr (MODE == GM_ROWS) {
         // Where tiles of 64 x 64 would leave compute units without work, c is divided among the waves of a workgroup instead: eight
-        // products with 4096 x 1024 weights take 14 us with a row each, 19 with 16, 24 with 24 and in tiles 26 (lines along c); 20 to 27 with
-        // up to 32 and in tiles 30 (across c).
+        // products with 4096 x 1024 weights take 15 us with a row each, 19 with 16, 23 with 24 and in tiles 25 (lines along c); 15 to 22 with
+        // up to 32 and in tiles 29 (across c).
         if (groups > 0 && groups * ((a.n + 63) / 64) < 256 && a.rows <= groups * (RCOL ? 32 : 24)) {
             if constexpr (!RCOL) return aligned ? launch_few<T, false, 1, 8, true>(a, s) : launch_few<T, false, 1, 8, false>(a, s);
             else return aligned ? launch_few<T, true, 4, 8, true>(a, s) : launch_few<T, true, 4, 8, false>(a, s);
