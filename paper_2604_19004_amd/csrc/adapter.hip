@@ -102,10 +102,10 @@ __global__ void __launch_bounds__(1024) k_order_rows(const int32_t *ids, int64_t
     }
 }
 
-// h = scale * the stretches' sums, one wave a slot.  The row is divided by the power of two of its largest magnitude (row_scale, given
+// h = scale * the stretches' sums, one wave a slot.  The row is divided by the power of two of its largest finite magnitude (row_scale, given
 // back when its products are added), and a 16-bit type holds it as its rounding and the rounding of what is left: 16 or 22 bits
-// together, whatever the range of the type; 8 or 11 alone would be off by as much as the result's own rounding.  Columns behind the
-// adapter's rank are 0.
+// together, whatever the range of the type; 8 or 11 alone would be off by as much as the result's own rounding.  Of an infinity nothing is
+// left.  Columns behind the adapter's rank are 0.
 template <class T>
 __global__ void __launch_bounds__(256) k_finish_shrink(AdapterSpace w, int64_t rows, int rank, const int32_t *ranks, const float *scale)
 {
@@ -126,10 +126,11 @@ __global__ void __launch_bounds__(256) k_finish_shrink(AdapterSpace w, int64_t r
                 for (int64_t s = 0; s < w.stretches; ++s) v[i] += w.part[s * n + slot * w.rank_up + r];
                 v[i] *= c;
             }
-            largest = max(largest, __float_as_uint(v[i]) & 0x7fffffffu);
+            const uint32_t magnitude = __float_as_uint(v[i]) & 0x7fffffffu;
+            if (magnitude < 0x7f800000u) largest = max(largest, magnitude);
         }
         largest = wave_max_u32(largest);
-        const int exponent = largest >= 0x7f800000u ? 0 : max((int)(largest >> 23), 1) - 127;   // (infinite or NaN rows stay as they are)
+        const int exponent = max((int)(largest >> 23), 1) - 127;
         if (lane == 0) w.row_scale[slot] = ldexpf(1.0f, exponent);
         T *h = static_cast<T *>(w.h);
 #pragma unroll
@@ -142,7 +143,7 @@ __global__ void __launch_bounds__(256) k_finish_shrink(AdapterSpace w, int64_t r
             } else {
                 const T hi = (T)x;
                 h[slot * 2 * w.rank_up + r] = hi;
-                h[slot * 2 * w.rank_up + w.rank_up + r] = (T)(x - (float)hi);
+                h[slot * 2 * w.rank_up + w.rank_up + r] = isinf(x) ? (T)0.0f : (T)(x - (float)hi);
             }
         }
     }

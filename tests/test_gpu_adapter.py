@@ -158,3 +158,37 @@ def test_refusals(rt):
                      (lambda: call(rank=257), "rank"), (lambda: call(adapters=-1), "range"), (lambda: call(ldb=7), "stride")):
         assert rc() == 1 and word in lib.ocean_last_error().decode()
     assert lib.ocean_adapter_workspace(10, 32, 24, 3, 300, 2) == 0
+
+
+def _same_with_infinities(got, want, bound):
+    """NaN where the definition has one, its infinities, and finite results to the bound."""
+    g = _np(got)
+    finite = np.isfinite(want)
+    return bool(np.array_equal(np.isnan(g), np.isnan(want)) and np.array_equal(g[np.isinf(want)], want[np.isinf(want)])
+                and np.all(np.abs(g[finite] - want[finite]) <= bound[finite]))
+
+
+@pytest.mark.parametrize("M", [9, 1200])
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16", "float16"])
+def test_infinite_inner_products_and_matrices(rt, M, dtype):
+    """An infinity follows the definition, however many rows there are: adapter 0 has one infinite inner product, adapter 1 also one of some hundred
+    thousand (beyond float16) the other way, adapters 2 and 3 an infinite number of B beside inner products of either size and of no remainder."""
+    import torch
+    K, N, R, L = 64, 264, 20, 5
+    x, w, a, b, _ = _case(M, K, N, R, L, dtype, 11)
+    x = x.abs().clamp(min=0.5, max=2)
+    b[b == 0] = 1
+    ids = torch.arange(M, dtype=torch.int32) % (L + 1) - 1
+    a[0, 3] = float("inf")
+    a[1, 3], a[1, 4], b[1, :, 3], b[1, :, 4] = float("inf"), 4096, 0.5, -0.25
+    a[2] = a[2].abs() + 0.5
+    b[2, 5, 0], b[2, 200, 19], b[2, 7, 8] = float("inf"), float("-inf"), float("nan")
+    a[3] = 0
+    a[3, :, 0], x[:, 0], b[3, 9, 2] = 0.25, 0.5, float("inf")     # inner products of 1 / 8: nothing is left of them
+    with np.errstate(invalid="ignore"):
+        want, mag = O.adapter(_np(x), _np(w), _np(a), _np(b), _np(ids))
+    rows = [[m for m in range(M) if ids[m] == i] for i in range(L)]
+    assert np.isinf(want[rows[0]]).all() and (want[rows[1]] == np.inf).all() and np.isinf(want[rows[2]][:, [5, 200]]).all() and (want[rows[3]][:, 9] == np.inf).all()
+    bound = ((K + R + 4) * 2.0 ** -24 + HALVES[dtype]) * np.nan_to_num(mag, nan=0, posinf=0) + EPS[dtype] * np.abs(np.nan_to_num(want, posinf=0, neginf=0)) + TINY[dtype]
+    got = rt.adapter_matmul(x.cuda(), w.cuda(), a.cuda(), b.cuda(), ids.cuda())
+    assert _same_with_infinities(got, want, bound)
