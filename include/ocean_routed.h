@@ -116,7 +116,8 @@ int ocean_grouped_weight_grad(const ocean_groups *g, int32_t dtype, int64_t inne
  * a + id * stride_a, B_a: outer x rank at b + id * stride_b, y: rows x outer.  ranks (adapters, or NULL): adapter a uses only
  * its first ranks[a] <= rank rows of A_a and columns of B_a; the others are not used, whatever they hold.  scale: NULL means 1.
  * rank <= OCEAN_ADAPTER_MAX_RANK, adapters <= OCEAN_ADAPTER_MAX.  The inner product x * A_a^T is kept to 32 bits (types of
- * 16 bits: to 2 * 16).  workspace: ocean_adapter_workspace bytes, aligned to 256, needed until the kernels have run.
+ * 16 bits: to 2 * 16 at least; float16: or to 2^-39 of the row's largest).  workspace: ocean_adapter_workspace bytes, aligned to 256, needed until the
+ * kernels have run.
  */
 #define OCEAN_ADAPTER_MAX_RANK 256
 #define OCEAN_ADAPTER_MAX 8192

@@ -104,8 +104,9 @@ __global__ void __launch_bounds__(1024) k_order_rows(const int32_t *ids, int64_t
 
 // h = scale * the stretches' sums, one wave a slot.  The row is divided by the power of two of its largest finite magnitude (row_scale, given
 // back when its products are added), and a 16-bit type holds it as its rounding and the rounding of what is left: 16 or 22 bits
-// together, whatever the range of the type; 8 or 11 alone would be off by as much as the result's own rounding.  Of an infinity nothing is
-// left.  Columns behind the adapter's rank are 0.
+// together; 8 or 11 alone would be off by as much as the result's own rounding.  float16 ends at 2^-24, so the row's largest is put at 2^14: of a
+// number beside a much larger one 2^-39 of that may be lost, and nothing overflows.  Of an infinity nothing is left.  Columns behind the
+// adapter's rank are 0.
 template <class T>
 __global__ void __launch_bounds__(256) k_finish_shrink(AdapterSpace w, int64_t rows, int rank, const int32_t *ranks, const float *scale)
 {
@@ -130,7 +131,8 @@ __global__ void __launch_bounds__(256) k_finish_shrink(AdapterSpace w, int64_t r
             if (magnitude < 0x7f800000u) largest = max(largest, magnitude);
         }
         largest = wave_max_u32(largest);
-        const int exponent = max((int)(largest >> 23), 1) - 127;
+        constexpr int TOP = std::is_same<T, f16_t>::value ? 14 : 0;   // the exponent that the largest is given
+        const int exponent = max((int)(largest >> 23) - TOP, 1) - 127;
         if (lane == 0) w.row_scale[slot] = ldexpf(1.0f, exponent);
         T *h = static_cast<T *>(w.h);
 #pragma unroll

@@ -192,3 +192,25 @@ def test_infinite_inner_products_and_matrices(rt, M, dtype):
     bound = ((K + R + 4) * 2.0 ** -24 + HALVES[dtype]) * np.nan_to_num(mag, nan=0, posinf=0) + EPS[dtype] * np.abs(np.nan_to_num(want, posinf=0, neginf=0)) + TINY[dtype]
     got = rt.adapter_matmul(x.cuda(), w.cuda(), a.cuda(), b.cuda(), ids.cuda())
     assert _same_with_infinities(got, want, bound)
+
+
+@pytest.mark.parametrize("M", [9, 2500])
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16", "float16"])
+@pytest.mark.parametrize("ratio", [20, 26, 28])
+def test_small_inner_products_beside_large_ones(rt, M, dtype, ratio):
+    """A row's inner products are 2^13 and 2^(13 - ratio), and B takes the small one only.  Of the largest 2^-39 may be lost (float16), of each 2^-15."""
+    import torch
+    K, N, R = 64, 136, 9
+    t = getattr(torch, dtype)
+    x, w = torch.ones(M, K).to(t), torch.zeros(N, K).to(t)
+    a, b = torch.zeros(1, R, K), torch.zeros(1, N, R)
+    a[0, 2, 0], a[0, 7, 1:3], b[0, :, 7] = 2.0 ** 13, 2.0 ** (12 - ratio) * 1.25, 8.0
+    b[0, ::3, 7] = -16.0
+    a, b = a.to(t), b.to(t)
+    assert float(a[0, 7, 1]) == 2.0 ** (12 - ratio) * 1.25
+    ids = torch.zeros(M, dtype=torch.int32)
+    want, mag = O.adapter(_np(x), _np(w), _np(a), _np(b), _np(ids))
+    got = _np(rt.adapter_matmul(x.cuda(), w.cuda(), a.cuda(), b.cuda(), ids.cuda()))
+    lost = 2.0 ** -39 * 2.0 ** 13 * 16 if dtype == "float16" else 0.0
+    assert np.all(np.abs(got - want) <= ((K + R + 4) * 2.0 ** -24 + HALVES[dtype]) * mag + EPS[dtype] * np.abs(want) + TINY[dtype] + lost)
+    assert np.all(np.abs(want) > 8 * lost)
