@@ -350,7 +350,8 @@ __global__ void __launch_bounds__(256) k_route_backward(ocean_routing r, const f
         }
 #pragma unroll
         for (int i = 0; i < NV; ++i)
-            if (there && i * G + sub < experts) dlogits[t * ldd + i * G + sub] = (T)(normalize ? g[i * G + sub] : g[i * G + sub] - e[i] * scale);
+            if (there && i * G + sub < experts)   // (a masked logit's is 0 also where the scale is infinite or NaN)
+                dlogits[t * ldd + i * G + sub] = (T)(normalize || !key[i] ? g[i * G + sub] : g[i * G + sub] - e[i] * scale);
         wave_sync();
     }
 }

@@ -264,3 +264,27 @@ def test_refusals(rt):
     few.k = 7
     assert lib.ocean_combine(ctypes.byref(few), y.data_ptr(), 1, 32, 32, y.data_ptr(), 32, None) == 1
     assert lib.ocean_route_workspace(-1, 6, 2) == 0
+
+
+@pytest.mark.parametrize("normalize", [True, False])
+@pytest.mark.parametrize("E", [40, 700])
+def test_masked_logits_get_no_gradient_whatever_that_of_the_weights_is(rt, E, normalize):
+    """Gradients of weights that overflowed reach a row's open logits, not its masked ones, and no other row."""
+    import torch
+    T, k = 90, 3
+    x = _logits(T, E, torch.float32, 7, "masked").cuda()
+    lowest = torch.finfo(torch.float32).min
+    masked = x.isnan() | (x <= lowest)
+    for bad in (float("nan"), float("inf"), float("-inf")):
+        r = rt.route(x, k, normalize=normalize)
+        dval = torch.randn(T * k, generator=torch.Generator().manual_seed(3)).cuda()
+        clean = rt.route_backward(r, dval, x, normalize=normalize)
+        ptr = r.row_ptr.tolist()
+        hit = [t for t in range(T) if ptr[t + 1] > ptr[t]][::4]
+        for t in hit:
+            dval[ptr[t]] = bad
+        got = rt.route_backward(r, dval, x, normalize=normalize)
+        assert not bool(got[masked].any())
+        rest = torch.ones(T, dtype=torch.bool)
+        rest[hit] = False
+        assert torch.equal(got[rest.cuda()], clean[rest.cuda()]) and not bool(got[hit].isfinite().all(1).any())
