@@ -85,7 +85,8 @@ int ocean_combine_backward(const ocean_routing *r, const void *dout, int64_t ld_
 /*
  * Products of ragged groups of rows with their group's matrix.  Group e has rows group_ptr[e] .. group_ptr[e+1]-1 of `rows`
  * rows (group_ptr: experts + 1 ascending offsets; values outside 0 .. rows are limited to it).  With row_index, row s of the left matrix
- * is row row_index[s] of x (an index outside 0 .. x_rows-1 stands for a row of zeros); NULL: row s itself, and x_rows = rows.
+ * is row row_index[s] of x; NULL: row s itself, and x_rows = rows.  An index outside 0 .. x_rows-1 stands for a row of zeros: its product is 0 and it
+ * adds nothing to a gradient, whatever w and dy[s] hold.
  */
 typedef struct ocean_groups {
     int64_t rows, experts;

@@ -105,3 +105,29 @@ def test_adapters(rt, M, c, n, dtype, order):
     floor = 2.0 ** -25 * 512 if dtype == "float16" else 0.0
     assert bool(((y.double() - want).abs() <= ((c + R + 4) * 2.0 ** -24 + (0.0 if dtype == "float32" else 2.0 ** -15)) * mag + EPS[dtype] * want.abs() + TINY[dtype]
                  + floor)[~broken].all())
+
+
+@pytest.mark.parametrize("outer,inner", DEPTH)
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16", "float16"])
+def test_slots_whose_row_is_outside_add_nothing(rt, outer, inner, dtype):
+    """Whatever their gradient holds, as their product is 0 whatever the matrix holds."""
+    import torch
+    sizes = [130, 0, 1, 300]
+    S, ptr = sum(sizes), _ptr(sizes)
+    x, dy = _rand(1, dtype, 200, inner), _rand(2, dtype, S, outer)
+    rows = torch.randint(0, 200, (S,), device="cuda", dtype=torch.int32, generator=torch.Generator(device="cuda").manual_seed(3))
+    out = torch.arange(S, device="cuda") % 5 == 2
+    rows[out] = torch.tensor([-1, 200, 2 ** 31 - 1, -2 ** 31], device="cuda", dtype=torch.int32).repeat(S)[:int(out.sum())]
+    dy[out] = float("nan")
+    dy[::10][out[::10]] = float("inf")
+    right = torch.where(out[:, None], 0.0, x.double()[rows.clamp(0, 199).long()])
+    left = torch.where(out[:, None], 0.0, dy.double())
+    dw, dt = rt.grouped_weight_grad(dy, x, ptr, rows=rows), rt.grouped_weight_grad(dy, x, ptr, rows=rows, transposed=True)
+    for e in range(4):
+        a, b = left[ptr[e]:ptr[e + 1]], right[ptr[e]:ptr[e + 1]]
+        want, mag = a.T @ b, a.abs().T @ b.abs()
+        assert _near(dw[e], want, mag, 300, dtype) and _near(dt[e], want.T, mag.T, 300, dtype), e
+    w = _rand(4, dtype, 4, outer, inner)
+    w[:, 0, 0] = float("inf")
+    assert not bool(rt.grouped_matmul(x, w, ptr, rows=rows)[out].any())
+    assert not bool(rt.grouped_matmul(x, w.transpose(1, 2).contiguous(), ptr, rows=rows, transposed=True)[out].any())
