@@ -79,6 +79,9 @@ int ocean_combine_backward(const ocean_routing *r, const void *dout, int64_t ld_
  * Sizes: rows and widths below 2^31 - 4096, experts of a grouped product at most OCEAN_GROUPS_MAX (each workgroup finds its group by
  * going through their offsets).  Straight loads to LDS address 4 GB from a matrix's first row that a workgroup
  * needs: gathered rows of an x larger than that go through registers, which is slower and otherwise the same.
+ * A result is made in one launch, which takes less than 2^24 tiles of 128 x 128 or, in 16 bits and aligned, 2^23 of 256 x 256: of (rows / 128 + experts that
+ * may have rows) by outer / 128, a gradient of matrices of experts by outer / 128 by inner / 128, adapters of rows / 128 by outer / 128, and of (rows / 64 +
+ * adapters) by rank / 64.  What is larger is refused.
  */
 #define OCEAN_GROUPS_MAX 16384
 

@@ -196,6 +196,7 @@ constexpr int FEW_ROWS = 64;
 // only and the adapters' rows, which each row reads for itself, are not many (4096 x 1024, rank 64: 256 rows 45 us, in tiles 55).
 inline bool few_enough(int64_t rows, int64_t outer, int64_t rank)
 {
+    if (outer >= 1ll << 27) return false;   // (a launch has fewer than 2^32 threads, 512 for 16 columns)
     return rows <= 128 || (rows * rank <= 20480 && (outer + 15) / 16 * ((rows + FEW_ROWS - 1) / FEW_ROWS) <= 320);
 }
 template <class T, int TN, int WAVES, bool ALIGNED>
@@ -296,34 +297,36 @@ hipError_t launch_adapter(const ocean_adapters &l, const int32_t *ids, int dtype
                                    sp.part, sp.rank_up, none, s);
         });
     }
-    hipLaunchKernelGGL(k_order_rows, dim3(1), dim3(1024), 0, s, ids, rows, (int)adapters, sp);
-    hipError_t err = hipGetLastError();
-    if (err != hipSuccess) return err;
     return with_type(dtype, [&](auto t) {
         using T = decltype(t);
-        GmmArgs a{};
-        a.l = x, a.ldl = ldx, a.rows = rows, a.c = inner;
-        a.index = sp.perm, a.index_rows = rows;
+        GmmArgs shrink{};
+        shrink.l = x, shrink.ldl = ldx, shrink.rows = rows, shrink.c = inner;
+        shrink.index = sp.perm, shrink.index_rows = rows;
+        GmmArgs a = shrink;
+        shrink.r = l.a, shrink.ldr = l.ld_a, shrink.stride = l.stride_a;
+        shrink.out = sp.part, shrink.ldo = sp.rank_up;
+        shrink.ptr = sp.ptr, shrink.groups = adapters;
+        shrink.n = rank, shrink.c_part = sp.c_part;
+        a.r = w, a.ldr = ldw;
+        a.out = y, a.ldo = ldy, a.n = outer;
+        a.slot_id = sp.slot_id, a.adapters = adapters;
+        a.h = sp.h, a.row_scale = sp.row_scale, a.b = l.b, a.ldb = l.ld_b, a.stride_b = l.stride_b, a.ranks = l.ranks, a.rank = rank, a.rank_up = sp.rank_up;
+        const bool aligned = pieces_aligned(x, ldx, 0, size) && pieces_aligned(w, ldw, 0, size) && inner % e == 0 && x_fits && offsets_fit(256, ldw, size);
+        if (!some_tile_launches<T, GM_EXPAND>(a, aligned) || (!none && !launches<GM_SHRINK>(shrink, 64, 64, 256))) return TOO_MANY_TILES;
+        hipLaunchKernelGGL(k_order_rows, dim3(1), dim3(1024), 0, s, ids, rows, (int)adapters, sp);
+        hipError_t r = hipGetLastError();
+        if (r != hipSuccess) return r;
         if (!none) {
-            a.r = l.a, a.ldr = l.ld_a, a.stride = l.stride_a;
-            a.out = sp.part, a.ldo = sp.rank_up;
-            a.ptr = sp.ptr, a.groups = adapters;
-            a.n = rank, a.c_part = sp.c_part;
-            const bool aligned = pieces_aligned(x, ldx, 0, size) && pieces_aligned(l.a, l.ld_a, l.stride_a, size) && inner % e == 0 && x_fits &&
-                                 offsets_fit(256, l.ld_a, size);
-            hipError_t r = aligned ? launch_gmm<T, false, false, 64, 64, 4, 1, true, 2, GM_SHRINK, float>(a, s)
-                                   : launch_gmm<T, false, false, 64, 64, 4, 1, false, 2, GM_SHRINK, float>(a, s);
+            const bool whole = pieces_aligned(x, ldx, 0, size) && pieces_aligned(l.a, l.ld_a, l.stride_a, size) && inner % e == 0 && x_fits &&
+                               offsets_fit(256, l.ld_a, size);
+            r = whole ? launch_gmm<T, false, false, 64, 64, 4, 1, true, 2, GM_SHRINK, float>(shrink, s)
+                      : launch_gmm<T, false, false, 64, 64, 4, 1, false, 2, GM_SHRINK, float>(shrink, s);
             if (r != hipSuccess) return r;
             hipLaunchKernelGGL((k_finish_shrink<T>), dim3((uint32_t)std::min((rows + 3) / 4, (int64_t)1 << 20)), dim3(256), 0, s, sp, rows, rank,
                                l.ranks, l.scale);
             r = hipGetLastError();
             if (r != hipSuccess) return r;
         }
-        a.r = w, a.ldr = ldw, a.stride = 0;
-        a.out = y, a.ldo = ldy, a.n = outer;
-        a.slot_id = sp.slot_id, a.adapters = adapters;
-        a.h = sp.h, a.row_scale = sp.row_scale, a.b = l.b, a.ldb = l.ld_b, a.stride_b = l.stride_b, a.ranks = l.ranks, a.rank = rank, a.rank_up = sp.rank_up;
-        const bool aligned = pieces_aligned(x, ldx, 0, size) && pieces_aligned(w, ldw, 0, size) && inner % e == 0 && x_fits && offsets_fit(256, ldw, size);
         return launch_tiles<T, false, false, GM_EXPAND>(a, [&](int64_t bm) { return (rows + bm - 1) / bm; }, aligned, s);
     });
 }

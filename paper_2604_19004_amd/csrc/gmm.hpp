@@ -829,16 +829,33 @@ __global__ void __launch_bounds__(WAVES_M * WAVES_N * WAVE, 2) k_gmm(GmmArgs a, 
 
 inline int64_t up8(int64_t n) { return (n + 7) & ~(int64_t)7; }
 
+// Tiles of bm x bn, down and across, and the workgroups that they take.  (Ragged groups: a group's last tile may hold a single row, and the
+// others of `rows` are whole.)
+struct Grid { int64_t mt, nt, blocks; };
+template <GmmMode MODE> Grid grid_of(const GmmArgs &a, int64_t bm, int64_t bn)
+{
+    Grid g;
+    g.nt = (a.n + bn - 1) / bn;
+    g.mt = MODE == GM_DEPTH ? (a.m + bm - 1) / bm : MODE == GM_EXPAND ? (a.rows + bm - 1) / bm : a.rows / bm + std::min(a.groups, a.rows);
+    // (GM_ROWS: the last 8 at least have no tile and clear the rows of no group)
+    g.blocks = (MODE == GM_ROWS ? 8 : 0) + (MODE == GM_DEPTH ? up8(g.mt * g.nt) * a.groups : up8(g.mt * g.nt * (MODE == GM_SHRINK ? (a.c + a.c_part - 1) / a.c_part : 1)));
+    return g;
+}
+// Whether one launch has them: it has fewer than 2^32 threads.
+template <GmmMode MODE> bool launches(const GmmArgs &a, int64_t bm, int64_t bn, int threads) { return grid_of<MODE>(a, bm, bn).blocks * threads < (1ll << 32); }
+// Whether any tile does that launch_tiles may take.  (Where a smaller one does, one of these does.)
+template <class T, GmmMode MODE> bool some_tile_launches(const GmmArgs &a, bool aligned)
+{
+    return launches<MODE>(a, 128, 128, 256) || (sizeof(T) == 2 && aligned && launches<MODE>(a, 256, 256, 512));
+}
+
 template <class T, bool LCOL, bool RCOL, int BM, int BN, int WAVES_M, int WAVES_N, bool ASYNC, int STAGES, GmmMode MODE, class O = T>
 hipError_t launch_gmm(const GmmArgs &a, hipStream_t s)
 {
-    const int64_t nt = (a.n + BN - 1) / BN;
-    const int64_t mt = MODE == GM_DEPTH ? (a.m + BM - 1) / BM : MODE == GM_EXPAND ? (a.rows + BM - 1) / BM : a.rows / BM + std::min(a.groups, a.rows) + 1;
-    // (GM_ROWS: the last 8 at least have no tile and clear the rows of no group)
-    const int64_t blocks = (MODE == GM_ROWS ? 8 : 0) + (MODE == GM_DEPTH ? up8(mt * nt) * a.groups : up8(mt * nt * (MODE == GM_SHRINK ? (a.c + a.c_part - 1) / a.c_part : 1)));
+    const Grid g = grid_of<MODE>(a, BM, BN);
     constexpr int threads = WAVES_M * WAVES_N * WAVE;
-    if (blocks * threads >= (1ll << 32)) return hipErrorInvalidConfiguration;
-    hipLaunchKernelGGL((k_gmm<T, LCOL, RCOL, BM, BN, WAVES_M, WAVES_N, ASYNC, STAGES, MODE, O>), dim3((uint32_t)blocks), dim3(threads), 0, s, a, (int)mt, (int)nt);
+    if (g.blocks * threads >= (1ll << 32)) return TOO_MANY_TILES;
+    hipLaunchKernelGGL((k_gmm<T, LCOL, RCOL, BM, BN, WAVES_M, WAVES_N, ASYNC, STAGES, MODE, O>), dim3((uint32_t)g.blocks), dim3(threads), 0, s, a, (int)g.mt, (int)g.nt);
     return hipGetLastError();
 }
 
@@ -866,11 +883,13 @@ template <class T, bool LCOL, bool RCOL, GmmMode MODE, class F> hipError_t launc
     // (gradients of weights in a single round wait for the deepest group: 8 uneven groups, 32768 rows, 2048 x 1024, in 256 tiles of 256 x 256 264
     // us, in 1024 of 128 x 128 170; with even ones some 130 and 165)
     const double alone = MODE == GM_DEPTH && a.groups > 1 && tiles(256, 256) <= 256 ? 1.6 : 1.0;
-    const double large = large_rounds(tiles(256, 256)) * alone,
-                 middle = WIDE ? (double)(int64_t)((tiles(128, 256) + 255) / 256) * 1.16 : rounds(tiles(128, 128), 0.89, 1.13),
-                 low = rounds(tiles(64, 128), 0.55, 0.69), small = rounds(tiles(64, 64), 0.44, 0.50);
+    // (more tiles than a launch has: never)
+    auto unless = [&](int64_t bm, int64_t bn, int threads, double time) { return launches<MODE>(a, bm, bn, threads) ? time : 1e300; };
+    const double large = unless(256, 256, 512, large_rounds(tiles(256, 256)) * alone),
+                 middle = WIDE ? unless(128, 256, 512, (double)(int64_t)((tiles(128, 256) + 255) / 256) * 1.16) : unless(128, 128, 256, rounds(tiles(128, 128), 0.89, 1.13)),
+                 low = unless(64, 128, 256, rounds(tiles(64, 128), 0.55, 0.69)), small = unless(64, 64, 256, rounds(tiles(64, 64), 0.44, 0.50));
     if (!aligned) {   // (through registers: 8356 rows of 4517 by four 832 x 4517, 462 tiles of 128 x 128, 121 us and 169 in those of 64 x 64)
-        if (tiles(128, 128) >= 256) return launch_gmm<T, LCOL, RCOL, 128, 128, 2, 2, false, 2, MODE>(a, s);
+        if (tiles(128, 128) >= 256 || small == 1e300) return launch_gmm<T, LCOL, RCOL, 128, 128, 2, 2, false, 2, MODE>(a, s);
         return launch_gmm<T, LCOL, RCOL, 64, 64, 4, 1, false, 2, MODE>(a, s);
     }
     if constexpr (sizeof(T) == 2) {

@@ -20,6 +20,9 @@ template <> struct TypeTraits<float> { static constexpr int code = OCEAN_F32; st
 template <> struct TypeTraits<bf16_t> { static constexpr int code = OCEAN_BF16; static constexpr float lowest = -3.3895313892515355e38f; };
 template <> struct TypeTraits<f16_t> { static constexpr int code = OCEAN_F16; static constexpr float lowest = -65504.0f; };
 
+// What a launch function returns, and nothing has been launched then, where a result has more tiles than one launch takes.
+constexpr hipError_t TOO_MANY_TILES = hipErrorInvalidConfiguration;
+
 inline int type_size(int dtype) { return dtype == OCEAN_F32 ? 4 : 2; }
 
 #if defined(__HIPCC__)

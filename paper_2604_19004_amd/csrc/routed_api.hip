@@ -12,6 +12,7 @@ int bad(const char *msg) { return set_error(OCEAN_EINVAL, msg); }
 int launched(hipError_t e, const char *what)
 {
     if (e == hipSuccess) return OCEAN_OK;
+    if (e == TOO_MANY_TILES) return bad("the result has more tiles than one launch takes (see the sizes in ocean_routed.h)");
     char msg[256];
     std::snprintf(msg, sizeof msg, "%s: %s", what, hipGetErrorString(e));
     return set_error(OCEAN_EHIP, msg);

@@ -105,3 +105,51 @@ def test_combine(rt, x):
     assert bool(((dy[slot.view(-1)].view(-1, k, WIDE).double() - wdy).abs() <= (2.0 ** -23 + 2.0 ** -8) * wdy.abs() + 2.0 ** -133).all())
     wdval, dmag = (d[:, None, :] * rows).sum(2), (d[:, None, :] * rows).abs().sum(2)
     assert bool(((dval.view(T, k)[at].double() - wdval).abs() <= (WIDE / 32 + 40) * 2.0 ** -24 * dmag).all())
+
+
+@pytest.mark.parametrize("dtype,inner,more", [("bfloat16", 8, 64), ("bfloat16", 1, 64), ("float32", 1, 3)])
+def test_a_row_of_many_columns(rt, dtype, inner, more):
+    """More columns than a launch has tiles of 64 x 64 for, whatever the alignment: larger ones are taken."""
+    import torch
+    t, N = getattr(torch, dtype), (1 << 30) + more
+    x = torch.randn(1, inner, device="cuda", generator=torch.Generator(device="cuda").manual_seed(11)).to(t)
+    w = torch.empty(1, N, inner, device="cuda", dtype=t)
+    for at in range(0, N, 1 << 27):
+        w[0, at:at + (1 << 27)].normal_(generator=torch.Generator(device="cuda").manual_seed(at >> 27))
+    y = rt.grouped_matmul(x, w, torch.tensor([0, 1], device="cuda"))
+    eps = 2.0 ** -8 if dtype == "bfloat16" else 2.0 ** -24
+    for at in range(0, N, 1 << 27):
+        a = w[0, at:at + (1 << 27)].double()
+        want, mag = (a * x.double()).sum(1), (a * x.double()).abs().sum(1)
+        assert bool(((y[0, at:at + (1 << 27)].double() - want).abs() <= (inner + 2) * 2.0 ** -24 * mag + eps * want.abs() + 2.0 ** -133).all()), at
+
+
+def test_many_rows_of_few_columns(rt):
+    import torch
+    S, K, N = (1 << 30) + 100, 8, 8
+    x = torch.empty(S, K, device="cuda", dtype=torch.bfloat16)
+    for at in range(0, S, 1 << 27):
+        x[at:at + (1 << 27)].normal_(generator=torch.Generator(device="cuda").manual_seed(at >> 27))
+    w = _rand(12, 2, N, K)
+    ptr = torch.tensor([5, (1 << 29) + 77, S - 3], device="cuda")
+    y = rt.grouped_matmul(x, w, ptr)
+    assert not bool(y[:5].any()) and not bool(y[S - 3:].any())
+    for lo, hi, e in ((5, 1 << 20, 0), ((1 << 29) - 1000, (1 << 29) + 77, 0), ((1 << 29) + 77, (1 << 29) + 5000, 1), (S - (1 << 20), S - 3, 1)):
+        assert _same(y[lo:hi], x[lo:hi], w[e])
+
+
+def test_adapters_of_many_columns(rt):
+    import torch
+    M, K, N = 3, 8, (1 << 27) + 24
+    x, w, a, b = _rand(13, M, K), _rand(14, N, K), _rand(15, 2, 1, K), _rand(16, 2, N, 1)
+    y = rt.adapter_matmul(x, w, a, b, torch.tensor([1, -1, 0], device="cuda", dtype=torch.int32))
+    for m, i in ((0, 1), (1, -1), (2, 0)):
+        for at in range(0, N, 1 << 25):   # (products and sums: a library's product of a matrix of more than 2^27 rows with a vector is not relied on)
+            to = slice(at, at + (1 << 25))
+            terms = w[to].double() * x[m].double()
+            want, mag = terms.sum(1), terms.abs().sum(1)
+            if i >= 0:
+                h = a[i, 0].double() * x[m].double()
+                want += b[i, to, 0].double() * h.sum()
+                mag += b[i, to, 0].double().abs() * h.abs().sum()
+            assert bool(((y[m, to].double() - want).abs() <= ((K + 8) * 2.0 ** -24 + 2.0 ** -15) * mag + 2.0 ** -8 * want.abs() + 2.0 ** -133).all()), (m, at)

@@ -96,3 +96,19 @@ def test_refusals_of_sizes(rt):
                      (lambda: lib.ocean_grouped_weight_grad(b(two), 1, 4, 4, 0x1000, 4, 0x1000, 4, 0x1000, 4, 15, 0, None), "overlap"),
                      (lambda: lib.ocean_grouped_weight_grad(b(two), 1, 4, 4, 0x1000, 4, 0x1000, 4, 0x1000, 1 << 39, 16, 0, None), "overlap")):
         assert rc() == 1 and word in lib.ocean_last_error().decode(), word
+
+
+def test_results_of_more_tiles_than_a_launch_takes_are_refused(rt):
+    """Before anything is launched (the pointers name nothing)."""
+    lib = rt.load()
+    b = ctypes.byref
+    n = 1 << 23
+    groups, one = rt.ocean_groups(n, 3, 0x1000, None, n), rt.ocean_groups(100, 1, 0x1000, None, 100)
+    lora = rt.ocean_adapters(2, 8, 0x1000, 8, 64, 0x1000, 8, n * 8, None, None)
+    for dtype in (1, 2, 3):
+        for inner in (8, 7):
+            for rc in (lambda: lib.ocean_grouped_matmul(b(groups), dtype, inner, n, 0x1000, 8, 0x1000, 8, 8 * n, 0, 0x1000, n, None),
+                       lambda: lib.ocean_grouped_matmul(b(groups), dtype, inner, n, 0x1000, 8, 0x1000, n, 8 * n, 1, 0x1000, n, None),
+                       lambda: lib.ocean_grouped_weight_grad(b(one), dtype, n - 8 + inner, n, 0x1000, n, 0x1000, n, 0x1000, n, 0, 0, None),
+                       lambda: lib.ocean_adapter_matmul(b(lora), 0x1000, dtype, n, inner, n, 0x1000, 8, 0x1000, 8, 0x1000, n, 0x1000, 1 << 60, None)):
+                assert rc() == 1 and "tiles" in lib.ocean_last_error().decode(), (dtype, inner, lib.ocean_last_error())
