@@ -116,9 +116,10 @@ class Routing:
         return r
 
     def csr(self) -> DeviceCSR:
-        """The matrix as an operand of binding.spgemm; reads the number of its entries back."""
+        """The matrix as an operand of binding.spgemm (without val every weight is 1); reads the number of its entries back."""
         n = int(self.row_ptr[-1])
-        return DeviceCSR(self.tokens, self.experts, self.row_ptr, self.col_idx[:n], self.val[:n], [self])
+        val = self.val[:n] if self.val is not None else self.row_ptr.new_ones(n, dtype=_b._torch().float32)
+        return DeviceCSR(self.tokens, self.experts, self.row_ptr, self.col_idx[:n], val, [self])
 
     def _struct(self, weighted=True):
         return self._structs[bool(weighted)]

@@ -112,3 +112,19 @@ def test_results_of_more_tiles_than_a_launch_takes_are_refused(rt):
                        lambda: lib.ocean_grouped_weight_grad(b(one), dtype, n - 8 + inner, n, 0x1000, n, 0x1000, n, 0x1000, n, 0, 0, None),
                        lambda: lib.ocean_adapter_matmul(b(lora), 0x1000, dtype, n, inner, n, 0x1000, 8, 0x1000, 8, 0x1000, n, 0x1000, 1 << 60, None)):
                 assert rc() == 1 and "tiles" in lib.ocean_last_error().decode(), (dtype, inner, lib.ocean_last_error())
+
+
+def _small_routing(rt, weights=True):
+    import torch
+    i32 = torch.int32
+    return rt.Routing(3, 4, 2, torch.tensor([0, 2, 2, 3]), torch.tensor([0, 3, 1, -1, -1, -1], dtype=i32),
+                      torch.tensor([0.25, 0.75, 1, 0, 0, 0]) if weights else None, torch.tensor([0, 1, 2, 2, 3]),
+                      torch.tensor([0, 2, 0, -1, -1, -1], dtype=i32), torch.tensor([0, 2, 1, -1, -1, -1], dtype=i32))
+
+
+def test_a_routing_as_an_operand_of_the_sparse_product(rt):
+    """Without weights every one is 1."""
+    for weights, val in ((True, [0.25, 0.75, 1]), (False, [1, 1, 1])):
+        R = _small_routing(rt, weights).csr()
+        assert (R.rows, R.cols, R.nnz) == (3, 4, 3) and R.col_idx.tolist() == [0, 3, 1] and R.row_ptr.tolist() == [0, 2, 2, 3]
+        assert R.val.tolist() == val and str(R.val.dtype) == "torch.float32"
