@@ -115,6 +115,10 @@ class Routing:
         r._hold(r.row_ptr.device, True)
         return r
 
+    def __reduce__(self):
+        """Copies and pickles are made of the fields: the structs hold pointers to this one's lists."""
+        return Routing, tuple(getattr(self, name) for name in self.__dataclass_fields__)
+
     def csr(self) -> DeviceCSR:
         """The matrix as an operand of binding.spgemm (without val every weight is 1); reads the number of its entries back."""
         n = int(self.row_ptr[-1])

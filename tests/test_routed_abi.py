@@ -128,3 +128,19 @@ def test_a_routing_as_an_operand_of_the_sparse_product(rt):
         R = _small_routing(rt, weights).csr()
         assert (R.rows, R.cols, R.nnz) == (3, 4, 3) and R.col_idx.tolist() == [0, 3, 1] and R.row_ptr.tolist() == [0, 2, 2, 3]
         assert R.val.tolist() == val and str(R.val.dtype) == "torch.float32"
+
+
+def test_copies_of_a_routing_hold_their_own_lists(rt):
+    import copy
+    import dataclasses
+    import pickle
+    for weights in (True, False):
+        r = _small_routing(rt, weights)
+        for c in (copy.deepcopy(r), pickle.loads(pickle.dumps(r)), dataclasses.replace(r, slot=r.slot.clone()), copy.copy(r)):
+            assert (c.tokens, c.experts, c.k) == (3, 4, 2)
+            for weighted in (False, weights):
+                s = c._struct(weighted)
+                for name in ("row_ptr", "col_idx", "expert_ptr", "token", "slot"):
+                    assert getattr(c, name).tolist() == getattr(r, name).tolist() and getattr(s, name) == getattr(c, name).data_ptr(), name
+                assert s.val == (c.val.data_ptr() if weighted else None)
+        assert copy.deepcopy(r).slot.data_ptr() != r.slot.data_ptr()
