@@ -121,8 +121,9 @@ class Routing:
 
     def csr(self) -> DeviceCSR:
         """The matrix as an operand of binding.spgemm (without val every weight is 1); reads the number of its entries back."""
+        import torch
         n = int(self.row_ptr[-1])
-        val = self.val[:n] if self.val is not None else self.row_ptr.new_ones(n, dtype=_b._torch().float32)
+        val = self.val[:n] if self.val is not None else torch.ones(n, dtype=torch.float32, device=self._device)
         return DeviceCSR(self.tokens, self.experts, self.row_ptr, self.col_idx[:n], val, [self])
 
     def _struct(self, weighted=True):
