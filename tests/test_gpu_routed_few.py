@@ -83,3 +83,33 @@ def test_strides_and_alignment_against_the_definition(rt, sizes, K, N, dtype):
             xe, we, de = x[lo:hi].double(), w[e].double(), dy[lo:hi].double()
             for name, got, a, b in (("y", y[lo:hi], xe, we.T), ("dx", dx[lo:hi], de, we), ("dw", dw[e], de.T, xe), ("dt", dt[e], xe.T, de)):
                 assert _near(got, a @ b, a.abs() @ b.abs(), a.shape[1], dtype), (name, e, off, extra)
+
+
+@pytest.mark.parametrize("transposed", [False, True])
+@pytest.mark.parametrize("E,n,c,rows", [(128, 64, 2048, 24), (8, 1024, 4096, 24)])
+def test_rows_that_all_meet_in_one_group(rt, E, n, c, rows, transposed):
+    """As the routing of a step may have it: right, and no more than four times as long as with the same number in each."""
+    import torch
+    S = E * rows
+    x, w = _rand(1, "bfloat16", S, c), _rand(2, "bfloat16", E, *((c, n) if transposed else (n, c)))
+    even, one = torch.arange(E + 1, device="cuda") * rows, torch.zeros(E + 1, device="cuda", dtype=torch.int64)
+    one[E // 2 + 1:] = S
+    y = rt.grouped_matmul(x, w, one, transposed=transposed)
+    a, b = x.double(), w[E // 2].double()
+    b = b if transposed else b.T
+    assert _near(y, a @ b, a.abs() @ b.abs(), c, "bfloat16")
+
+    def least(ptr):
+        times = []
+        for _ in range(12):
+            s, e = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+            s.record()
+            for _ in range(10):
+                rt.grouped_matmul(x, w, ptr, transposed=transposed)
+            e.record()
+            torch.cuda.synchronize()
+            times.append(s.elapsed_time(e))
+        return min(times)
+
+    least(even)
+    assert least(one) <= 4 * least(even)
