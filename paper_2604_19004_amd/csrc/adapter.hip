@@ -192,12 +192,20 @@ __global__ void __launch_bounds__(256) k_shrink_few(ocean_adapters l, const int3
 // The shared projection of 16, 32, 48 or 64 rows (blockIdx.y-th 64) and TN * 16 columns, each result begun with the adapter's part.  Up to 16 rows it
 // is bound by W's bytes (4096 x 4096 in bfloat16: 9 us), with more by the rows, which every workgroup reads from the L2 (48: 19 us, 17 without adapters).
 constexpr int FEW_ROWS = 64;
-// Few rows: up to 128 (64 adapters of rank 16, 4096 x 4096: 37 us, in tiles 64; 192 rows 61 and 61), more while there are workgroups for one round
-// only and the adapters' rows, which each row reads for itself, are not many (4096 x 1024, rank 64: 256 rows 45 us, in tiles 55).
-inline bool few_enough(int64_t rows, int64_t outer, int64_t rank)
+// Few rows: up to 128, and more while one round holds the workgroups, two on a compute unit, and the adapters' rows, which each row reads for itself, are
+// not many.  In bfloat16, rows of 24 adapters, without tiles and in them, us:
+//   up to 128 rows, 4096 x 4096: 128 of rank 16 38 and 52, 64 57 and 75, 256 132 and 191 (192 rows, 64 adapters of rank 16: 61 and 61).  Who shares an adapter is
+//   not known here: all rows with the same one take 36 and 44, 54 and 46, 130 and 68, each with its own 39 and 90, 72 and 199, 217 and 776;
+//   2048 -> 2048, 128 rows of rank 64 29 and 58; wider results are less apart (4096 -> 8192, 128 of rank 16 60 and 53).
+//   512 workgroups: 256 x 2048 -> 2048 28 and 33 (rank 16), 43 and 45 (64); 513: 192 x 2000 -> 2736 35 and 33, 57 and 49.
+//   Lines of 10 KB: 256 x 5000 -> 2048 49 and 55, 65 and 66; 6144 -> 2048 68 and 64, 83 and 75, but 256 workgroups, 192 x 6144 -> 1360, 42 and 64, 54 and 80.
+//   In single precision tiles are slower at any length: 256 x 8192 -> 2048 167 and 240, 192 and 253.
+//   Rows * rank: 512 x 2000 -> 512 of rank 64 34 and 37, 640 columns 43 and 38 (256 x 1280 of rank 64, 16384: 38 and 43).
+inline bool few_enough(int64_t rows, int64_t inner, int64_t outer, int64_t rank, int size)
 {
     if (outer >= 1ll << 27) return false;   // (a launch has fewer than 2^32 threads, 512 for 16 columns)
-    return rows <= 128 || (rows * rank <= 20480 && (outer + 15) / 16 * ((rows + FEW_ROWS - 1) / FEW_ROWS) <= 320);
+    const int64_t workgroups = (outer + 15) / 16 * ((rows + FEW_ROWS - 1) / FEW_ROWS);
+    return rows <= 128 || (rows * rank <= 20480 && workgroups <= (size == 4 || inner * size <= 10240 ? 512 : 256));
 }
 template <class T, int TN, int WAVES, bool ALIGNED>
 __global__ void __launch_bounds__(WAVES * WAVE, 2) k_adapter_few(ocean_adapters l, const int32_t *ids, const T *x, int64_t ldx, int64_t inner, int64_t rows,
@@ -290,7 +298,7 @@ hipError_t launch_adapter(const ocean_adapters &l, const int32_t *ids, int dtype
     const int64_t adapters = none ? 0 : l.adapters;
     const bool x_fits = offsets_fit(std::max<int64_t>(rows, 256), ldx, size);
     const AdapterSpace sp = adapter_space(workspace, rows, inner, l.adapters, l.rank, dtype);
-    if (few_enough(rows, outer, l.rank)) {
+    if (few_enough(rows, inner, outer, l.rank, size)) {
         return with_type(dtype, [&](auto t) {
             using T = decltype(t);
             return launch_few_rows(l, ids, rows, inner, outer, static_cast<const T *>(x), ldx, static_cast<const T *>(w), ldw, static_cast<T *>(y), ldy,
