@@ -183,8 +183,8 @@ __device__ __forceinline__ void load_to_lds(const void *src, char *lds)
 {
     __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)src, (__attribute__((address_space(3))) void *)lds, 16, 0, 0);
 }
-// A piece from any address of the element type.
-template <class T> __device__ __forceinline__ uint4 load_any(const char *p)
+// A piece from any even address.
+__device__ __forceinline__ uint4 load_any(const char *p)
 {
     typedef uint32_t any_u32x4 __attribute__((ext_vector_type(4), aligned(2)));
     return __builtin_bit_cast(uint4, (u32x4)*reinterpret_cast<const any_u32x4 *>(p));
@@ -192,7 +192,7 @@ template <class T> __device__ __forceinline__ uint4 load_any(const char *p)
 // Up to a piece from any address of the element type; what lies behind `valid` elements is not read and 0.
 template <class T> __device__ __forceinline__ uint4 load_piece(const T *p, int valid)
 {
-    if (valid >= PIECE<T>) return load_any<T>(reinterpret_cast<const char *>(p));
+    if (valid >= PIECE<T>) return load_any(reinterpret_cast<const char *>(p));
     Vec<T, PIECE<T>> e = {};
 #pragma unroll
     for (int i = 0; i < PIECE<T>; ++i)
@@ -564,7 +564,7 @@ __global__ void __launch_bounds__(WAVES_M * WAVES_N * WAVE, 2) k_gmm(GmmArgs a, 
                 if (!(DEPTH && by_number) && feed.whole(left)) {   // (the same for all: no lane looks at its pieces' ends)
                     const char *base = feed.step(t);
 #pragma unroll
-                    for (int i = 0; i < TI::LOADS; ++i) dst[i] = load_any<T>(base + feed.off[i]);
+                    for (int i = 0; i < TI::LOADS; ++i) dst[i] = load_any(base + feed.off[i]);
                     return;
                 }
 #pragma unroll
