@@ -108,7 +108,8 @@ int ocean_grouped_matmul(const ocean_groups *g, int32_t dtype, int64_t inner, in
 
 /*
  * dW_e = sum over the rows s of group e of dy[s]^T x[row(s)] (outer x inner; transposed != 0: its transpose, inner x outer);
- * an empty group's is 0.  dy: rows x outer.  dW_e is written at dw + e * stride_dw elements.
+ * an empty group's is 0.  dy: rows x outer.  dW_e is written at dw + e * stride_dw elements; each begins behind the one before it (interleaved ones are
+ * refused).
  */
 int ocean_grouped_weight_grad(const ocean_groups *g, int32_t dtype, int64_t inner, int64_t outer, const void *dy, int64_t ld_dy,
                               const void *x, int64_t ld_x, void *dw, int64_t ld_dw, int64_t stride_dw, int32_t transposed,

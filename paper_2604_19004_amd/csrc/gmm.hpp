@@ -439,7 +439,7 @@ __global__ void __launch_bounds__(WAVES_M * WAVES_N * WAVE, 2) k_gmm(GmmArgs a, 
     __shared__ int s_wave[8], s_adapters;
     Work w;
     if (!locate(blockIdx.x >> 3, w)) {
-        if constexpr (MODE == GM_ROWS) {   // (some have no tile: see launch_gmm)
+        if constexpr (MODE == GM_ROWS) {   // (some have no tile: see grid_of)
             const int from = (tiles * nt + 7) / 8 * 8, part = (int)blockIdx.x - from;
             if (part >= 0) clear_outside<O>(a, 0, a.n, part, (int)gridDim.x - from);
         }

@@ -4,6 +4,8 @@ A routing matrix (tokens x experts, k entries a row) is made from logits, applie
 differentiated; the ragged groups of rows that it forms are multiplied with their experts' weights; and rows that each name a
 low-rank adapter are projected with it.  Every step runs in the HIP library, on the current stream or the one given; outputs and
 workspaces are torch tensors of that stream, nothing synchronises, and calls can be captured into a graph.  An `out` may not overlap what is read.  There is no CPU fallback.
+The calls are no part of torch's autograd: results carry no gradient function, also of inputs that require gradients, and a training step calls the gradients
+itself, as below (or from a torch.autograd.Function of its own).
 
 A training step of an experts' block, for x [T, D], w1 [E, F, D], w2 [E, D, F]:
 
@@ -230,7 +232,7 @@ def route(logits, k: int, *, normalize: bool = True, stream=None) -> Routing:
 
 
 def route_backward(routing: Routing, dval, logits, *, normalize: bool = True, out=None, stream=None):
-    """Gradient of the logits from dval [tokens*k], that of the weights in the order of routing.val."""
+    """Gradient of the logits from dval [tokens*k], that of the weights in the order of routing.val; normalize as in route.  Masked logits get 0."""
     import torch
     lib = load()
     ld = _matrix(logits, "logits", routing.tokens, routing.experts)
@@ -324,7 +326,7 @@ def grouped_matmul(x, w, expert_ptr, *, rows=None, transposed: bool = False, out
 
 def grouped_weight_grad(dy, x, expert_ptr, *, rows=None, transposed: bool = False, out=None, stream=None):
     """Gradient of grouped_matmul's w: the sum over the slots s of expert e of dy[s]^T x[rows[s]], [experts, outer, inner] (transposed:
-    [experts, inner, outer]); zeros for an expert without slots."""
+    [experts, inner, outer]); zeros for an expert without slots.  Slots whose row number is outside x add nothing, whatever dy holds there."""
     lib = load()
     ldx = _matrix(x, "x")
     code = _code(x.dtype)
