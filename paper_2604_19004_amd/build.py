@@ -10,7 +10,8 @@ CSRC = os.path.join(HERE, "csrc")
 INCLUDE = os.path.join(os.path.dirname(HERE), "include")
 LIB = os.path.join(HERE, "libocean_spgemm.so")
 SOURCES = ["analysis.hip", "binning.hip", "symbolic.hip", "numeric.hip", "esc.hip", "sortrow.hip", "placed.hip", "compact.hip", "order.hip", "ocean_api.hip",
-           "route.hip", "combine.hip", "grouped.hip", "adapter.hip", "routed_api.hip"]
+           "route.hip", "combine.hip", "grouped.hip", "adapter.hip", "routed_api.hip",
+           "balance.hip", "mx4.hip", "mx4_grouped.hip", "mx4_both.hip", "experts_api.hip"]
 
 HIPCC_FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-munsafe-fp-atomics",

@@ -906,9 +906,9 @@ template <class T, bool LCOL, bool RCOL, GmmMode MODE, class F> hipError_t launc
 }
 
 // Whether the places of an operand's pieces fit the 32-bit offsets of Feed: `lines` lines of `ld` elements from its base.
-bool offsets_fit(int64_t lines, int64_t ld, int size) { return lines * ld * size < (1ll << 32) - 65536; }
+inline bool offsets_fit(int64_t lines, int64_t ld, int size) { return lines * ld * size < (1ll << 32) - 65536; }
 
-bool pieces_aligned(const void *p, int64_t ld, int64_t stride, int size)
+inline bool pieces_aligned(const void *p, int64_t ld, int64_t stride, int size)
 {
     const int e = 16 / size;
     return reinterpret_cast<uintptr_t>(p) % 16 == 0 && ld % e == 0 && stride % e == 0;

@@ -1,0 +1,345 @@
+// Products of ragged groups of rows with their group's matrix in four bits, rows in their own type.
+//
+// Every number of four bits is a bfloat16 number, every float16 number the sum of two and every single precision number of three: so all products are
+// made by the bfloat16 matrix instructions, x in 1, 2 or 3 parts (exactly: single precision at a third of their rate is three times that of its own).
+#include "mx4_tiles.hpp"
+
+namespace ocean {
+
+namespace {
+
+template <class T> constexpr int PARTS_OF = std::is_same<T, bf16_t>::value ? 1 : std::is_same<T, f16_t>::value ? 2 : 3;
+
+// 8 numbers as sums of bfloat16 numbers: each part takes the 8 leading bits of what is left, the last one the rest.  An infinite number or NaN is its first part.
+template <class T> __device__ __forceinline__ void split(const T (&x)[8], bf16x8 (&out)[PARTS_OF<T>])
+{
+    constexpr int PARTS = PARTS_OF<T>;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+        if constexpr (PARTS == 1) {
+            out[0][k] = x[k];
+        } else {
+            float left = (float)x[k];
+            const bool finite = (__float_as_uint(left) & 0x7f800000u) != 0x7f800000u;
+            const uint32_t quiet = left != left ? 0x00400000u : 0u;
+#pragma unroll
+            for (int p = 0; p < PARTS; ++p) {
+                const uint32_t bits = (__float_as_uint(left) | (p == 0 ? quiet : 0u)) & 0xffff0000u;
+                out[p][k] = __builtin_bit_cast(bf16_t, (uint16_t)(bits >> 16));
+                left = finite ? left - __uint_as_float(bits) : 0.0f;
+            }
+        }
+    }
+}
+
+// A tile: x straight to LDS (bfloat16, whole pieces) or through registers, where it is split; the matrix's codes through registers, where they are widened.
+template <class T, bool RCOL, int BM, int BN, int WAVES_M, int WAVES_N, bool ASYNC>
+__global__ void __launch_bounds__(WAVES_M * WAVES_N * WAVE, 2) k_gmm_mx4(GmmArgs a, Mx4Args m, int nt)
+{
+    constexpr int THREADS = WAVES_M * WAVES_N * WAVE, WM = BM / WAVES_M, WN = BN / WAVES_N, TM = WM / 16, TN = WN / 16, PARTS = PARTS_OF<T>;
+    constexpr int STEP_C = STEP<bf16_t>;
+    static_assert(!ASYNC || PARTS == 1, "parts are made in registers");
+    using TL = Tile<bf16_t, false, false, BM, THREADS, LINE>;
+    using TR = Tile<bf16_t, RCOL, !RCOL, BN, THREADS, LINE>;
+    constexpr int BUFFER = PARTS * TL::BYTES + TR::BYTES;
+    // A thread's share of the matrix's step: E numbers of a line side by side, in one block.
+    constexpr int E = BN * STEP_C / THREADS, WORDS = E / 8, A_LINE = (RCOL ? BN : STEP_C) / E;
+    static_assert(E == 16 || E == 32, "part of a block");
+    __shared__ __align__(16) char lds[2 * BUFFER];
+    RowsTile w;
+    if (!rows_tile<T>(a, BM, BN, nt, w)) return;
+    const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid / WAVE);
+    const int wm = (wave / WAVES_N) * WM, wn = (wave % WAVES_N) * WN;
+    const int depth = (int)a.c, steps = (depth + STEP_C - 1) / STEP_C;
+
+    Feed<bf16_t, TL, false, true> feed;
+    int64_t row[ASYNC ? 1 : TL::LOADS];   // elements to the line's row
+    if constexpr (ASYNC) {
+        const int64_t first = a.index ? 0 : w.m0;
+        feed.lines(tid, static_cast<const bf16_t *>(a.l) + first * a.ldl, a.ldl, [&](int line) { return tile_row(a, w, line) - first; });
+    } else {
+#pragma unroll
+        for (int i = 0; i < TL::LOADS; ++i) row[i] = tile_row(a, w, TL::line_of(tid, i)) * a.ldl;
+    }
+    const int line = tid / A_LINE, part = tid % A_LINE;
+    const uint8_t *codes = m.codes + w.group * m.stride_codes, *scales = m.scales + w.group * m.stride_scales;
+    if constexpr (RCOL) {
+        const int block = min((w.n0 + part * E) / MX4_BLOCK, m.blocks - 1);   // (what comes of columns behind the end is not stored)
+        codes += block * 16 + part * E % MX4_BLOCK / 2;
+        scales += block;
+    } else {
+        const int64_t n = min(w.n0 + line, (int)a.n - 1);
+        codes += n * m.ld_codes + part * (E / 2);
+        scales += n * m.ld_scales;
+    }
+
+    struct Raw { uint4 v[sizeof(T) / 2]; };
+    Raw kept[ASYNC ? 1 : TL::LOADS];
+    uint32_t kept_codes[WORDS], kept_scale = 0;
+    // Workgroups begin at different steps and go round, so that they don't all read lines that begin in the same memory channels; what is left
+    // of the lines behind whole steps comes last.
+    const int whole = depth / STEP_C, turn = whole == 0 ? 0 : (w.n0 / BN + w.group * 5) % whole;
+    auto at = [&](int t) { return t == whole ? t : t + turn >= whole ? t + turn - whole : t + turn; };
+    auto fetch = [&](int t_) {
+        const int t = at(t_), c0 = t * STEP_C, left = min(STEP_C, depth - c0);
+        const bool there = RCOL ? line < left : c0 + part * E < m.blocks * MX4_BLOCK;
+        const uint8_t *from = RCOL ? codes + (int64_t)(there ? c0 + line : 0) * m.ld_codes : codes + (there ? c0 / 2 : 0);
+        if constexpr (!RCOL) from = there ? from : codes - part * (E / 2);
+        if constexpr (WORDS == 4) {
+            const uint4 v = *reinterpret_cast<const uint4 *>(from);
+            kept_codes[0] = v.x, kept_codes[1] = v.y, kept_codes[2] = v.z, kept_codes[3] = v.w;
+        } else {
+            const uint2 v = *reinterpret_cast<const uint2 *>(from);
+            kept_codes[0] = v.x, kept_codes[1] = v.y;
+        }
+        kept_scale = RCOL ? scales[(int64_t)(there ? c0 + line : 0) * m.ld_scales] : scales[there ? (c0 + part * E) / MX4_BLOCK : 0];
+        if (!there) {
+#pragma unroll
+            for (int j = 0; j < WORDS; ++j) kept_codes[j] = 0;
+            kept_scale = 127;
+        }
+        if constexpr (ASYNC) {
+            char *to = lds + (t_ & 1) * BUFFER + wave * (WAVE * 16);
+            if (left == STEP_C) {
+                const char *base = feed.step(t);
+#pragma unroll
+                for (int i = 0; i < TL::LOADS; ++i) load_to_lds(base + feed.off[i], to + i * THREADS * 16);
+            } else {
+#pragma unroll
+                for (int i = 0; i < TL::LOADS; ++i)
+                    load_to_lds(either(feed.valid(tid, i, left) > 0, feed.step(t) + feed.off[i], &g_zero_piece), to + i * THREADS * 16);
+            }
+        } else {
+            const T *x = static_cast<const T *>(a.l) + c0;
+#pragma unroll
+            for (int i = 0; i < TL::LOADS; ++i) {
+                const T *p = x + row[i] + TL::piece_of(tid, i) * 8;
+                const int valid = left - TL::piece_of(tid, i) * 8;
+#pragma unroll
+                for (int j = 0; j < (int)sizeof(T) / 2; ++j)
+                    kept[i].v[j] = left == STEP_C ? load_any(reinterpret_cast<const char *>(p + j * PIECE<T>)) : load_piece(p + j * PIECE<T>, valid - j * PIECE<T>);
+            }
+        }
+    };
+    auto stash = [&](int t_) {
+        char *to = lds + (t_ & 1) * BUFFER;
+        if constexpr (!ASYNC) {
+#pragma unroll
+            for (int i = 0; i < TL::LOADS; ++i) {
+                bf16x8 p[PARTS];
+                split<T>(__builtin_bit_cast(decltype(Vec<T, 8>{}), kept[i]).e, p);
+#pragma unroll
+                for (int k = 0; k < PARTS; ++k) *reinterpret_cast<bf16x8 *>(to + k * TL::BYTES + (i * THREADS + tid) * 16) = p[k];
+            }
+        }
+        if constexpr (!RCOL) {
+            const int valid = depth - (at(t_) * STEP_C + part * E);
+            if (valid < E) {   // (codes behind the end meet zeros of x, but may be infinite numbers)
+#pragma unroll
+                for (int j = 0; j < WORDS; ++j) kept_codes[j] = mx4_first(kept_codes[j], valid - j * 8);
+            }
+        }
+        const int swizzle = RCOL ? col_xor<bf16_t, TR::PIECES>(line) : row_xor<!RCOL, TR::PIECES>(line);
+        char *to_line = to + PARTS * TL::BYTES + line * TR::PIECES * 16;
+        const float scale = mx4_scale(kept_scale);
+#pragma unroll
+        for (int j = 0; j < WORDS; ++j) {
+            bf16_t v[8];
+            mx4_widen<bf16_t>(kept_codes[j], scale, v);
+            *reinterpret_cast<bf16x8 *>(to_line + ((part * WORDS + j) ^ swizzle) * 16) = bf16x8{v[0], v[1], v[2], v[3], v[4], v[5], v[6], v[7]};
+        }
+    };
+
+    const uint32_t at_l = TL::place(wm), at_r = TR::place(wn);
+    f32x4 acc[TM][TN] = {};
+    // (single precision: the sums of 256 products are put aside, as in k_gmm)
+    constexpr bool ASIDE = sizeof(T) == 4;
+    f32x4 sums[ASIDE ? TM : 1][ASIDE ? TN : 1] = {};
+    auto put_aside = [&] {
+        if constexpr (ASIDE) {
+#pragma unroll
+            for (int i = 0; i < TM; ++i)
+#pragma unroll
+                for (int j = 0; j < TN; ++j) {
+                    sums[i][j] += acc[i][j];
+                    acc[i][j] = f32x4{};
+                }
+        }
+    };
+    auto multiply = [&](int buffer) {
+        const char *from = lds + buffer * BUFFER;
+        auto half = [&](auto h) {
+            Frag<bf16_t> fr[TN], fl[TM];
+            TR::template read<decltype(h)::value>(from + PARTS * TL::BYTES, at_r, fr);
+#pragma unroll
+            for (int p = PARTS - 1; p >= 0; --p) {
+                TL::template read<decltype(h)::value>(from + p * TL::BYTES, at_l, fl);
+                mma<bf16_t>(acc, fr, fl);
+            }
+        };
+        half(std::integral_constant<int, 0>{});
+        half(std::integral_constant<int, 1>{});
+    };
+    if (steps > 0) {
+        fetch(0);
+        stash(0);
+    }
+    for (int t = 0; t < steps; ++t) {
+        asm volatile("" ::: "memory");
+        __builtin_amdgcn_s_waitcnt(0x0070);   // vmcnt(0), lgkmcnt(0): this wave's part of the step is in LDS, and what it read of the step before has come
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+        if (t + 1 < steps) fetch(t + 1);
+        multiply(t & 1);
+        if (ASIDE && t % 4 == 3) put_aside();
+        if (t + 1 < steps) stash(t + 1);
+    }
+    if constexpr (ASIDE) {
+#pragma unroll
+        for (int i = 0; i < TM; ++i)
+#pragma unroll
+            for (int j = 0; j < TN; ++j) acc[i][j] += sums[i][j];
+    }
+    store_tile<T, BM, BN, WAVES_M, WAVES_N, !RCOL, sizeof(lds)>(a, w, acc, lds);
+}
+
+// Few rows: the matrix is read once, straight into registers, each wave every WAVES-th 128 numbers of its lines, a block a lane (so a lane's 32 numbers
+// of c are those of its block, in four matrix instructions; x is read to match).
+template <class T, int TN, int WAVES>
+__global__ void __launch_bounds__(WAVES * WAVE, 2) k_few_mx4(GmmArgs a, Mx4Args m)
+{
+    constexpr int PARTS = PARTS_OF<T>;
+    __shared__ __align__(16) float s_sums[WAVES * 64 * (TN * 16 + 4)];
+    __shared__ int64_t s_row[64];
+    RowsTile w;
+    int rows;
+    if (!few_rows_tile<T, TN * 16>(a, w, rows, s_row)) return;
+    const int lane = lane_id(), r = lane % 16, g = lane / 16, wave = threadIdx.x / WAVE;
+    const uint8_t *codes[TN], *scales[TN];
+#pragma unroll
+    for (int j = 0; j < TN; ++j) {
+        const int64_t n = min(w.n0 + j * 16 + r, (int)a.n - 1);
+        codes[j] = m.codes + w.group * m.stride_codes + n * m.ld_codes + g * 16;
+        scales[j] = m.scales + w.group * m.stride_scales + n * m.ld_scales + g;
+    }
+    T *out = static_cast<T *>(a.out);
+    auto store = [&](int row, int64_t col, float v) { out[(int64_t)(w.m0 + row) * a.ldo + col] = (T)(s_row[row] < 0 ? 0.0f : v); };
+    auto tile = [&](auto tm) {
+        constexpr int TM = decltype(tm)::value, UNROLL = TM == 1 ? 2 : 1;
+        const T *x[TM];
+#pragma unroll
+        for (int i = 0; i < TM; ++i) x[i] = static_cast<const T *>(a.l) + max(s_row[min(i * 16 + r, rows - 1)], (int64_t)0) * a.ldl + g * MX4_BLOCK;
+        f32x4 acc[TM][TN] = {};
+        const int whole = (int)(a.c / 128), steps = (int)((a.c + 127) / 128);
+        auto step = [&](const uint4 (&v)[TN], const uint32_t (&s)[TN], int t, bool all) {
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const int valid = all ? 8 : (int)a.c - (t * 128 + g * MX4_BLOCK + q * 8);
+                Frag<bf16_t> fw[TN];
+#pragma unroll
+                for (int j = 0; j < TN; ++j) {
+                    const uint32_t word = q == 0 ? v[j].x : q == 1 ? v[j].y : q == 2 ? v[j].z : v[j].w;
+                    bf16_t e[8];
+                    mx4_widen<bf16_t>(mx4_first(word, valid), mx4_scale(s[j]), e);
+                    fw[j] = bf16x8{e[0], e[1], e[2], e[3], e[4], e[5], e[6], e[7]};
+                }
+#pragma unroll
+                for (int i = 0; i < TM; ++i) {
+                    T e[8];
+                    bf16x8 p[PARTS];
+                    load8<T, false>(x[i] + t * 128 + q * 8, min(valid, 8), e);
+                    split<T>(e, p);
+#pragma unroll
+                    for (int k = PARTS - 1; k >= 0; --k)
+#pragma unroll
+                        for (int j = 0; j < TN; ++j) mma_part(acc[i][j], fw[j], p[k], 0);
+                }
+            }
+        };
+        int t = wave;
+        for (; t + (UNROLL - 1) * WAVES < whole; t += UNROLL * WAVES) {
+            uint4 v[UNROLL][TN];
+            uint32_t s[UNROLL][TN];
+#pragma unroll
+            for (int u = 0; u < UNROLL; ++u)
+#pragma unroll
+                for (int j = 0; j < TN; ++j) {
+                    v[u][j] = *reinterpret_cast<const uint4 *>(codes[j] + (t + u * WAVES) * 64);
+                    s[u][j] = scales[j][(t + u * WAVES) * 4];
+                }
+#pragma unroll
+            for (int u = 0; u < UNROLL; ++u) step(v[u], s[u], t + u * WAVES, true);
+        }
+        for (; t < steps; t += WAVES) {
+            uint4 v[TN];
+            uint32_t s[TN];
+            const bool there = t * 4 + g < m.blocks;
+#pragma unroll
+            for (int j = 0; j < TN; ++j) {
+                v[j] = there ? *reinterpret_cast<const uint4 *>(codes[j] + t * 64) : make_uint4(0, 0, 0, 0);
+                s[j] = there ? scales[j][t * 4] : 127u;
+            }
+            step(v, s, t, false);
+        }
+        const float first[(TM * TN * 256 + WAVES * WAVE - 1) / (WAVES * WAVE)] = {};
+        few_finish<T, TM, TN, WAVES>(acc, first, rows, w.n0, a.n, s_sums, store);
+    };
+    if (rows <= 16) tile(std::integral_constant<int, 1>{});
+    else if (rows <= 32) tile(std::integral_constant<int, 2>{});
+    else tile(std::integral_constant<int, 4>{});
+}
+
+template <class T, bool RCOL, int BM, int BN, int WAVES_M, int WAVES_N, bool ASYNC> hipError_t launch_tile(const GmmArgs &a, const Mx4Args &m, hipStream_t s)
+{
+    const Grid g = grid_of<GM_ROWS>(a, BM, BN);
+    constexpr int threads = WAVES_M * WAVES_N * WAVE;
+    if (g.blocks * threads >= (1ll << 32)) return TOO_MANY_TILES;
+    hipLaunchKernelGGL((k_gmm_mx4<T, RCOL, BM, BN, WAVES_M, WAVES_N, ASYNC>), dim3((uint32_t)g.blocks), dim3(threads), 0, s, a, m, (int)g.nt);
+    return hipGetLastError();
+}
+
+template <class T, bool RCOL> hipError_t pick(const GmmArgs &a, const Mx4Args &m, bool straight, hipStream_t s)
+{
+    const int64_t groups = std::min(a.groups, a.rows);
+    auto m_tiles = [&](int64_t bm) { return std::max(groups, a.rows / bm + groups / 2); };
+    auto tiles = [&](int64_t bm, int64_t bn) { return (double)m_tiles(bm) * (double)((a.n + bn - 1) / bn); };
+    if constexpr (!RCOL) {
+        if (groups > 0 && groups * ((a.n + 63) / 64) < 256 && a.rows <= groups * 24) {
+            hipLaunchKernelGGL((k_few_mx4<T, 1, 8>), few_grid(a, 16), dim3(8 * WAVE), 0, s, a, m);
+            return hipGetLastError();
+        }
+    }
+    if constexpr (std::is_same<T, bf16_t>::value) {
+        if (straight) {
+            if (tiles(128, 128) >= 512 && launches<GM_ROWS>(a, 256, 256, 512)) return launch_tile<T, RCOL, 256, 256, 2, 4, true>(a, m, s);
+            if (tiles(64, 64) >= 512 || !launches<GM_ROWS>(a, 64, 64, 256)) return launch_tile<T, RCOL, 128, 128, 2, 2, true>(a, m, s);
+            return launch_tile<T, RCOL, 64, 64, 4, 1, true>(a, m, s);
+        }
+    }
+    if (tiles(64, 64) >= 512 || !launches<GM_ROWS>(a, 64, 64, 256)) return launch_tile<T, RCOL, 128, 128, 2, 2, false>(a, m, s);
+    return launch_tile<T, RCOL, 64, 64, 4, 1, false>(a, m, s);
+}
+
+}  // namespace
+
+hipError_t launch_grouped_mx4(const ocean_groups &g, int dtype, const void *x, int64_t ldx, const ocean_mx4 &w, bool transposed, void *y, int64_t ldy, hipStream_t s)
+{
+    const int64_t outer = transposed ? w.inner : w.rows, inner = transposed ? w.rows : w.inner;
+    if (g.rows == 0 || outer == 0) return hipSuccess;
+    GmmArgs a{};
+    a.l = x, a.ldl = ldx;
+    a.out = y, a.ldo = ldy;
+    a.ptr = g.group_ptr, a.groups = g.experts, a.rows = g.rows;
+    a.n = outer, a.c = inner;
+    a.index = g.row_index, a.index_rows = g.row_index ? g.x_rows : g.rows;
+    if (g.x_rows == 0 || inner == 0) a.c = 0, a.index_rows = 0, a.index = nullptr;
+    const Mx4Args m = mx4_args(w);
+    // (the rows of a tile lie within 256 lines, gathered ones anywhere in x)
+    const bool straight = dtype == OCEAN_BF16 && pieces_aligned(x, ldx, 0, 2) && inner % 8 == 0 && offsets_fit(g.row_index ? std::max<int64_t>(g.x_rows, 256) : 256, ldx, 2);
+    return with_type(dtype, [&](auto t) {
+        using T = decltype(t);
+        return transposed ? pick<T, true>(a, m, straight, s) : pick<T, false>(a, m, straight, s);
+    });
+}
+
+}  // namespace ocean
