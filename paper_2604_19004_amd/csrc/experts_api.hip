@@ -28,6 +28,15 @@ const char *mx4_fault(const ocean_mx4 *q, bool written)
     return nullptr;
 }
 
+// (tiles reach a matrix's lines by 32-bit offsets)
+const char *product_fault(const ocean_mx4 *w, const ocean_groups *g)
+{
+    if (const char *why = mx4_fault(w, false)) return why;
+    if (w->count != g->experts) return "the matrices in four bits are not as many as the groups";
+    if (w->ld_codes >= (1 << 23) || w->ld_scales >= (1 << 23)) return "row strides of the matrices of a product must be below 2^23 bytes";
+    return nullptr;
+}
+
 const char *converted_fault(const ocean_mx4 *q, const void *p, int32_t dtype, int64_t ld, int64_t stride, bool to_q)
 {
     if (!known_type(dtype)) return "dtype must be OCEAN_F32, OCEAN_BF16 or OCEAN_F16";
@@ -89,8 +98,7 @@ int ocean_grouped_matmul_mx4(const ocean_groups *g, int32_t dtype, const void *x
 {
     if (!known_type(dtype)) return bad("dtype must be OCEAN_F32, OCEAN_BF16 or OCEAN_F16");
     REFUSE(groups_fault(g));
-    REFUSE(mx4_fault(w, false));
-    if (w->count != g->experts) return bad("the matrices in four bits are not as many as the groups");
+    REFUSE(product_fault(w, g));
     REFUSE(matrix_fault(x, g->x_rows, transposed ? w->rows : w->inner, ld_x, dtype));
     REFUSE(matrix_fault(y, g->rows, transposed ? w->inner : w->rows, ld_y, dtype));
     return launched(launch_grouped_mx4(*g, dtype, x, ld_x, *w, transposed != 0, y, ld_y, static_cast<hipStream_t>(stream)), "ocean_grouped_matmul_mx4");
@@ -102,8 +110,7 @@ int ocean_grouped_matmul_mx4_mx4(const ocean_groups *g, const ocean_mx4 *x, cons
     if (!known_type(dtype)) return bad("dtype must be OCEAN_F32, OCEAN_BF16 or OCEAN_F16");
     REFUSE(groups_fault(g));
     REFUSE(mx4_fault(x, false));
-    REFUSE(mx4_fault(w, false));
-    if (w->count != g->experts) return bad("the matrices in four bits are not as many as the groups");
+    REFUSE(product_fault(w, g));
     if (x->count != 1 || x->rows != g->x_rows || x->inner != w->inner) return bad("x must be one matrix of x_rows rows with the matrices' inner");
     REFUSE(matrix_fault(y, g->rows, w->rows, ld_y, dtype));
     return launched(launch_grouped_mx4_mx4(*g, *x, *w, dtype, y, ld_y, static_cast<hipStream_t>(stream)), "ocean_grouped_matmul_mx4_mx4");

@@ -26,12 +26,6 @@ __device__ __forceinline__ u32x4 first_codes(u32x4 v, int valid)
     return v;
 }
 
-// 4 bytes from memory straight to LDS; the wave's 256 bytes begin at `lds`.
-__device__ __forceinline__ void load_word_to_lds(const void *src, char *lds)
-{
-    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)src, (__attribute__((address_space(3))) void *)lds, 4, 0, 0);
-}
-
 template <class O, int BM, int BN, int WAVES_M, int WAVES_N, int STAGES>
 __global__ void __launch_bounds__(WAVES_M * WAVES_N * WAVE, 2) k_gmm_mx4_mx4(GmmArgs a, Mx4Args x, Mx4Args m, int nt)
 {
@@ -48,77 +42,94 @@ __global__ void __launch_bounds__(WAVES_M * WAVES_N * WAVE, 2) k_gmm_mx4_mx4(Gmm
     const int depth = m.blocks * 16, steps = (m.blocks + STEP_BLOCKS - 1) / STEP_BLOCKS;   // bytes of a line
     const uint8_t *w_codes = m.codes + w.group * m.stride_codes, *w_scales = m.scales + w.group * m.stride_scales;
 
-    Feed<uint8_t, TL, false, true> feed_l;
-    Feed<uint8_t, TR, false, true> feed_r;
-    const int64_t base = a.index ? 0 : w.m0;
-    feed_l.lines(tid, x.codes + base * x.ld_codes, x.ld_codes, [&](int line) { return tile_row(a, w, line) - base; });
-    feed_r.lines(tid, w_codes + (int64_t)w.n0 * m.ld_codes, m.ld_codes, [&](int line) -> int64_t { return min(line, (int)a.n - 1 - w.n0); });
-    // Scales lie in LDS as [half of the step][line of x, then of the matrix], a word of four blocks each.
-    const uint8_t *scale[SCALE_LOADS];
+    const int64_t first = a.index ? 0 : w.m0;
+    const Memory l_codes = memory_at(x.codes + first * x.ld_codes), r_codes = memory_at(w_codes + (int64_t)w.n0 * m.ld_codes);
+    uint32_t off_l[TL::LOADS], off_r[TR::LOADS], off_s[SCALE_LOADS];
+#pragma unroll
+    for (int i = 0; i < TL::LOADS; ++i) off_l[i] = (uint32_t)(tile_row(a, w, TL::line_of(tid, i)) - first) * (uint32_t)x.ld_codes + TL::piece_of(tid, i) * 16;
+#pragma unroll
+    for (int i = 0; i < TR::LOADS; ++i) off_r[i] = (uint32_t)min(TR::line_of(tid, i), (int)a.n - 1 - w.n0) * (uint32_t)m.ld_codes + TR::piece_of(tid, i) * 16;
+    // Scales lie in LDS as [half of the step][line of x, then of the matrix], a word of four blocks each; a wave's words are all of one operand and half.
+    const uint8_t *l_scales = x.scales + first * x.ld_scales, *r_scales = w_scales + (int64_t)w.n0 * m.ld_scales;
 #pragma unroll
     for (int i = 0; i < SCALE_LOADS; ++i) {
-        const int q = i * THREADS + tid, half = q / LINES, line = q % LINES;
-        scale[i] = (line < BM ? x.scales + tile_row(a, w, line) * x.ld_scales : w_scales + min(w.n0 + line - BM, (int)a.n - 1) * m.ld_scales) + half * 4;
+        const int line = (i * THREADS + tid) % LINES;
+        off_s[i] = line < BM ? (uint32_t)(tile_row(a, w, line) - first) * (uint32_t)x.ld_scales : (uint32_t)min(line - BM, (int)a.n - 1 - w.n0) * (uint32_t)m.ld_scales;
     }
     // (the order of the steps is that of k_gmm_mx4)
-    const int whole = m.blocks / STEP_BLOCKS, turn = whole == 0 ? 0 : (w.n0 / BN + w.group * 5) % whole;
+    const int whole = (int)(a.c / (STEP_BLOCKS * MX4_BLOCK)), turn = whole == 0 ? 0 : (w.n0 / BN + w.group * 5) % whole;
     auto at = [&](int t) { return t == whole ? t : t + turn >= whole ? t + turn - whole : t + turn; };
     auto fetch = [&](int t_, int buffer) {
-        const int t = at(t_), left = min(LINE, depth - t * LINE);
+        const int t = at(t_), left = depth - t * LINE;
         char *to = lds + buffer * BUFFER, *to_wave = to + wave * (WAVE * 16);
-        auto move = [&](auto &feed, auto tile, char *dst) {
-            using TI = decltype(tile);
-            const char *from = feed.step(t);
 #pragma unroll
-            for (int i = 0; i < TI::LOADS; ++i) {
-                if (left == LINE) load_to_lds(from + feed.off[i], dst + i * THREADS * 16);
-                else load_to_lds(either(feed.valid(tid, i, left) > 0, from + feed.off[i], &g_zero_piece), dst + i * THREADS * 16);
-            }
-        };
-        move(feed_l, TL{}, to_wave);
-        move(feed_r, TR{}, to_wave + TL::BYTES);
+        for (int i = 0; i < TL::LOADS; ++i)
+            memory_to_lds<16>(l_codes, TL::piece_of(tid, i) * 16 < left ? off_l[i] : NOWHERE, t * LINE, to_wave + i * THREADS * 16);
+#pragma unroll
+        for (int i = 0; i < TR::LOADS; ++i)
+            memory_to_lds<16>(r_codes, TR::piece_of(tid, i) * 16 < left ? off_r[i] : NOWHERE, t * LINE, to_wave + TL::BYTES + i * THREADS * 16);
 #pragma unroll
         for (int i = 0; i < SCALE_LOADS; ++i) {
-            const int half = (i * THREADS + tid) / LINES;
-            const bool there = t * STEP_BLOCKS + half * HALF_BLOCKS < m.blocks;
-            load_word_to_lds(either(there, scale[i] + t * STEP_BLOCKS, &g_zero_piece), to + CODES + (i * THREADS + wave * WAVE) * 4);
+            const int word = i * THREADS + wave * WAVE, half = word / LINES, block = t * STEP_BLOCKS + half * HALF_BLOCKS;
+            const Memory scales = memory_at(word % LINES < BM ? l_scales : r_scales);
+            memory_to_lds<4>(scales, block < m.blocks ? off_s[i] : NOWHERE, block, to + CODES + word * 4);
         }
+    };
+
+    // The end of the lines: of this thread's pieces, codes of x behind it become 0 and scales of blocks behind it 1 (an empty block's could be NaN).
+    auto end_lines = [&](int t, char *buffer) {
+#pragma unroll
+        for (int i = 0; i < TL::LOADS; ++i) {
+            const int valid = (int)a.c - (t * STEP_BLOCKS + TL::piece_of(tid, i)) * MX4_BLOCK;
+            u32x4 *piece = reinterpret_cast<u32x4 *>(buffer + (i * THREADS + tid) * 16);
+            if (valid < MX4_BLOCK) *piece = first_codes(*piece, valid);
+        }
+#pragma unroll
+        for (int i = 0; i < SCALE_LOADS; ++i) {
+            const int word = i * THREADS + tid, there = m.blocks - (t * STEP_BLOCKS + word / LINES * HALF_BLOCKS);
+            uint32_t *scales = reinterpret_cast<uint32_t *>(buffer + CODES + word * 4);
+            if (there < HALF_BLOCKS) *scales = there <= 0 ? 0x7f7f7f7fu : (*scales & ((1u << 8 * there) - 1u)) | 0x7f7f7f7fu << 8 * there;
+        }
+        __builtin_amdgcn_s_waitcnt(0xc07f);   // lgkmcnt(0)
     };
 
     const uint32_t at_l = TL::place(wm), at_r = TR::place(wn);
     f32x4 acc[TM][TN] = {};
-    auto multiply = [&](int t_, int buffer) {
+    // A step in portions: 128 numbers of c of all the wave's columns and AT_ONCE of its 16s of rows, the next portion's reads under way meanwhile (all at once
+    // don't fit the registers beside the sums).
+    constexpr int AT_ONCE = TM < 4 ? TM : 4, PER_HALF = TM / AT_ONCE, PORTIONS = 2 * PER_HALF;
+    auto multiply = [&](int buffer) {
         const char *from = lds + buffer * BUFFER;
         const uint32_t *scales = reinterpret_cast<const uint32_t *>(from + CODES);
-        const int t = at(t_);
-        auto half = [&](auto h_) {
-            constexpr int h = decltype(h_)::value;
-            u32x4 fr[TN], fl[TM];
-            uint32_t sr[TN], sl[TM];
-            TR::template read<h>(from + TL::BYTES, at_r, fr);
-            TL::template read<h>(from, at_l, fl);
+        u32x4 fr[2][TN], fl[2][AT_ONCE];
+        uint32_t sr[2][TN], sl[2][AT_ONCE];
+        auto read = [&](auto portion) {
+            constexpr int p = decltype(portion)::value, h = p / PER_HALF, i0 = p % PER_HALF * AT_ONCE;
+            if constexpr (i0 == 0) {
+                TR::template read<h>(from + TL::BYTES, at_r, fr[h]);
 #pragma unroll
-            for (int j = 0; j < TN; ++j) sr[j] = scales[h * LINES + BM + wn + tile_line<true>(j, r)] >> (8 * g);
-#pragma unroll
-            for (int i = 0; i < TM; ++i) sl[i] = scales[h * LINES + wm + tile_line<false>(i, r)] >> (8 * g);
-            const int left = (int)a.c - (t * STEP_BLOCKS + h * HALF_BLOCKS) * MX4_BLOCK;
-            if (left < HALF_BLOCKS * MX4_BLOCK) {   // (the end of the lines: codes behind it count as 0, and scales as 1)
-                const int valid = left - g * MX4_BLOCK;
-#pragma unroll
-                for (int i = 0; i < TM; ++i) {
-                    fl[i] = first_codes(fl[i], valid);
-                    sl[i] = valid > 0 ? sl[i] : 127u;
-                }
-#pragma unroll
-                for (int j = 0; j < TN; ++j) sr[j] = valid > 0 ? sr[j] : 127u;
+                for (int j = 0; j < TN; ++j) sr[h][j] = scales[h * LINES + BM + wn + tile_line<true>(j, r)] >> (8 * g);
             }
+            TL::template read<h>(from + tile_line<false>(i0, 0) * LINE, at_l, fl[p & 1]);
 #pragma unroll
-            for (int i = 0; i < TM; ++i)
-#pragma unroll
-                for (int j = 0; j < TN; ++j) mma_mx4(acc[i][j], fr[j], sr[j], fl[i], sl[i]);
+            for (int i = 0; i < AT_ONCE; ++i) sl[p & 1][i] = scales[h * LINES + wm + tile_line<false>(i0 + i, r)] >> (8 * g);
         };
-        half(std::integral_constant<int, 0>{});
-        half(std::integral_constant<int, 1>{});
+        auto portion = [&](auto portion) {
+            constexpr int p = decltype(portion)::value, h = p / PER_HALF, i0 = p % PER_HALF * AT_ONCE;
+            if constexpr (p < PORTIONS) {
+                if constexpr (p + 1 < PORTIONS) read(std::integral_constant<int, p + 1>{});
+#pragma unroll
+                for (int i = 0; i < AT_ONCE; ++i)
+#pragma unroll
+                    for (int j = 0; j < TN; ++j) mma_mx4(acc[i0 + i][j], fr[h][j], sr[h][j], fl[p & 1][i], sl[p & 1][i]);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+        };
+        read(std::integral_constant<int, 0>{});
+        portion(std::integral_constant<int, 0>{});
+        portion(std::integral_constant<int, 1>{});
+        portion(std::integral_constant<int, 2>{});
+        portion(std::integral_constant<int, 3>{});
     };
 #pragma unroll
     for (int t = 0; t < STAGES - 1; ++t)
@@ -132,79 +143,80 @@ __global__ void __launch_bounds__(WAVES_M * WAVES_N * WAVE, 2) k_gmm_mx4_mx4(Gmm
         asm volatile("" ::: "memory");
         if (t + STAGES - 2 < steps) __builtin_amdgcn_s_waitcnt(0x0070 | (LATER & 15) | (LATER >> 4) << 14);
         else __builtin_amdgcn_s_waitcnt(0x0070);
+        asm volatile("" ::: "memory");
+        if (t == whole) end_lines(t, lds + buffer * BUFFER);
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
         if (t + STAGES - 1 < steps) fetch(t + STAGES - 1, buffer == 0 ? STAGES - 1 : buffer - 1);   // (in place of the step before)
-        multiply(t, buffer);
+        multiply(buffer);
         buffer = buffer + 1 == STAGES ? 0 : buffer + 1;
     }
     store_tile<O, BM, BN, WAVES_M, WAVES_N, true, sizeof(lds)>(a, w, acc, lds);
 }
 
-// Few rows: the matrix is read once, straight into registers, each wave every WAVES-th 128 numbers of its lines, a block and its scale a lane.
+// Few rows: the matrix is read once, straight into registers, a block and its scale a lane.
 template <class O, int TN, int WAVES>
 __global__ void __launch_bounds__(WAVES * WAVE, 2) k_few_mx4_mx4(GmmArgs a, Mx4Args x, Mx4Args m)
 {
-    __shared__ __align__(16) float s_sums[WAVES * 64 * (TN * 16 + 4)];
-    __shared__ int64_t s_row[64];
+    __shared__ __align__(16) float s_sums[few_lds(TN, WAVES)];
+    __shared__ int64_t s_row[FEW_ROWS];
     RowsTile w;
-    int rows;
-    if (!few_rows_tile<O, TN * 16>(a, w, rows, s_row)) return;
-    const int lane = lane_id(), r = lane % 16, g = lane / 16, wave = threadIdx.x / WAVE;
+    if (!few_rows_tile<O, TN * 16>(a, w)) return;
+    const int lane = lane_id(), r = lane % 16, g = lane / 16, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE);
+    const uint8_t *codes[TN], *scales[TN];
+#pragma unroll
+    for (int j = 0; j < TN; ++j) {
+        const int64_t n = min(w.n0 + j * 16 + r, (int)a.n - 1);
+        codes[j] = m.codes + w.group * m.stride_codes + n * m.ld_codes;
+        scales[j] = m.scales + w.group * m.stride_scales + n * m.ld_scales;
+    }
+    const int whole = (int)(a.c / 128), steps = (int)((a.c + 127) / 128), rows = min(FEW_ROWS, w.hi - w.m0);
+    auto load_w = [&](Mx4Blocks<TN> &to, int t) { to.load(codes, scales, min(t * 4 + g, m.blocks - 1)); };
     O *out = static_cast<O *>(a.out);
     auto store = [&](int row, int64_t col, float v) { out[(int64_t)(w.m0 + row) * a.ldo + col] = (O)(s_row[row] < 0 ? 0.0f : v); };
     auto tile = [&](auto tm) {
-        constexpr int TM = decltype(tm)::value, UNROLL = TM == 1 ? 4 : 2, N = TM + TN;
-        const uint8_t *codes[N], *scales[N];   // of x's lines, then the matrix's
+        constexpr int TM = decltype(tm)::value, U = TM <= 2 && TN <= 2 ? 4 : 2;
+        Mx4Blocks<TN> now[U];
+        if (wave < steps) {
+#pragma unroll
+            for (int u = 0; u < U; ++u) load_w(now[u], wave + u * WAVES);
+        }
+        if ((int)threadIdx.x < rows) {
+            const int64_t row = a.index ? a.index[w.m0 + threadIdx.x] : w.m0 + threadIdx.x;
+            s_row[threadIdx.x] = (uint64_t)row < (uint64_t)a.index_rows ? row : -1;
+        }
+        __syncthreads();
+        const uint8_t *x_codes[TM], *x_scales[TM];
 #pragma unroll
         for (int i = 0; i < TM; ++i) {
             const int64_t row = max(s_row[min(i * 16 + r, rows - 1)], (int64_t)0);
-            codes[i] = x.codes + row * x.ld_codes + g * 16;
-            scales[i] = x.scales + row * x.ld_scales + g;
-        }
-#pragma unroll
-        for (int j = 0; j < TN; ++j) {
-            const int64_t n = min(w.n0 + j * 16 + r, (int)a.n - 1);
-            codes[TM + j] = m.codes + w.group * m.stride_codes + n * m.ld_codes + g * 16;
-            scales[TM + j] = m.scales + w.group * m.stride_scales + n * m.ld_scales + g;
+            x_codes[i] = x.codes + row * x.ld_codes;
+            x_scales[i] = x.scales + row * x.ld_scales;
         }
         f32x4 acc[TM][TN] = {};
-        const int whole = (int)(a.c / 128), steps = (int)((a.c + 127) / 128);
-        int t = wave;
-        for (; t + (UNROLL - 1) * WAVES < whole; t += UNROLL * WAVES) {
-            u32x4 v[UNROLL][N];
-            uint32_t s[UNROLL][N];
+        Mx4Blocks<TM> xs[U];
+        auto load_x = [&](int t, bool) {
 #pragma unroll
-            for (int u = 0; u < UNROLL; ++u)
+            for (int u = 0; u < U; ++u) xs[u].load(x_codes, x_scales, min((t + u * WAVES) * 4 + g, m.blocks - 1));
+        };
+        auto use = [&](Mx4Blocks<TN> (&b)[U], int t0, bool end) {
 #pragma unroll
-                for (int k = 0; k < N; ++k) {
-                    v[u][k] = *reinterpret_cast<const u32x4 *>(codes[k] + (t + u * WAVES) * 64);
-                    s[u][k] = scales[k][(t + u * WAVES) * 4];
+            for (int u = 0; u < U; ++u) {
+                const int t = t0 + u * WAVES;
+                if (end && t >= whole) {
+                    const int valid = (int)max(min(a.c - ((int64_t)t * 128 + g * MX4_BLOCK), (int64_t)32), (int64_t)0);
+                    b[u].end(valid);
+                    xs[u].end(valid);
                 }
-#pragma unroll
-            for (int u = 0; u < UNROLL; ++u)
 #pragma unroll
                 for (int i = 0; i < TM; ++i)
 #pragma unroll
-                    for (int j = 0; j < TN; ++j) mma_mx4(acc[i][j], v[u][TM + j], s[u][TM + j], v[u][i], s[u][i]);
-        }
-        for (; t < steps; t += WAVES) {
-            u32x4 v[N];
-            uint32_t s[N];
-            const int valid = (int)a.c - (t * 128 + g * MX4_BLOCK);
-#pragma unroll
-            for (int k = 0; k < N; ++k) {
-                v[k] = valid > 0 ? *reinterpret_cast<const u32x4 *>(codes[k] + t * 64) : u32x4{};
-                s[k] = valid > 0 ? scales[k][t * 4] : 127u;
-                if (k < TM) v[k] = first_codes(v[k], valid);
+                    for (int j = 0; j < TN; ++j)
+                        mma_mx4(acc[i][j], __builtin_bit_cast(u32x4, b[u].v[j]), b[u].s[j], __builtin_bit_cast(u32x4, xs[u].v[i]), xs[u].s[i]);
             }
-#pragma unroll
-            for (int i = 0; i < TM; ++i)
-#pragma unroll
-                for (int j = 0; j < TN; ++j) mma_mx4(acc[i][j], v[TM + j], s[TM + j], v[i], s[i]);
-        }
-        const float first[(TM * TN * 256 + WAVES * WAVE - 1) / (WAVES * WAVE)] = {};
-        few_finish<O, TM, TN, WAVES>(acc, first, rows, w.n0, a.n, s_sums, store);
+        };
+        few_walk<U, WAVES>(now, wave, steps, load_w, load_x, use);
+        few_meet<TM, TN, WAVES>(acc, rows, w.n0, a.n, s_sums, store);
     };
     if (rows <= 16) tile(std::integral_constant<int, 1>{});
     else if (rows <= 32) tile(std::integral_constant<int, 2>{});
@@ -225,9 +237,15 @@ template <class O> hipError_t pick(const GmmArgs &a, const Mx4Args &x, const Mx4
     const int64_t groups = std::min(a.groups, a.rows);
     auto m_tiles = [&](int64_t bm) { return std::max(groups, a.rows / bm + groups / 2); };
     auto tiles = [&](int64_t bm, int64_t bn) { return (double)m_tiles(bm) * (double)((a.n + bn - 1) / bn); };
-    if (groups > 0 && groups * ((a.n + 63) / 64) < 256 && a.rows <= groups * 24) {
-        hipLaunchKernelGGL((k_few_mx4_mx4<O, 1, 8>), few_grid(a, 16), dim3(8 * WAVE), 0, s, a, x, m);
-        return hipGetLastError();
+    // (tiles reach 256 lines of the matrix and the rows of x that they gather by 32-bit offsets)
+    const bool reached = offsets_fit(a.index ? std::max<int64_t>(a.index_rows, 256) : 256, std::max(x.ld_codes, x.ld_scales), 1);
+    if (few(a) || !reached) {
+        const int columns = few_columns(a);
+        auto launch = [&](auto tn) {
+            hipLaunchKernelGGL((k_few_mx4_mx4<O, decltype(tn)::value, 8>), few_grid(a, decltype(tn)::value * 16), dim3(8 * WAVE), 0, s, a, x, m);
+            return hipGetLastError();
+        };
+        return columns == 4 ? launch(std::integral_constant<int, 4>{}) : columns == 2 ? launch(std::integral_constant<int, 2>{}) : launch(std::integral_constant<int, 1>{});
     }
     if constexpr (sizeof(O) == 2)   // (results of 32 bits do not fit the operands' place in LDS)
         if (tiles(128, 128) >= 512 && launches<GM_ROWS>(a, 256, 256, 512)) return launch_tile<O, 256, 256, 2, 4, 2>(a, x, m, s);

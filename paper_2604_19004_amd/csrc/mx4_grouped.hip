@@ -52,25 +52,29 @@ __global__ void __launch_bounds__(WAVES_M * WAVES_N * WAVE, 2) k_gmm_mx4(GmmArgs
     const int wm = (wave / WAVES_N) * WM, wn = (wave % WAVES_N) * WN;
     const int depth = (int)a.c, steps = (depth + STEP_C - 1) / STEP_C;
 
-    Feed<bf16_t, TL, false, true> feed;
-    int64_t row[ASYNC ? 1 : TL::LOADS];   // elements to the line's row
-    if constexpr (ASYNC) {
-        const int64_t first = a.index ? 0 : w.m0;
-        feed.lines(tid, static_cast<const bf16_t *>(a.l) + first * a.ldl, a.ldl, [&](int line) { return tile_row(a, w, line) - first; });
-    } else {
+    // Offsets of the thread's pieces of x from `x_memory` (ASYNC, in bytes), or its lines' rows (elements).
+    const int64_t first = a.index ? 0 : w.m0;
+    const Memory x_memory = memory_at(static_cast<const T *>(a.l) + first * a.ldl);
+    uint32_t off[ASYNC ? TL::LOADS : 1];
+    int64_t row[ASYNC ? 1 : TL::LOADS];
 #pragma unroll
-        for (int i = 0; i < TL::LOADS; ++i) row[i] = tile_row(a, w, TL::line_of(tid, i)) * a.ldl;
+    for (int i = 0; i < TL::LOADS; ++i) {
+        if constexpr (ASYNC) off[i] = (uint32_t)(((tile_row(a, w, TL::line_of(tid, i)) - first) * a.ldl + TL::piece_of(tid, i) * 8) * 2);
+        else row[i] = tile_row(a, w, TL::line_of(tid, i)) * a.ldl;
     }
+    // The thread's line (a row of the matrix, or one c) and its part of it; what comes of columns behind the end is not stored.
     const int line = tid / A_LINE, part = tid % A_LINE;
     const uint8_t *codes = m.codes + w.group * m.stride_codes, *scales = m.scales + w.group * m.stride_scales;
+    if constexpr (!RCOL) codes += w.n0 * m.ld_codes, scales += w.n0 * m.ld_scales;
+    uint32_t code_off, scale_off;
     if constexpr (RCOL) {
-        const int block = min((w.n0 + part * E) / MX4_BLOCK, m.blocks - 1);   // (what comes of columns behind the end is not stored)
-        codes += block * 16 + part * E % MX4_BLOCK / 2;
-        scales += block;
+        const int block = min((w.n0 + part * E) / MX4_BLOCK, m.blocks - 1);
+        code_off = (uint32_t)(line * (int)m.ld_codes + block * 16 + part * E % MX4_BLOCK / 2);
+        scale_off = (uint32_t)(line * (int)m.ld_scales + block);
     } else {
-        const int64_t n = min(w.n0 + line, (int)a.n - 1);
-        codes += n * m.ld_codes + part * (E / 2);
-        scales += n * m.ld_scales;
+        const int n = min(line, (int)a.n - 1 - w.n0);
+        code_off = (uint32_t)n * (uint32_t)m.ld_codes + part * (E / 2);
+        scale_off = (uint32_t)n * (uint32_t)m.ld_scales + part * E / MX4_BLOCK;
     }
 
     struct Raw { uint4 v[sizeof(T) / 2]; };
@@ -83,32 +87,22 @@ __global__ void __launch_bounds__(WAVES_M * WAVES_N * WAVE, 2) k_gmm_mx4(GmmArgs
     auto fetch = [&](int t_) {
         const int t = at(t_), c0 = t * STEP_C, left = min(STEP_C, depth - c0);
         const bool there = RCOL ? line < left : c0 + part * E < m.blocks * MX4_BLOCK;
-        const uint8_t *from = RCOL ? codes + (int64_t)(there ? c0 + line : 0) * m.ld_codes : codes + (there ? c0 / 2 : 0);
-        if constexpr (!RCOL) from = there ? from : codes - part * (E / 2);
+        const Memory code_memory = memory_at(RCOL ? codes + (int64_t)c0 * m.ld_codes : codes), scale_memory = memory_at(RCOL ? scales + (int64_t)c0 * m.ld_scales : scales);
+        const uint32_t code_at = there ? code_off : NOWHERE, scale_at = there ? scale_off : NOWHERE;   // (zeros: a code of 0 is 0 at any scale but NaN)
         if constexpr (WORDS == 4) {
-            const uint4 v = *reinterpret_cast<const uint4 *>(from);
-            kept_codes[0] = v.x, kept_codes[1] = v.y, kept_codes[2] = v.z, kept_codes[3] = v.w;
-        } else {
-            const uint2 v = *reinterpret_cast<const uint2 *>(from);
-            kept_codes[0] = v.x, kept_codes[1] = v.y;
-        }
-        kept_scale = RCOL ? scales[(int64_t)(there ? c0 + line : 0) * m.ld_scales] : scales[there ? (c0 + part * E) / MX4_BLOCK : 0];
-        if (!there) {
+            const u32x4 v = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(code_memory, code_at, RCOL ? 0 : c0 / 2, 0));
 #pragma unroll
-            for (int j = 0; j < WORDS; ++j) kept_codes[j] = 0;
-            kept_scale = 127;
+            for (int j = 0; j < 4; ++j) kept_codes[j] = v[j];
+        } else {
+            const auto v = __builtin_amdgcn_raw_buffer_load_b64(code_memory, code_at, RCOL ? 0 : c0 / 2, 0);
+            kept_codes[0] = v[0], kept_codes[1] = v[1];
         }
+        kept_scale = __builtin_amdgcn_raw_buffer_load_b8(scale_memory, scale_at, RCOL ? 0 : c0 / MX4_BLOCK, 0);
         if constexpr (ASYNC) {
             char *to = lds + (t_ & 1) * BUFFER + wave * (WAVE * 16);
-            if (left == STEP_C) {
-                const char *base = feed.step(t);
 #pragma unroll
-                for (int i = 0; i < TL::LOADS; ++i) load_to_lds(base + feed.off[i], to + i * THREADS * 16);
-            } else {
-#pragma unroll
-                for (int i = 0; i < TL::LOADS; ++i)
-                    load_to_lds(either(feed.valid(tid, i, left) > 0, feed.step(t) + feed.off[i], &g_zero_piece), to + i * THREADS * 16);
-            }
+            for (int i = 0; i < TL::LOADS; ++i)
+                memory_to_lds<16>(x_memory, TL::piece_of(tid, i) * 8 < left ? off[i] : NOWHERE, (uint32_t)c0 * 2, to + i * THREADS * 16);
         } else {
             const T *x = static_cast<const T *>(a.l) + c0;
 #pragma unroll
@@ -203,86 +197,97 @@ __global__ void __launch_bounds__(WAVES_M * WAVES_N * WAVE, 2) k_gmm_mx4(GmmArgs
     store_tile<T, BM, BN, WAVES_M, WAVES_N, !RCOL, sizeof(lds)>(a, w, acc, lds);
 }
 
-// Few rows: the matrix is read once, straight into registers, each wave every WAVES-th 128 numbers of its lines, a block a lane (so a lane's 32 numbers
-// of c are those of its block, in four matrix instructions; x is read to match).
+// Few rows: the matrix is read once, straight into registers.  A lane's 32 numbers of c are those of its block, in four matrix instructions; x is read
+// to match.
 template <class T, int TN, int WAVES>
 __global__ void __launch_bounds__(WAVES * WAVE, 2) k_few_mx4(GmmArgs a, Mx4Args m)
 {
     constexpr int PARTS = PARTS_OF<T>;
-    __shared__ __align__(16) float s_sums[WAVES * 64 * (TN * 16 + 4)];
-    __shared__ int64_t s_row[64];
+    __shared__ __align__(16) float s_sums[few_lds(TN, WAVES)];
+    __shared__ int64_t s_row[FEW_ROWS];
     RowsTile w;
-    int rows;
-    if (!few_rows_tile<T, TN * 16>(a, w, rows, s_row)) return;
-    const int lane = lane_id(), r = lane % 16, g = lane / 16, wave = threadIdx.x / WAVE;
+    if (!few_rows_tile<T, TN * 16>(a, w)) return;
+    const int lane = lane_id(), r = lane % 16, g = lane / 16, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE);
     const uint8_t *codes[TN], *scales[TN];
 #pragma unroll
     for (int j = 0; j < TN; ++j) {
         const int64_t n = min(w.n0 + j * 16 + r, (int)a.n - 1);
-        codes[j] = m.codes + w.group * m.stride_codes + n * m.ld_codes + g * 16;
-        scales[j] = m.scales + w.group * m.stride_scales + n * m.ld_scales + g;
+        codes[j] = m.codes + w.group * m.stride_codes + n * m.ld_codes;
+        scales[j] = m.scales + w.group * m.stride_scales + n * m.ld_scales;
     }
+    const int whole = (int)(a.c / 128), steps = (int)((a.c + 127) / 128), rows = min(FEW_ROWS, w.hi - w.m0);
+    auto load_w = [&](Mx4Blocks<TN> &to, int t) { to.load(codes, scales, min(t * 4 + g, m.blocks - 1)); };
     T *out = static_cast<T *>(a.out);
     auto store = [&](int row, int64_t col, float v) { out[(int64_t)(w.m0 + row) * a.ldo + col] = (T)(s_row[row] < 0 ? 0.0f : v); };
     auto tile = [&](auto tm) {
-        constexpr int TM = decltype(tm)::value, UNROLL = TM == 1 ? 2 : 1;
+        constexpr int TM = decltype(tm)::value, U = TM == 1 && sizeof(T) == 2 ? (TN <= 2 ? 4 : 2) : 1;
+        Mx4Blocks<TN> now[U];
+        if (wave < steps) {
+#pragma unroll
+            for (int u = 0; u < U; ++u) load_w(now[u], wave + u * WAVES);
+        }
+        if ((int)threadIdx.x < rows) {
+            const int64_t row = a.index ? a.index[w.m0 + threadIdx.x] : w.m0 + threadIdx.x;
+            s_row[threadIdx.x] = (uint64_t)row < (uint64_t)a.index_rows ? row : -1;
+        }
+        __syncthreads();
         const T *x[TM];
 #pragma unroll
         for (int i = 0; i < TM; ++i) x[i] = static_cast<const T *>(a.l) + max(s_row[min(i * 16 + r, rows - 1)], (int64_t)0) * a.ldl + g * MX4_BLOCK;
         f32x4 acc[TM][TN] = {};
-        const int whole = (int)(a.c / 128), steps = (int)((a.c + 127) / 128);
-        auto step = [&](const uint4 (&v)[TN], const uint32_t (&s)[TN], int t, bool all) {
+        struct Eight { uint4 v[sizeof(T) / 2]; };
+        Eight xs[U][TM][4];
+        auto load_x = [&](int t0, bool end) {
 #pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                const int valid = all ? 8 : (int)a.c - (t * 128 + g * MX4_BLOCK + q * 8);
-                Frag<bf16_t> fw[TN];
+            for (int u = 0; u < U; ++u) {
+                const int t = t0 + u * WAVES;
+                if (!end || t < whole) {
 #pragma unroll
-                for (int j = 0; j < TN; ++j) {
-                    const uint32_t word = q == 0 ? v[j].x : q == 1 ? v[j].y : q == 2 ? v[j].z : v[j].w;
-                    bf16_t e[8];
-                    mx4_widen<bf16_t>(mx4_first(word, valid), mx4_scale(s[j]), e);
-                    fw[j] = bf16x8{e[0], e[1], e[2], e[3], e[4], e[5], e[6], e[7]};
-                }
+                    for (int i = 0; i < TM; ++i)
 #pragma unroll
-                for (int i = 0; i < TM; ++i) {
-                    T e[8];
-                    bf16x8 p[PARTS];
-                    load8<T, false>(x[i] + t * 128 + q * 8, min(valid, 8), e);
-                    split<T>(e, p);
+                        for (int q = 0; q < 4; ++q)
 #pragma unroll
-                    for (int k = PARTS - 1; k >= 0; --k)
+                            for (int p = 0; p < (int)sizeof(T) / 2; ++p) xs[u][i][q].v[p] = load_any(reinterpret_cast<const char *>(x[i] + t * 128 + q * 8 + p * PIECE<T>));
+                } else {
+                    const int64_t left = a.c - ((int64_t)t * 128 + g * MX4_BLOCK);
 #pragma unroll
-                        for (int j = 0; j < TN; ++j) mma_part(acc[i][j], fw[j], p[k], 0);
+                    for (int i = 0; i < TM; ++i)
+#pragma unroll
+                        for (int q = 0; q < 4; ++q)
+#pragma unroll
+                            for (int p = 0; p < (int)sizeof(T) / 2; ++p)
+                                xs[u][i][q].v[p] = load_piece(x[i] + (int64_t)t * 128 + q * 8 + p * PIECE<T>, (int)max(min(left - q * 8 - p * PIECE<T>, (int64_t)8), (int64_t)0));
                 }
             }
         };
-        int t = wave;
-        for (; t + (UNROLL - 1) * WAVES < whole; t += UNROLL * WAVES) {
-            uint4 v[UNROLL][TN];
-            uint32_t s[UNROLL][TN];
+        auto use = [&](Mx4Blocks<TN> (&b)[U], int t0, bool end) {
 #pragma unroll
-            for (int u = 0; u < UNROLL; ++u)
+            for (int u = 0; u < U; ++u) {
+                const int t = t0 + u * WAVES;
+                if (end && t >= whole) b[u].end((int)max(min(a.c - ((int64_t)t * 128 + g * MX4_BLOCK), (int64_t)32), (int64_t)0));
 #pragma unroll
-                for (int j = 0; j < TN; ++j) {
-                    v[u][j] = *reinterpret_cast<const uint4 *>(codes[j] + (t + u * WAVES) * 64);
-                    s[u][j] = scales[j][(t + u * WAVES) * 4];
+                for (int q = 0; q < 4; ++q) {
+                    Frag<bf16_t> fw[TN];
+#pragma unroll
+                    for (int j = 0; j < TN; ++j) {
+                        bf16_t e[8];
+                        mx4_widen<bf16_t>(q == 0 ? b[u].v[j].x : q == 1 ? b[u].v[j].y : q == 2 ? b[u].v[j].z : b[u].v[j].w, mx4_scale(b[u].s[j]), e);
+                        fw[j] = bf16x8{e[0], e[1], e[2], e[3], e[4], e[5], e[6], e[7]};
+                    }
+#pragma unroll
+                    for (int i = 0; i < TM; ++i) {
+                        bf16x8 p[PARTS];
+                        split<T>(__builtin_bit_cast(decltype(Vec<T, 8>{}), xs[u][i][q]).e, p);
+#pragma unroll
+                        for (int k = PARTS - 1; k >= 0; --k)
+#pragma unroll
+                            for (int j = 0; j < TN; ++j) mma_part(acc[i][j], fw[j], p[k], 0);
+                    }
                 }
-#pragma unroll
-            for (int u = 0; u < UNROLL; ++u) step(v[u], s[u], t + u * WAVES, true);
-        }
-        for (; t < steps; t += WAVES) {
-            uint4 v[TN];
-            uint32_t s[TN];
-            const bool there = t * 4 + g < m.blocks;
-#pragma unroll
-            for (int j = 0; j < TN; ++j) {
-                v[j] = there ? *reinterpret_cast<const uint4 *>(codes[j] + t * 64) : make_uint4(0, 0, 0, 0);
-                s[j] = there ? scales[j][t * 4] : 127u;
             }
-            step(v, s, t, false);
-        }
-        const float first[(TM * TN * 256 + WAVES * WAVE - 1) / (WAVES * WAVE)] = {};
-        few_finish<T, TM, TN, WAVES>(acc, first, rows, w.n0, a.n, s_sums, store);
+        };
+        few_walk<U, WAVES>(now, wave, steps, load_w, load_x, use);
+        few_meet<TM, TN, WAVES>(acc, rows, w.n0, a.n, s_sums, store);
     };
     if (rows <= 16) tile(std::integral_constant<int, 1>{});
     else if (rows <= 32) tile(std::integral_constant<int, 2>{});
@@ -304,9 +309,13 @@ template <class T, bool RCOL> hipError_t pick(const GmmArgs &a, const Mx4Args &m
     auto m_tiles = [&](int64_t bm) { return std::max(groups, a.rows / bm + groups / 2); };
     auto tiles = [&](int64_t bm, int64_t bn) { return (double)m_tiles(bm) * (double)((a.n + bn - 1) / bn); };
     if constexpr (!RCOL) {
-        if (groups > 0 && groups * ((a.n + 63) / 64) < 256 && a.rows <= groups * 24) {
-            hipLaunchKernelGGL((k_few_mx4<T, 1, 8>), few_grid(a, 16), dim3(8 * WAVE), 0, s, a, m);
-            return hipGetLastError();
+        if (few(a)) {
+            const int columns = few_columns(a);
+            auto launch = [&](auto tn) {
+                hipLaunchKernelGGL((k_few_mx4<T, decltype(tn)::value, 8>), few_grid(a, decltype(tn)::value * 16), dim3(8 * WAVE), 0, s, a, m);
+                return hipGetLastError();
+            };
+            return columns == 4 ? launch(std::integral_constant<int, 4>{}) : columns == 2 ? launch(std::integral_constant<int, 2>{}) : launch(std::integral_constant<int, 1>{});
         }
     }
     if constexpr (std::is_same<T, bf16_t>::value) {
@@ -335,6 +344,7 @@ hipError_t launch_grouped_mx4(const ocean_groups &g, int dtype, const void *x, i
     if (g.x_rows == 0 || inner == 0) a.c = 0, a.index_rows = 0, a.index = nullptr;
     const Mx4Args m = mx4_args(w);
     // (the rows of a tile lie within 256 lines, gathered ones anywhere in x)
+    // (whole pieces: a piece of x lies before its row's end or behind it)
     const bool straight = dtype == OCEAN_BF16 && pieces_aligned(x, ldx, 0, 2) && inner % 8 == 0 && offsets_fit(g.row_index ? std::max<int64_t>(g.x_rows, 256) : 256, ldx, 2);
     return with_type(dtype, [&](auto t) {
         using T = decltype(t);

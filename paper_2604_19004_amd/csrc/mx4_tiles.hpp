@@ -16,14 +16,18 @@ struct Mx4Args {
 };
 inline Mx4Args mx4_args(const ocean_mx4 &w) { return Mx4Args{w.codes, w.scales, w.ld_codes, w.stride_codes, w.ld_scales, w.stride_scales, (int)mx4_blocks(w.inner)}; }
 
-// `there ? a : b` of addresses by masks, in which the compiler cannot see a branch.  (It made one of the plain choice where a workgroup's first step is the end of
-// the lines, and there used a piece's offset, in lanes whose piece exists, from a register that it had only written in the others.)
-__device__ __forceinline__ const void *either(bool there, const void *a, const void *b)
+// Memory from `base` on, for loads of 32-bit offsets: an offset of NOWHERE reads zeros (the hardware's range check), so that the end of the lines takes
+// no branch.  (With a choice of addresses there, the compiler made a branch of it and, where a workgroup's first step was the end, used a piece's
+// offset from a register that it had written in the other lanes only.)
+typedef __amdgpu_buffer_rsrc_t Memory;
+constexpr uint32_t MEMORY_BYTES = 0xfffff000u, NOWHERE = 0xfffffff0u;
+__device__ __forceinline__ Memory memory_at(const void *base) { return __builtin_amdgcn_make_buffer_rsrc(const_cast<void *>(base), 0, MEMORY_BYTES, 0x00027000); }
+// BYTES bytes a lane straight to LDS, where the wave's lie side by side from `lds` on.
+template <int BYTES> __device__ __forceinline__ void memory_to_lds(Memory m, uint32_t offset, uint32_t step, char *lds)
 {
-    uint32_t mask = there ? ~0u : 0u;
-    asm volatile("" : "+v"(mask));
-    const uint64_t m = (uint64_t)mask << 32 | mask, x = reinterpret_cast<uint64_t>(a), y = reinterpret_cast<uint64_t>(b);
-    return reinterpret_cast<const void *>(y ^ ((x ^ y) & m));
+    auto *to = (__attribute__((address_space(3))) void *)lds;
+    if constexpr (BYTES == 16) __builtin_amdgcn_raw_ptr_buffer_load_lds(m, to, 16, offset, step, 0, 0);
+    else __builtin_amdgcn_raw_ptr_buffer_load_lds(m, to, 4, offset, step, 0, 0);
 }
 
 // Which tile a workgroup has, of those that groups of rows make (mt: the most there may be); false: none, and it has cleared its share of the
@@ -107,28 +111,102 @@ __device__ __forceinline__ void store_tile(const GmmArgs &a, const RowsTile &w, 
     }
 }
 
-// The tile of few rows that workgroup (x, y) of k_few... has, as in k_few; the rows' numbers in s_row (-1: zeros).
-template <class O, int COLS> __device__ __forceinline__ bool few_rows_tile(const GmmArgs &a, RowsTile &w, int &rows, int64_t *s_row)
+// Few rows: workgroup (x, y) has columns 16 TN x .. of the y-th tile of up to 64 rows of a group, as in k_few.  Its waves take every WAVES-th 128 numbers
+// of c, a block of 32 of a line a lane, and their sums meet in LDS.
+constexpr int FEW_ROWS = 64;
+template <class O, int COLS> __device__ __forceinline__ bool few_rows_tile(const GmmArgs &a, RowsTile &w)
 {
-    constexpr int FEW_ROWS = 64;
     int tiles = 0;
     w.n0 = (int)blockIdx.x * COLS;
     auto item_of = [&](int n) { tiles = n; return (int)blockIdx.y; };
-    if (!find_tile(a, FEW_ROWS, item_of, w.group, w.m0, w.hi)) {
-        clear_outside<O>(a, w.n0, min((int64_t)COLS, a.n - w.n0), (int)blockIdx.y - tiles, (int)gridDim.y - tiles);
-        return false;
-    }
-    rows = min(FEW_ROWS, w.hi - w.m0);
-    if ((int)threadIdx.x < rows) {
-        const int64_t row = a.index ? a.index[w.m0 + threadIdx.x] : w.m0 + threadIdx.x;
-        s_row[threadIdx.x] = (uint64_t)row < (uint64_t)a.index_rows ? row : -1;
-    }
-    __syncthreads();
-    return true;
+    if (find_tile(a, FEW_ROWS, item_of, w.group, w.m0, w.hi)) return true;
+    clear_outside<O>(a, w.n0, min((int64_t)COLS, a.n - w.n0), (int)blockIdx.y - tiles, (int)gridDim.y - tiles);
+    return false;
 }
+
+// A block of each of TN lines of a matrix, and its scale.
+template <int TN> struct Mx4Blocks {
+    uint4 v[TN];
+    uint32_t s[TN];
+    __device__ __forceinline__ void load(const uint8_t *const (&codes)[TN], const uint8_t *const (&scales)[TN], int block)
+    {
+#pragma unroll
+        for (int j = 0; j < TN; ++j) {
+            v[j] = *reinterpret_cast<const uint4 *>(codes[j] + (int64_t)block * 16);
+            s[j] = scales[j][block];
+        }
+    }
+    // only the first `valid` numbers
+    __device__ __forceinline__ void end(int valid)
+    {
+#pragma unroll
+        for (int j = 0; j < TN; ++j) {
+            v[j] = make_uint4(mx4_first(v[j].x, valid), mx4_first(v[j].y, valid - 8), mx4_first(v[j].z, valid - 16), mx4_first(v[j].w, valid - 24));
+            s[j] = valid > 0 ? s[j] : 127u;
+        }
+    }
+};
+
+// The walk of a wave over its steps of 128 numbers, U at a time, the matrix's blocks of the next ones under way meanwhile: first(t) loads those of step t
+// into `next` ahead of everything else, x(u, t) what they meet, use(u, t, end) multiplies; `end`: the step may reach behind the lines' end, and is then
+// told what is there by its blocks.
+template <int U, int WAVES, class Blocks, class LoadW, class LoadX, class Use>
+__device__ __forceinline__ void few_walk(Blocks (&now)[U], int wave, int steps, LoadW load_w, LoadX load_x, Use use)
+{
+    int t = wave;
+    for (; t + U * WAVES < steps; t += U * WAVES) {   // (all of these lie before the end)
+        Blocks next[U];
+        load_x(t, false);
+#pragma unroll
+        for (int u = 0; u < U; ++u) load_w(next[u], t + (U + u) * WAVES);
+        use(now, t, false);
+#pragma unroll
+        for (int u = 0; u < U; ++u) now[u] = next[u];
+    }
+    if (t < steps) {
+        load_x(t, true);
+        use(now, t, true);
+    }
+}
+
+// The waves' sums meet, 16 rows at a time; store(row, column, sum) is called once for each of the tile's.
+template <int TM, int TN, int WAVES, class Store>
+__device__ __forceinline__ void few_meet(const f32x4 (&acc)[TM][TN], int rows, int64_t n0, int64_t n, float *lds, Store store)
+{
+    constexpr int COLS = TN * 16, LD = COLS + 4, THREADS = WAVES * WAVE;
+    const int lane = lane_id(), r = lane % 16, g = lane / 16, wave = threadIdx.x / WAVE;
+#pragma unroll
+    for (int i = 0; i < TM; ++i) {
+        if (i > 0) __syncthreads();
+#pragma unroll
+        for (int j = 0; j < TN; ++j) *reinterpret_cast<f32x4 *>(lds + (wave * 16 + r) * LD + j * 16 + g * 4) = acc[i][j];
+        __syncthreads();
+        for (int k = threadIdx.x; k < 16 * COLS; k += THREADS) {
+            const int row = k / COLS, col = k % COLS;
+            if (i * 16 + row >= rows || n0 + col >= n) continue;
+            float v = 0.0f;
+#pragma unroll
+            for (int s = 0; s < WAVES; ++s) v += lds[(s * 16 + row) * LD + col];
+            store(i * 16 + row, n0 + col, v);
+        }
+    }
+}
+constexpr int few_lds(int tn, int waves) { return waves * 16 * (tn * 16 + 4); }   // floats
 inline dim3 few_grid(const GmmArgs &a, int cols)
 {
-    return dim3((uint32_t)((a.n + cols - 1) / cols), (uint32_t)(a.rows / 64 + std::min(a.groups, a.rows)) + 1);
+    return dim3((uint32_t)((a.n + cols - 1) / cols), (uint32_t)(a.rows / FEW_ROWS + std::min(a.groups, a.rows)) + 1);
+}
+
+// Columns of a workgroup, in sixteens.
+inline int few_columns(const GmmArgs &a)
+{
+    const int64_t tiles = std::min(a.groups, a.rows);
+    return tiles * ((a.n + 63) / 64) >= 512 ? 4 : tiles * ((a.n + 31) / 32) >= 512 ? 2 : 1;
+}
+inline bool few(const GmmArgs &a)
+{
+    const int64_t groups = std::min(a.groups, a.rows);
+    return groups > 0 && a.rows <= groups * 48 && a.n <= (1 << 20) && a.rows / FEW_ROWS + groups < 65535;
 }
 
 }  // namespace
