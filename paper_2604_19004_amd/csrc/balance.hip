@@ -8,7 +8,8 @@ namespace ocean {
 
 namespace {
 
-constexpr int TPB = 256, FINISH_TPB = 1024;
+constexpr int TPB = 256, SUM_TPB = 1024, FINISH_TPB = 1024;
+constexpr int64_t AT_ONCE = 1536;     // workgroups of the gradient that run together, six a compute unit
 constexpr int64_t MAX_BLOCKS = 256;   // workgroups of the first pass, each of which leaves a sum per expert
 
 // Sums of a workgroup's rows, per expert, of logsumexp^2, and its rows that have an open logit.
@@ -33,52 +34,101 @@ inline BalanceSpace balance_space(void *at, int64_t experts, size_t *bytes)
     return w;
 }
 
-// A row's softmax relative to its largest logit: e[i] = exp(logit - top) (0: masked), their sum (0: the row has no open logit), and its
-// logsumexp = top + log(sum).
-template <class T, int G, int NV>
-__device__ __forceinline__ float row_softmax(const T *row, int experts, bool there, uint32_t (&key)[NV], float (&e)[NV], float &top)
+// The rows of a turn of the workgroup, from row t0 on: what lies behind the last row reads as 0 and is not written.
+template <class T> __device__ __forceinline__ Memory rows_from(const T *p, int64_t ld, int64_t t0, int64_t tokens, int experts)
+{
+    const int64_t bytes = t0 < tokens ? ((tokens - 1 - t0) * ld + experts) * (int64_t)sizeof(T) : 0;
+    return memory_at(p + t0 * ld, (uint32_t)min(bytes, (int64_t)MEMORY_BYTES));
+}
+// Offsets of a lane's columns of row `row` of a turn.
+template <class T, int G, int NV> __device__ __forceinline__ void offsets_of(uint32_t (&at)[NV], int row, int64_t ld, int experts)
 {
     const int sub = lane_id() % G;
-    uint32_t first = 0;
+#pragma unroll
+    for (int i = 0; i < NV; ++i) at[i] = i * G + sub < experts ? (uint32_t)((row * ld + i * G + sub) * (int64_t)sizeof(T)) : NOWHERE;
+}
+template <class T> using Bits = std::conditional_t<sizeof(T) == 4, uint32_t, uint16_t>;
+template <class T> __device__ __forceinline__ T load_one(Memory m, uint32_t at)
+{
+    if constexpr (sizeof(T) == 4) return __builtin_bit_cast(T, (uint32_t)__builtin_amdgcn_raw_buffer_load_b32(m, at, 0, 0));
+    else return __builtin_bit_cast(T, (uint16_t)__builtin_amdgcn_raw_buffer_load_b16(m, at, 0, 0));
+}
+template <class T> __device__ __forceinline__ void store_one(T v, Memory m, uint32_t at)
+{
+    if constexpr (sizeof(T) == 4) __builtin_amdgcn_raw_buffer_store_b32(__builtin_bit_cast(uint32_t, v), m, at, 0, 0);
+    else __builtin_amdgcn_raw_buffer_store_b16(__builtin_bit_cast(uint16_t, v), m, at, 0, 0);
+}
+
+// e^d for d <= 0: 2^(d log2 e) with what the product's rounding left, off by two roundings or so; below 2^-126 it is 0.
+__device__ __forceinline__ float exp_of(float d)
+{
+    constexpr float LOG2E = 1.44269504f, REST = (float)(1.4426950408889634074 - (double)LOG2E), LN2 = 0.693147181f;
+    const float t = d * LOG2E, left = fmaf(d, REST, fmaf(d, LOG2E, -t)), e = __builtin_amdgcn_exp2f(t);
+    return d > -1e30f ? fmaf(e, left * LN2, e) : 0.0f;   // (-inf, where t - t is NaN)
+}
+
+template <int G> __device__ __forceinline__ float lanes_top(float v)
+{
+    if constexpr (G == 16)
+        return __uint_as_float(row16(__float_as_uint(v), [](uint32_t x, uint32_t y) { return __float_as_uint(fmaxf(__uint_as_float(x), __uint_as_float(y))); }));
+    else return key_value(lanes_max<G>(order_key(v)));
+}
+
+// A row's softmax relative to its largest logit: e[i] = exp(x[i] - top), their sum (0: the row has no open logit).  x: the logits, -inf where they are masked or
+// not there.
+template <class T, int G, int NV>
+__device__ __forceinline__ float row_softmax(const T (&row)[NV], const uint32_t (&at)[NV], bool there, float (&x)[NV], float (&e)[NV], float &top)
+{
+    top = -INFINITY;
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-        const int c = i * G + sub;
-        key[i] = there && c < experts ? logit_key(row[c]) : 0u;
+        const float v = (float)row[i];
+        x[i] = v > TypeTraits<T>::lowest && at[i] != NOWHERE ? fminf(v, -TypeTraits<T>::lowest) : -INFINITY;   // (NaN is not)
+        top = fmaxf(top, x[i]);
     }
-#pragma unroll
-    for (int i = 0; i < NV; ++i) first = max(first, key[i]);
-    first = lanes_max<G>(first);
-    top = first ? key_value(first) : 0.0f;
+    top = lanes_top<G>(there ? top : -INFINITY);
+    if (!(top > -INFINITY)) top = 0.0f;
     float sum = 0.0f;
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-        e[i] = key[i] ? expf(key_value(key[i]) - top) : 0.0f;
+        e[i] = exp_of(x[i] - top);
         sum += e[i];
     }
-    return lanes_sum<G>(sum);
+    sum = lanes_sum<G>(sum);
+    return there ? sum : 0.0f;
 }
 
 // G lanes share a row and keep their columns' sums over all rows that they see; those of a workgroup meet in LDS in a fixed order.
 template <class T, int G, int NV>
-__global__ void __launch_bounds__(TPB) k_balance(const T *logits, int64_t ld, int64_t tokens, int experts, BalanceSpace w)
+__global__ void __launch_bounds__(SUM_TPB) k_balance(const T *logits, int64_t ld, int64_t tokens, int experts, BalanceSpace w)
 {
-    constexpr int GROUPS = TPB / G;
+    constexpr int GROUPS = SUM_TPB / G;
     __shared__ float s_prob[GROUPS][NV * G];
     __shared__ float s_z[GROUPS];
     __shared__ int s_rows[GROUPS];
     const int sub = lane_id() % G, group = threadIdx.x / G;
     float prob[NV] = {}, z = 0.0f;
     int rows = 0;
+    uint32_t at[NV];
+    offsets_of<T, G, NV>(at, group, ld, experts);
+    T now[NV], next[NV];
+    auto load = [&](T (&to)[NV], int64_t t0) {
+        const Memory m = rows_from(logits, ld, t0, tokens, experts);
+#pragma unroll
+        for (int i = 0; i < NV; ++i) to[i] = load_one<T>(m, at[i]);
+    };
+    load(now, (int64_t)blockIdx.x * GROUPS);
     for (int64_t t0 = (int64_t)blockIdx.x * GROUPS; t0 < tokens; t0 += (int64_t)gridDim.x * GROUPS) {
-        const int64_t t = t0 + group;
-        uint32_t key[NV];
-        float e[NV], top;
-        const float sum = row_softmax<T, G, NV>(logits + min(t, tokens - 1) * ld, experts, t < tokens, key, e, top);
+        load(next, t0 + (int64_t)gridDim.x * GROUPS);   // (the next row is on its way)
+        float x[NV], e[NV], top;
+        const float sum = row_softmax<T, G, NV>(now, at, t0 + group < tokens, x, e, top);
         const float scale = sum > 0.0f ? 1.0f / sum : 0.0f, lse = sum > 0.0f ? top + logf(sum) : 0.0f;
 #pragma unroll
         for (int i = 0; i < NV; ++i) prob[i] += e[i] * scale;
         z += lse * lse;
         rows += sum > 0.0f;
+#pragma unroll
+        for (int i = 0; i < NV; ++i) now[i] = next[i];
     }
 #pragma unroll
     for (int i = 0; i < NV; ++i) s_prob[group][i * G + sub] = prob[i];
@@ -87,55 +137,75 @@ __global__ void __launch_bounds__(TPB) k_balance(const T *logits, int64_t ld, in
         s_rows[group] = rows;
     }
     __syncthreads();
-    for (int c = threadIdx.x; c < experts; c += TPB) {
+    for (int c = threadIdx.x; c < experts; c += SUM_TPB) {
         float v = 0.0f;
+#pragma unroll 16
         for (int i = 0; i < GROUPS; ++i) v += s_prob[i][c];
         w.prob[(int64_t)blockIdx.x * experts + c] = v;
     }
-    if (threadIdx.x == 0) {
+    if (threadIdx.x >= SUM_TPB - WAVE) {   // (the last wave, which has no column unless there are many)
+        const int lane = lane_id();
         float v = 0.0f;
-        int64_t n = 0;
-        for (int i = 0; i < GROUPS; ++i) {
+        uint32_t n = 0;
+        for (int i = lane; i < GROUPS; i += WAVE) {
             v += s_z[i];
-            n += s_rows[i];
+            n += (uint32_t)s_rows[i];   // (a workgroup has fewer than 2^32 rows)
         }
-        w.z[blockIdx.x] = v;
-        w.rows[blockIdx.x] = n;
+        v = wave_sum(v);
+        n = wave_sum_u32(n);
+        if (lane == 0) {
+            w.z[blockIdx.x] = v;
+            w.rows[blockIdx.x] = n;
+        }
     }
 }
 
 __device__ __forceinline__ int64_t entries_of(const int64_t *expert_ptr, int e) { return max(expert_ptr[e + 1] - expert_ptr[e], (int64_t)0); }
+template <class V> __device__ __forceinline__ V wave_total(V v)
+{
+#pragma unroll
+    for (int d = WAVE / 2; d > 0; d >>= 1) v += __shfl_xor(v, d);
+    return v;
+}
 
-// The workgroups' sums together, in 64 bits.
+// The workgroups' sums together, in 64 bits: 1024 / experts threads an expert, each every so many workgroups.  A chain of two trips to memory and three barriers.
 __global__ void __launch_bounds__(FINISH_TPB) k_balance_finish(const int64_t *expert_ptr, int experts, int blocks, BalanceSpace w, ocean_balance out)
 {
-    __shared__ double s_sum[FINISH_TPB];
-    __shared__ double s_f[FINISH_TPB / WAVE];
-    __shared__ int64_t s_n[FINISH_TPB / WAVE];
-    const int tid = threadIdx.x, cols = min(FINISH_TPB, (experts + WAVE - 1) / WAVE * WAVE), parts = FINISH_TPB / cols;
-    const int part = tid / cols, c = tid % cols;
+    constexpr int WAVES = FINISH_TPB / WAVE, DEEP = 32;
+    __shared__ double s_sum[FINISH_TPB], s_z, s_f[WAVES];
+    __shared__ int64_t s_rows, s_n[WAVES];
+    const int tid = threadIdx.x, wave = tid / WAVE, cols = (experts + WAVE - 1) / WAVE * WAVE, parts = FINISH_TPB / cols;
+    const int part = tid / cols, c = tid - part * cols;
+    const int64_t count = tid < experts ? entries_of(expert_ptr, tid) : 0;
     double v = 0.0;
     if (c < experts && part < parts)
-        for (int b = part; b < blocks; b += parts) v += (double)w.prob[(int64_t)b * experts + c];
+        for (int b0 = part; b0 < blocks; b0 += parts * DEEP) {
+            float x[DEEP];
+#pragma unroll
+            for (int i = 0; i < DEEP; ++i) x[i] = w.prob[(int64_t)min(b0 + i * parts, blocks - 1) * experts + c];   // (no branch: all are under way at once)
+#pragma unroll
+            for (int i = 0; i < DEEP; ++i) v += (double)(b0 + i * parts < blocks ? x[i] : 0.0f);
+        }
     s_sum[tid] = v;
-    int64_t rows = 0;
-    double z = 0.0;
-    for (int b = tid; b < blocks; b += FINISH_TPB) {
-        rows += w.rows[b];
-        z += (double)w.z[b];
+    if (wave == WAVES - 1) {
+        int64_t rows = 0;
+        double z = 0.0;
+#pragma unroll
+        for (int i = 0; i < (int)(MAX_BLOCKS / WAVE); ++i) {
+            const int b = i * WAVE + lane_id();
+            rows += b < blocks ? w.rows[b] : 0;
+            z += b < blocks ? (double)w.z[b] : 0.0;
+        }
+        rows = wave_total(rows);
+        z = wave_total(z);
+        if (lane_id() == 0) s_rows = rows, s_z = z;
     }
-    auto all = [&](auto x, auto *lds) {   // sum over the workgroup
-        for (int d = WAVE / 2; d > 0; d >>= 1) x += __shfl_xor(x, d);
-        __syncthreads();
-        if (lane_id() == 0) lds[tid / WAVE] = x;
-        __syncthreads();
-        x = 0;
-        for (int i = 0; i < FINISH_TPB / WAVE; ++i) x += lds[i];
-        return x;
-    };
-    rows = all(rows, s_n);
-    z = all(z, s_f);
-    const int64_t count = tid < experts ? entries_of(expert_ptr, tid) : 0, n = all(count, s_n);
+    const int64_t n_wave = wave_total(count);
+    if (lane_id() == 0) s_n[wave] = n_wave;
+    __syncthreads();
+    int64_t n = 0;
+    for (int i = 0; i < WAVES; ++i) n += s_n[i];
+    const int64_t rows = s_rows;
     double prob = 0.0;
     if (tid < experts) {
         for (int p = 0; p < parts; ++p) prob += s_sum[p * cols + tid];
@@ -143,10 +213,14 @@ __global__ void __launch_bounds__(FINISH_TPB) k_balance_finish(const int64_t *ex
         out.prob[tid] = (float)prob;
         out.counts[tid] = count;
     }
-    const double balance = all(n > 0 ? (double)count / (double)n * prob : 0.0, s_f);
+    const double even = wave_total(n > 0 ? (double)count / (double)n * prob : 0.0);
+    if (lane_id() == 0) s_f[wave] = even;
+    __syncthreads();
     if (tid == 0) {
+        double balance = 0.0;
+        for (int i = 0; i < WAVES; ++i) balance += s_f[i];
         out.loss[0] = (float)(balance * experts);
-        out.loss[1] = rows > 0 ? (float)(z / (double)rows) : 0.0f;
+        out.loss[1] = rows > 0 ? (float)(s_z / (double)rows) : 0.0f;
         out.rows[0] = rows;
     }
 }
@@ -171,12 +245,44 @@ __global__ void __launch_bounds__(TPB) k_balance_backward(ocean_balance b, ocean
     const float per_row = rows > 0 ? 1.0f / (float)rows : 0.0f, even = dloss[0] * per_row * (float)experts, size = 2.0f * dloss[1] * per_row;
 #pragma unroll
     for (int i = 0; i < NV; ++i) share[i] = total > 0.0f ? share[i] / total : 0.0f;
+    uint32_t from[NV], to[NV];
+    offsets_of<T, G, NV>(from, at, ld, experts);
+    offsets_of<T, G, NV>(to, at, ldd, experts);
+    T now[NV], next[NV];
+    auto load = [&](T (&v)[NV], int64_t t0) {
+        const Memory m = rows_from(logits, ld, t0, r.tokens, experts);
+#pragma unroll
+        for (int i = 0; i < NV; ++i) v[i] = load_one<T>(m, from[i]);
+    };
+    // A row's entries are loaded before its softmax is worked out, and where they lie a turn ahead.
+    constexpr int TURNS = WEIGHTS ? OCEAN_ROUTE_MAX_K / G : 1;
+    int64_t lo = 0, hi = 0, lo_next = 0, hi_next = 0;
+    auto place = [&](int64_t t0, int64_t &first, int64_t &last) {
+        const int64_t t = min(t0 + at, r.tokens - 1);
+        first = r.row_ptr[t], last = r.row_ptr[t + 1];
+    };
+    load(now, (int64_t)blockIdx.x * ROWS);
+    if constexpr (WEIGHTS) place((int64_t)blockIdx.x * ROWS, lo, hi);
     for (int64_t t0 = (int64_t)blockIdx.x * ROWS; t0 < r.tokens; t0 += (int64_t)gridDim.x * ROWS) {
         const bool there = t0 + at < r.tokens;
-        const int64_t t = there ? t0 + at : r.tokens - 1;
-        uint32_t key[NV];
-        float e[NV], top;
-        const float sum = row_softmax<T, G, NV>(logits + t * ld, experts, there, key, e, top);
+        int col[TURNS];
+        float weight[TURNS], grad[TURNS];
+        if constexpr (WEIGHTS) {
+            lo = min(max(lo, (int64_t)0), cap);
+            hi = min(max(hi, lo), lo + min(cap - lo, (int64_t)r.k));   // (a row has at most k)
+#pragma unroll
+            for (int j = 0; j < TURNS; ++j) {
+                if (j > 0 && j * G >= r.k) break;   // (the same for all)
+                const int64_t p = lo + j * G + sub;
+                col[j] = p < hi ? r.col_idx[p] : -1;
+                weight[j] = p < hi ? r.val[p] : 0.0f;
+                grad[j] = p < hi ? dval[p] : 0.0f;
+            }
+            place(t0 + (int64_t)gridDim.x * ROWS, lo_next, hi_next);
+        }
+        load(next, t0 + (int64_t)gridDim.x * ROWS);
+        float x[NV], e[NV], top;
+        const float sum = row_softmax<T, G, NV>(now, from, there, x, e, top);
         const float scale = sum > 0.0f ? 1.0f / sum : 0.0f, lse = sum > 0.0f ? top + logf(sum) : 0.0f;
         float met = 0.0f;
 #pragma unroll
@@ -191,33 +297,31 @@ __global__ void __launch_bounds__(TPB) k_balance_backward(ocean_balance b, ocean
 #pragma unroll
             for (int i = 0; i < NV; ++i) g[i * G + sub] = 0.0f;
             wave_sync();
-            const int64_t lo = min(max(r.row_ptr[t], (int64_t)0), cap), hi = min(max(r.row_ptr[t + 1], lo), lo + min(cap - lo, (int64_t)OCEAN_ROUTE_MAX_K));
-            constexpr int TURNS = OCEAN_ROUTE_MAX_K / G;
-            int col[TURNS];
-            float weight[TURNS], grad[TURNS];
 #pragma unroll
             for (int j = 0; j < TURNS; ++j) {
-                const int64_t p = lo + j * G + sub;
-                col[j] = p < hi ? r.col_idx[p] : -1;
-                weight[j] = p < hi ? r.val[p] : 0.0f;
-                grad[j] = p < hi ? dval[p] : 0.0f;
+                if (j > 0 && j * G >= r.k) break;
                 mean += weight[j] * grad[j];
             }
             mean = lanes_sum<G>(mean);
 #pragma unroll
-            for (int j = 0; j < TURNS; ++j)
+            for (int j = 0; j < TURNS; ++j) {
+                if (j > 0 && j * G >= r.k) break;
                 if ((unsigned)col[j] < (unsigned)experts) g[col[j]] = normalize ? weight[j] * (grad[j] - mean) : weight[j] * grad[j];
+            }
             wave_sync();
+            lo = lo_next, hi = hi_next;
         }
+        const Memory out = rows_from(dlogits, ldd, t0, r.tokens, experts);
+        const float all = size * lse - even * met;
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
-            const int c = i * G + sub;
-            if (!there || c >= experts) continue;
-            float v = e[i] > 0.0f ? e[i] * (even * (share[i] - met) + size * lse) : 0.0f;
-            if constexpr (WEIGHTS) v += normalize ? s_g[at][c] : s_g[at][c] - e[i] * mean;
-            dlogits[t * ldd + c] = (T)(key[i] ? v : 0.0f);   // (masked: also where a loss's gradient is infinite or NaN)
+            float v = e[i] > 0.0f ? e[i] * fmaf(even, share[i], all) : 0.0f;
+            if constexpr (WEIGHTS) v += normalize ? s_g[at][i * G + sub] : s_g[at][i * G + sub] - e[i] * mean;
+            store_one<T>((T)(x[i] > -INFINITY ? v : 0.0f), out, to[i]);   // (masked: also where a loss's gradient is infinite or NaN)
         }
         if constexpr (WEIGHTS) wave_sync();
+#pragma unroll
+        for (int i = 0; i < NV; ++i) now[i] = next[i];
     }
 }
 
@@ -239,9 +343,9 @@ hipError_t launch_balance(const ocean_routing &r, const void *logits, int dtype,
         const hipError_t e = with_type(dtype, [&](auto t) {
             using T = decltype(t);
             return with_columns(r.experts, [&](auto g, auto nv) {
-                constexpr int G = decltype(g)::value, ROWS = TPB / G;
+                constexpr int G = decltype(g)::value, ROWS = SUM_TPB / G;
                 blocks = (int)std::min((r.tokens + ROWS - 1) / ROWS, MAX_BLOCKS);
-                hipLaunchKernelGGL((k_balance<T, G, decltype(nv)::value>), dim3(blocks), dim3(TPB), 0, s, static_cast<const T *>(logits), ld, r.tokens,
+                hipLaunchKernelGGL((k_balance<T, G, decltype(nv)::value>), dim3(blocks), dim3(SUM_TPB), 0, s, static_cast<const T *>(logits), ld, r.tokens,
                                    (int)r.experts, w);
                 return hipGetLastError();
             });
@@ -260,7 +364,9 @@ hipError_t launch_balance_backward(const ocean_balance &b, const ocean_routing &
         using T = decltype(t);
         return with_columns(r.experts, [&](auto g, auto nv) {
             constexpr int G = decltype(g)::value, NV = decltype(nv)::value;
-            const dim3 grid((uint32_t)std::min((r.tokens * G + TPB - 1) / TPB, (int64_t)1 << 20));
+            // (as many turns each: 65536 rows of 100 in 1366 workgroups of three)
+            const int64_t turns = (r.tokens * G + TPB - 1) / TPB, each = (turns + AT_ONCE - 1) / AT_ONCE;
+            const dim3 grid((uint32_t)((turns + each - 1) / each));
             auto launch = [&](auto kernel) {
                 hipLaunchKernelGGL(kernel, grid, dim3(TPB), 0, s, b, r, dloss, dval, static_cast<const T *>(logits), ld, normalize ? 1 : 0,
                                    static_cast<T *>(dlogits), ldd);

@@ -45,6 +45,13 @@ const char *converted_fault(const ocean_mx4 *q, const void *p, int32_t dtype, in
     return matrices_fault(p, q->count, stride, q->rows, q->inner, ld, dtype, !to_q);
 }
 
+// (turns of 64 rows are reached by 32-bit offsets)
+const char *logits_fault(const void *p, const ocean_routing *r, int64_t ld, int32_t dtype)
+{
+    if (const char *why = matrix_fault(p, r->tokens, r->experts, ld, dtype)) return why;
+    return ld >= (1 << 23) ? "row strides of logits must be below 2^23 elements" : nullptr;
+}
+
 }  // namespace
 
 extern "C" {
@@ -61,7 +68,7 @@ int ocean_route_balance(const ocean_routing *r, const void *logits, int32_t dtyp
     if (!known_type(dtype)) return bad("dtype must be OCEAN_F32, OCEAN_BF16 or OCEAN_F16");
     REFUSE(routing_fault(r, false, false));
     if (!r->expert_ptr) return bad("expert_ptr is null");
-    REFUSE(matrix_fault(logits, r->tokens, r->experts, ld, dtype));
+    REFUSE(logits_fault(logits, r, ld, dtype));
     if (!out || !out->loss || !out->counts || !out->prob || !out->rows) return bad("the balance or an array of it is null");
     if (!workspace || !aligned(workspace, 256) || workspace_bytes < balance_workspace(r->tokens, r->experts))
         return bad("workspace is null, not aligned to 256 bytes or smaller than ocean_route_balance_workspace");
@@ -75,8 +82,8 @@ int ocean_route_balance_backward(const ocean_balance *b, const ocean_routing *r,
     REFUSE(routing_fault(r, dval != nullptr, false));
     if (dval && r->tokens > 0 && !r->col_idx) return bad("col_idx is null");
     if (!b || !b->counts || !b->rows || !dloss) return bad("the balance, its counts or rows, or dloss is null");
-    REFUSE(matrix_fault(logits, r->tokens, r->experts, ld, dtype));
-    REFUSE(matrix_fault(dlogits, r->tokens, r->experts, ld_dlogits, dtype));
+    REFUSE(logits_fault(logits, r, ld, dtype));
+    REFUSE(logits_fault(dlogits, r, ld_dlogits, dtype));
     return launched(launch_balance_backward(*b, *r, logits, dtype, ld, dloss, dval, normalize != 0, dlogits, ld_dlogits, static_cast<hipStream_t>(stream)),
                     "ocean_route_balance_backward");
 }

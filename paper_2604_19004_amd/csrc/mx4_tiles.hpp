@@ -16,12 +16,6 @@ struct Mx4Args {
 };
 inline Mx4Args mx4_args(const ocean_mx4 &w) { return Mx4Args{w.codes, w.scales, w.ld_codes, w.stride_codes, w.ld_scales, w.stride_scales, (int)mx4_blocks(w.inner)}; }
 
-// Memory from `base` on, for loads of 32-bit offsets: an offset of NOWHERE reads zeros (the hardware's range check), so that the end of the lines takes
-// no branch.  (With a choice of addresses there, the compiler made a branch of it and, where a workgroup's first step was the end, used a piece's
-// offset from a register that it had written in the other lanes only.)
-typedef __amdgpu_buffer_rsrc_t Memory;
-constexpr uint32_t MEMORY_BYTES = 0xfffff000u, NOWHERE = 0xfffffff0u;
-__device__ __forceinline__ Memory memory_at(const void *base) { return __builtin_amdgcn_make_buffer_rsrc(const_cast<void *>(base), 0, MEMORY_BYTES, 0x00027000); }
 // BYTES bytes a lane straight to LDS, where the wave's lie side by side from `lds` on.
 template <int BYTES> __device__ __forceinline__ void memory_to_lds(Memory m, uint32_t offset, uint32_t step, char *lds)
 {

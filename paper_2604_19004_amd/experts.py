@@ -89,8 +89,8 @@ def route_balance(logits, routing, *, stream=None) -> Balance:
     s, here = _at(logits.device, stream, logits, *lists)
     with here:
         E, dev = routing.experts, logits.device
-        counts, rows = torch.empty(E + 1, dtype=torch.int64, device=dev).split((E, 1))
-        loss, prob = torch.empty(E + 2, dtype=torch.float32, device=dev).split((2, E))
+        counts, rows = torch.empty(E, dtype=torch.int64, device=dev), torch.empty(1, dtype=torch.int64, device=dev)
+        loss, prob = torch.empty(2, dtype=torch.float32, device=dev), torch.empty(E, dtype=torch.float32, device=dev)
         nbytes = lib.ocean_route_balance_workspace(routing.tokens, E)
         space = torch.empty(nbytes, dtype=torch.uint8, device=dev)
         c = ocean_balance(loss.data_ptr(), counts.data_ptr(), prob.data_ptr(), rows.data_ptr())
@@ -170,6 +170,20 @@ class Mx4:
         count, rows = (1, c.shape[0]) if c.dim() == 2 else c.shape[:2]
         self.__dict__.update(_struct=ocean_mx4(count, rows, self.inner, _ptr(c), ldc, sc, _ptr(s), lds, ss))
 
+    @classmethod
+    def _made(cls, shape, device):
+        """One with new arrays."""
+        import torch
+        *many, inner = shape
+        blocks = _blocks(inner)
+        width, up = 16 * blocks, (blocks + 3) // 4 * 4
+        codes, scales = torch.empty((*many, width), dtype=torch.uint8, device=device), torch.empty((*many, up), dtype=torch.uint8, device=device)
+        count, rows = many if len(many) == 2 else (1, many[0])
+        q = object.__new__(cls)
+        q.__dict__.update(codes=codes, scales=scales, inner=inner,
+                          _struct=ocean_mx4(count, rows, inner, _ptr(codes), width, rows * width, _ptr(scales), up, rows * up))
+        return q
+
     def __reduce__(self):
         """Copies and pickles are made of the fields: the struct holds pointers to this one's arrays."""
         return Mx4, (self.codes, self.scales, self.inner)
@@ -213,13 +227,11 @@ def mx4_quantize(x, *, out: Mx4 = None, stream=None) -> Mx4:
         raise ValueError(f"x must be [rows, inner] or [count, rows, inner], not {tuple(x.shape)}")
     code = _code(x.dtype)
     ld, stride = _cube(x, "x")
-    blocks = _blocks(x.shape[-1])
     held = () if out is None else (out.codes, out.scales)
     s, here = _at(x.device, stream, x, *held)
     with here:
         if out is None:
-            out = Mx4(torch.empty((*x.shape[:-1], 16 * blocks), dtype=torch.uint8, device=x.device),
-                      torch.empty((*x.shape[:-1], (blocks + 3) // 4 * 4), dtype=torch.uint8, device=x.device), x.shape[-1])
+            out = Mx4._made(x.shape, x.device)
         elif tuple(out.shape) != tuple(x.shape) or out.codes.device != x.device:
             raise ValueError(f"out must be {tuple(x.shape)} on {x.device}, not {tuple(out.shape)} on {out.codes.device}")
         _b._check(lib.ocean_mx4_quantize(_ptr(x), code, ld, stride, C.byref(out._struct), s))
