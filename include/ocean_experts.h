@@ -22,7 +22,7 @@ extern "C" {
  * prob[e] = the mean of softmax(row)[e], counts[e] = the entries of expert e in the routing (n of all), and
  *   loss[0] = experts * sum over e of counts[e] / n * prob[e]   (1 where all are used evenly),
  *   loss[1] = the mean of logsumexp(row)^2.
- * Without such rows, or without entries, what has no value is 0.
+ * Without such rows, or without entries, what has no value is 0.  Row strides of logits and of their gradient are below 2^23 elements.
  */
 typedef struct ocean_balance {
     float *loss;        /* 2 */
@@ -52,8 +52,7 @@ int ocean_route_balance_backward(const ocean_balance *b, const ocean_routing *r,
  * the point: 0, 0.5, 1, 1.5, 2, 3, 4, 6; the number is that times 2^(s - 127); s = 255 makes a block of NaN.  (The format called
  * MXFP4: e2m1 with e8m0.)  With blocks = (inner + 31) / 32: row i of matrix e has its codes at codes + e * stride_codes + i * ld_codes
  * (16 * blocks bytes; those behind `inner` are not used, whatever they hold) and its scales at scales + e * stride_scales + i * ld_scales (blocks bytes, and
- * up to the next multiple of 4 there has to be memory, whose content does not count).  Strides are in bytes.  Codes, ld_codes and stride_codes are multiples of 16,
- * scales, ld_scales and stride_scales of 4.  Numbers beyond a type's range are infinite in it; single precision and bfloat16 hold all with s <= 252.
+ * up to the next multiple of 16 there has to be memory, whose content does not count).  Strides are in bytes; codes, scales and all strides are multiples of 16.  Numbers beyond a type's range are infinite in it; single precision and bfloat16 hold all with s <= 252.
  */
 typedef struct ocean_mx4 {
     int64_t count, rows, inner;
@@ -66,7 +65,7 @@ typedef struct ocean_mx4 {
 /*
  * x, `count` matrices of rows x inner at stride_x elements, into q.  A block's scale is 2^(floor(log2 of its largest magnitude) - 2), not below
  * 2^-127, or 1 where all are 0; its numbers are rounded to the nearest (ties to the even code) and magnitudes beyond 6 become 6.  A block that holds an
- * infinite number or NaN becomes NaN.  Codes behind `inner` are 0.  Scales' bytes up to the next multiple of 4 are 0.  count * rows < 2^31 - 4096.
+ * infinite number or NaN becomes NaN.  Codes behind `inner` are 0, and so are scales' bytes up to the next multiple of 16.  count * rows < 2^31 - 4096.
  */
 int ocean_mx4_quantize(const void *x, int32_t dtype, int64_t ld_x, int64_t stride_x, const ocean_mx4 *q, ocean_stream_t stream);
 
@@ -76,7 +75,7 @@ int ocean_mx4_dequantize(const ocean_mx4 *q, int32_t dtype, void *out, int64_t l
 /*
  * As ocean_grouped_matmul, with matrices in four bits: y[s] = x[row(s)] * W_e^T for the rows of group e (transposed == 0; x: x_rows x w->inner, y: rows x
  * w->rows), or y[s] = x[row(s)] * W_e (transposed != 0; x: x_rows x w->rows, y: rows x w->inner), which is the gradient of x's rows.
- * w->count is the groups' `experts`.  The matrices' numbers are taken as they are, x's too: as bfloat16, or as the exact sum of two (float16) or three (single
+ * w->count is the groups' `experts`, and its row strides are below 2^23.  The matrices' numbers are taken as they are, x's too: as bfloat16, or as the exact sum of two (float16) or three (single
  * precision; what is left of a number below 2^-133 is not kept) such.
  */
 int ocean_grouped_matmul_mx4(const ocean_groups *g, int32_t dtype, const void *x, int64_t ld_x, const ocean_mx4 *w, int32_t transposed, void *y,

@@ -12,17 +12,17 @@ const char *mx4_fault(const ocean_mx4 *q, bool written)
     if (!q) return "the matrix in four bits is null";
     if (q->count < 0 || q->count > OCEAN_GROUPS_MAX || q->rows < 0 || q->rows >= MAX_DIM || q->inner < 0 || q->inner >= MAX_DIM)
         return "count (OCEAN_GROUPS_MAX), rows or inner of the matrix in four bits out of range";
-    const int64_t blocks = mx4_blocks(q->inner), width = blocks * 16, words = (blocks + 3) / 4 * 4;
+    const int64_t blocks = mx4_blocks(q->inner), width = blocks * 16, up = (blocks + 15) / 16 * 16;
     if (q->ld_codes % 16 || q->stride_codes % 16 || !aligned(q->codes, 16)) return "codes are not aligned to 16 bytes (base and strides)";
-    if (q->ld_scales % 4 || q->stride_scales % 4 || !aligned(q->scales, 4)) return "scales are not aligned to 4 bytes (base and strides)";
-    if (q->ld_codes < width || q->ld_scales < words) return "a row stride of codes or scales is less than the row's width";
+    if (q->ld_scales % 16 || q->stride_scales % 16 || !aligned(q->scales, 16)) return "scales are not aligned to 16 bytes (base and strides)";
+    if (q->ld_codes < width || q->ld_scales < up) return "a row stride of codes or scales is less than the row's width";
     if (q->ld_codes >= (1ll << 40) || q->ld_scales >= (1ll << 40) || (q->rows > 1 && (q->ld_codes > (1ll << 46) / q->rows || q->ld_scales > (1ll << 46) / q->rows)))
         return "a matrix in four bits spans more than 2^46 bytes";
     if (q->stride_codes < 0 || q->stride_codes >= (1ll << 44) || q->stride_scales < 0 || q->stride_scales >= (1ll << 44))
         return "the stride between matrices in four bits is out of range";
     if (q->count > 0 && q->rows > 0 && blocks > 0) {
         if (!q->codes || !q->scales) return "codes or scales are null";
-        if (written && q->count > 1 && (q->stride_codes < (q->rows - 1) * q->ld_codes + width || q->stride_scales < (q->rows - 1) * q->ld_scales + words))
+        if (written && q->count > 1 && (q->stride_codes < (q->rows - 1) * q->ld_codes + width || q->stride_scales < (q->rows - 1) * q->ld_scales + up))
             return "matrices in four bits that are written overlap";
     }
     return nullptr;

@@ -73,7 +73,7 @@ Shape shape_of(int64_t rows, int64_t units)
 hipError_t launch_mx4_quantize(const void *x, int dtype, int64_t ldx, int64_t stride, const ocean_mx4 &q, hipStream_t s)
 {
     if (q.count == 0 || q.rows == 0 || q.inner == 0) return hipSuccess;
-    const int units = (int)((mx4_blocks(q.inner) + 3) / 4 * 16);
+    const int units = (int)((mx4_blocks(q.inner) + 15) / 16 * 64);
     const Shape shape = shape_of(q.count * q.rows, units);
     return with_type(dtype, [&](auto t) {
         using T = decltype(t);

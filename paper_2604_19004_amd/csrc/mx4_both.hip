@@ -155,32 +155,27 @@ __global__ void __launch_bounds__(WAVES_M * WAVES_N * WAVE, 2) k_gmm_mx4_mx4(Gmm
 }
 
 // Few rows: the matrix is read once, straight into registers, a block and its scale a lane.
-template <class O, int TN, int WAVES>
+template <class O, int ROWS, int TN, int WAVES>
 __global__ void __launch_bounds__(WAVES * WAVE, 2) k_few_mx4_mx4(GmmArgs a, Mx4Args x, Mx4Args m)
 {
     __shared__ __align__(16) float s_sums[few_lds(TN, WAVES)];
-    __shared__ int64_t s_row[FEW_ROWS];
+    __shared__ __align__(16) uint8_t s_scales[2][TN * 16 * FewScales<TN, WAVES>::PITCH];
+    __shared__ int64_t s_row[ROWS];
     RowsTile w;
-    if (!few_rows_tile<O, TN * 16>(a, w)) return;
+    if (!few_rows_tile<O, ROWS, TN * 16>(a, w)) return;
     const int lane = lane_id(), r = lane % 16, g = lane / 16, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE);
-    const uint8_t *codes[TN], *scales[TN];
+    const uint8_t *codes[TN];
 #pragma unroll
-    for (int j = 0; j < TN; ++j) {
-        const int64_t n = min(w.n0 + j * 16 + r, (int)a.n - 1);
-        codes[j] = m.codes + w.group * m.stride_codes + n * m.ld_codes;
-        scales[j] = m.scales + w.group * m.stride_scales + n * m.ld_scales;
-    }
-    const int whole = (int)(a.c / 128), steps = (int)((a.c + 127) / 128), rows = min(FEW_ROWS, w.hi - w.m0);
-    auto load_w = [&](Mx4Blocks<TN> &to, int t) { to.load(codes, scales, min(t * 4 + g, m.blocks - 1)); };
+    for (int j = 0; j < TN; ++j) codes[j] = m.codes + w.group * m.stride_codes + min(w.n0 + j * 16 + r, (int)a.n - 1) * m.ld_codes;
+    const int whole = (int)(a.c / 128), steps = (int)((a.c + 127) / 128), rows = min(ROWS, w.hi - w.m0);
     O *out = static_cast<O *>(a.out);
     auto store = [&](int row, int64_t col, float v) { out[(int64_t)(w.m0 + row) * a.ldo + col] = (O)(s_row[row] < 0 ? 0.0f : v); };
     auto tile = [&](auto tm) {
-        constexpr int TM = decltype(tm)::value, U = TM <= 2 && TN <= 2 ? 4 : 2;
-        Mx4Blocks<TN> now[U];
-        if (wave < steps) {
-#pragma unroll
-            for (int u = 0; u < U; ++u) load_w(now[u], wave + u * WAVES);
-        }
+        constexpr int TM = decltype(tm)::value, U = TN == 2 && TM <= 2 ? 4 : 2;
+        // (on their way while the rows are found)
+        FewScales<TN, WAVES> scales(m.scales + w.group * m.stride_scales, m.ld_scales, w.n0, a.n, m.blocks);
+        Mx4Batch<TN, U> b;
+        if (steps > 0) b.load(codes, min(wave * 4, steps - 1), g, m.blocks);
         if ((int)threadIdx.x < rows) {
             const int64_t row = a.index ? a.index[w.m0 + threadIdx.x] : w.m0 + threadIdx.x;
             s_row[threadIdx.x] = (uint64_t)row < (uint64_t)a.index_rows ? row : -1;
@@ -194,33 +189,53 @@ __global__ void __launch_bounds__(WAVES * WAVE, 2) k_few_mx4_mx4(GmmArgs a, Mx4A
             x_scales[i] = x.scales + row * x.ld_scales;
         }
         f32x4 acc[TM][TN] = {};
-        Mx4Blocks<TM> xs[U];
-        auto load_x = [&](int t, bool) {
+        // U steps from t0 on; END: some of them may reach behind the lines' end.
+        auto multiply = [&](int t0, auto end) {
+            Mx4Batch<TM, U> xs;
+            xs.load(x_codes, t0, g, m.blocks);
+            const uint8_t *words[TM];
 #pragma unroll
-            for (int u = 0; u < U; ++u) xs[u].load(x_codes, x_scales, min((t + u * WAVES) * 4 + g, m.blocks - 1));
-        };
-        auto use = [&](Mx4Blocks<TN> (&b)[U], int t0, bool end) {
+            for (int i = 0; i < TM; ++i) words[i] = x_scales[i] + (int64_t)t0 * 4;
+            xs.load_scales(words);
 #pragma unroll
             for (int u = 0; u < U; ++u) {
-                const int t = t0 + u * WAVES;
-                if (end && t >= whole) {
-                    const int valid = (int)max(min(a.c - ((int64_t)t * 128 + g * MX4_BLOCK), (int64_t)32), (int64_t)0);
-                    b[u].end(valid);
-                    xs[u].end(valid);
+                if constexpr (decltype(end)::value) {
+                    const int valid = t0 + u < steps ? (int)max(min(a.c - ((int64_t)(t0 + u) * 128 + g * MX4_BLOCK), (int64_t)MX4_BLOCK), (int64_t)0) : 0;
+                    b.end(u, valid);
+                    xs.end(u, valid);
                 }
 #pragma unroll
                 for (int i = 0; i < TM; ++i)
 #pragma unroll
                     for (int j = 0; j < TN; ++j)
-                        mma_mx4(acc[i][j], __builtin_bit_cast(u32x4, b[u].v[j]), b[u].s[j], __builtin_bit_cast(u32x4, xs[u].v[i]), xs[u].s[i]);
+                        mma_mx4(acc[i][j], __builtin_bit_cast(u32x4, b.v[u][j]), b.s[j][u] >> 8 * g, __builtin_bit_cast(u32x4, xs.v[u][i]), xs.s[i][u] >> 8 * g);
             }
         };
-        few_walk<U, WAVES>(now, wave, steps, load_w, load_x, use);
+        for (int pass = 0; pass * WAVES * 4 < steps; ++pass) {
+            scales.store(s_scales[pass & 1]);
+            __syncthreads();
+            scales.next();
+            const int first = (pass * WAVES + wave) * 4;
+#pragma unroll
+            for (int i = 0; i < 4; i += U) {
+                const int t = first + i, t_next = i + U < 4 ? t + U : first + WAVES * 4;
+                if (t >= steps) break;
+                const uint8_t *words[TN];
+#pragma unroll
+                for (int j = 0; j < TN; ++j) words[j] = s_scales[pass & 1] + (j * 16 + r) * FewScales<TN, WAVES>::PITCH + (wave * 4 + i) * 4;
+                b.load_scales(words);
+                if (t + U <= whole) multiply(t, std::false_type{});
+                else multiply(t, std::true_type{});
+                if (t_next < steps) b.load(codes, t_next, g, m.blocks);
+            }
+        }
         few_meet<TM, TN, WAVES>(acc, rows, w.n0, a.n, s_sums, store);
     };
-    if (rows <= 16) tile(std::integral_constant<int, 1>{});
-    else if (rows <= 32) tile(std::integral_constant<int, 2>{});
-    else tile(std::integral_constant<int, 4>{});
+    if (ROWS == 16 || rows <= 16) tile(std::integral_constant<int, 1>{});
+    else if constexpr (ROWS >= 32) {
+        if (ROWS == 32 || rows <= 32) tile(std::integral_constant<int, 2>{});
+        else if constexpr (ROWS == 64) tile(std::integral_constant<int, 4>{});
+    }
 }
 
 template <class O, int BM, int BN, int WAVES_M, int WAVES_N, int STAGES> hipError_t launch_tile(const GmmArgs &a, const Mx4Args &x, const Mx4Args &m, hipStream_t s)
@@ -240,12 +255,13 @@ template <class O> hipError_t pick(const GmmArgs &a, const Mx4Args &x, const Mx4
     // (tiles reach 256 lines of the matrix and the rows of x that they gather by 32-bit offsets)
     const bool reached = offsets_fit(a.index ? std::max<int64_t>(a.index_rows, 256) : 256, std::max(x.ld_codes, x.ld_scales), 1);
     if (few(a) || !reached) {
-        const int columns = few_columns(a);
-        auto launch = [&](auto tn) {
-            hipLaunchKernelGGL((k_few_mx4_mx4<O, decltype(tn)::value, 8>), few_grid(a, decltype(tn)::value * 16), dim3(8 * WAVE), 0, s, a, x, m);
+        return launch_few(a, [&](auto rows, auto tn, auto waves) {
+            constexpr int ROWS = decltype(rows)::value, TN = decltype(tn)::value, WAVES = decltype(waves)::value;
+            const dim3 grid = few_grid(a, ROWS, TN * 16);
+            if (grid.x >= 1u << 23 || grid.y > 65535u) return TOO_MANY_TILES;
+            hipLaunchKernelGGL((k_few_mx4_mx4<O, ROWS, TN, WAVES>), grid, dim3(WAVES * WAVE), 0, s, a, x, m);
             return hipGetLastError();
-        };
-        return columns == 4 ? launch(std::integral_constant<int, 4>{}) : columns == 2 ? launch(std::integral_constant<int, 2>{}) : launch(std::integral_constant<int, 1>{});
+        });
     }
     if constexpr (sizeof(O) == 2)   // (results of 32 bits do not fit the operands' place in LDS)
         if (tiles(128, 128) >= 512 && launches<GM_ROWS>(a, 256, 256, 512)) return launch_tile<O, 256, 256, 2, 4, 2>(a, x, m, s);

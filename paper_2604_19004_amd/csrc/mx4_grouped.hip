@@ -199,33 +199,28 @@ __global__ void __launch_bounds__(WAVES_M * WAVES_N * WAVE, 2) k_gmm_mx4(GmmArgs
 
 // Few rows: the matrix is read once, straight into registers.  A lane's 32 numbers of c are those of its block, in four matrix instructions; x is read
 // to match.
-template <class T, int TN, int WAVES>
+template <class T, int ROWS, int TN, int WAVES>
 __global__ void __launch_bounds__(WAVES * WAVE, 2) k_few_mx4(GmmArgs a, Mx4Args m)
 {
     constexpr int PARTS = PARTS_OF<T>;
     __shared__ __align__(16) float s_sums[few_lds(TN, WAVES)];
-    __shared__ int64_t s_row[FEW_ROWS];
+    __shared__ __align__(16) uint8_t s_scales[2][TN * 16 * FewScales<TN, WAVES>::PITCH];
+    __shared__ int64_t s_row[ROWS];
     RowsTile w;
-    if (!few_rows_tile<T, TN * 16>(a, w)) return;
+    if (!few_rows_tile<T, ROWS, TN * 16>(a, w)) return;
     const int lane = lane_id(), r = lane % 16, g = lane / 16, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE);
-    const uint8_t *codes[TN], *scales[TN];
+    const uint8_t *codes[TN];
 #pragma unroll
-    for (int j = 0; j < TN; ++j) {
-        const int64_t n = min(w.n0 + j * 16 + r, (int)a.n - 1);
-        codes[j] = m.codes + w.group * m.stride_codes + n * m.ld_codes;
-        scales[j] = m.scales + w.group * m.stride_scales + n * m.ld_scales;
-    }
-    const int whole = (int)(a.c / 128), steps = (int)((a.c + 127) / 128), rows = min(FEW_ROWS, w.hi - w.m0);
-    auto load_w = [&](Mx4Blocks<TN> &to, int t) { to.load(codes, scales, min(t * 4 + g, m.blocks - 1)); };
+    for (int j = 0; j < TN; ++j) codes[j] = m.codes + w.group * m.stride_codes + min(w.n0 + j * 16 + r, (int)a.n - 1) * m.ld_codes;
+    const int whole = (int)(a.c / 128), steps = (int)((a.c + 127) / 128), rows = min(ROWS, w.hi - w.m0);
     T *out = static_cast<T *>(a.out);
     auto store = [&](int row, int64_t col, float v) { out[(int64_t)(w.m0 + row) * a.ldo + col] = (T)(s_row[row] < 0 ? 0.0f : v); };
     auto tile = [&](auto tm) {
-        constexpr int TM = decltype(tm)::value, U = TM == 1 && sizeof(T) == 2 ? (TN <= 2 ? 4 : 2) : 1;
-        Mx4Blocks<TN> now[U];
-        if (wave < steps) {
-#pragma unroll
-            for (int u = 0; u < U; ++u) load_w(now[u], wave + u * WAVES);
-        }
+        constexpr int TM = decltype(tm)::value, U = TM == 4 || sizeof(T) * TM > 4 ? 1 : sizeof(T) * TM * TN > 4 ? 2 : 4;
+        // (on their way while the rows are found)
+        FewScales<TN, WAVES> scales(m.scales + w.group * m.stride_scales, m.ld_scales, w.n0, a.n, m.blocks);
+        Mx4Batch<TN, U> b;
+        if (steps > 0) b.load(codes, min(wave * 4, steps - 1), g, m.blocks);
         if ((int)threadIdx.x < rows) {
             const int64_t row = a.index ? a.index[w.m0 + threadIdx.x] : w.m0 + threadIdx.x;
             s_row[threadIdx.x] = (uint64_t)row < (uint64_t)a.index_rows ? row : -1;
@@ -236,42 +231,38 @@ __global__ void __launch_bounds__(WAVES * WAVE, 2) k_few_mx4(GmmArgs a, Mx4Args 
         for (int i = 0; i < TM; ++i) x[i] = static_cast<const T *>(a.l) + max(s_row[min(i * 16 + r, rows - 1)], (int64_t)0) * a.ldl + g * MX4_BLOCK;
         f32x4 acc[TM][TN] = {};
         struct Eight { uint4 v[sizeof(T) / 2]; };
-        Eight xs[U][TM][4];
-        auto load_x = [&](int t0, bool end) {
+        // U steps from t0 on; END: some of them may reach behind the lines' end.
+        auto multiply = [&](int t0, auto end) {
+            constexpr bool END = decltype(end)::value;
+            Eight xs[U][TM][4];
 #pragma unroll
             for (int u = 0; u < U; ++u) {
-                const int t = t0 + u * WAVES;
-                if (!end || t < whole) {
-#pragma unroll
-                    for (int i = 0; i < TM; ++i)
-#pragma unroll
-                        for (int q = 0; q < 4; ++q)
-#pragma unroll
-                            for (int p = 0; p < (int)sizeof(T) / 2; ++p) xs[u][i][q].v[p] = load_any(reinterpret_cast<const char *>(x[i] + t * 128 + q * 8 + p * PIECE<T>));
-                } else {
-                    const int64_t left = a.c - ((int64_t)t * 128 + g * MX4_BLOCK);
-#pragma unroll
-                    for (int i = 0; i < TM; ++i)
-#pragma unroll
-                        for (int q = 0; q < 4; ++q)
-#pragma unroll
-                            for (int p = 0; p < (int)sizeof(T) / 2; ++p)
-                                xs[u][i][q].v[p] = load_piece(x[i] + (int64_t)t * 128 + q * 8 + p * PIECE<T>, (int)max(min(left - q * 8 - p * PIECE<T>, (int64_t)8), (int64_t)0));
+                const T *at = nullptr;
+                int valid = MX4_BLOCK;
+                if constexpr (END) {
+                    valid = t0 + u < steps ? (int)max(min(a.c - ((int64_t)(t0 + u) * 128 + g * MX4_BLOCK), (int64_t)MX4_BLOCK), (int64_t)0) : 0;
+                    b.end(u, valid);
                 }
-            }
-        };
-        auto use = [&](Mx4Blocks<TN> (&b)[U], int t0, bool end) {
 #pragma unroll
-            for (int u = 0; u < U; ++u) {
-                const int t = t0 + u * WAVES;
-                if (end && t >= whole) b[u].end((int)max(min(a.c - ((int64_t)t * 128 + g * MX4_BLOCK), (int64_t)32), (int64_t)0));
+                for (int i = 0; i < TM; ++i)
+#pragma unroll
+                    for (int q = 0; q < 4; ++q)
+#pragma unroll
+                        for (int p = 0; p < (int)sizeof(T) / 2; ++p) {
+                            at = x[i] + (int64_t)(t0 + u) * 128 + q * 8 + p * PIECE<T>;
+                            xs[u][i][q].v[p] = END ? load_piece(at, valid - q * 8 - p * PIECE<T>) : load_any(reinterpret_cast<const char *>(at));
+                        }
+            }
+#pragma unroll
+            for (int u = 0; u < U; ++u)
 #pragma unroll
                 for (int q = 0; q < 4; ++q) {
                     Frag<bf16_t> fw[TN];
 #pragma unroll
                     for (int j = 0; j < TN; ++j) {
+                        const uint4 &v = b.v[u][j];
                         bf16_t e[8];
-                        mx4_widen<bf16_t>(q == 0 ? b[u].v[j].x : q == 1 ? b[u].v[j].y : q == 2 ? b[u].v[j].z : b[u].v[j].w, mx4_scale(b[u].s[j]), e);
+                        mx4_widen<bf16_t>(q == 0 ? v.x : q == 1 ? v.y : q == 2 ? v.z : v.w, mx4_scale(b.scale(u, j, g)), e);
                         fw[j] = bf16x8{e[0], e[1], e[2], e[3], e[4], e[5], e[6], e[7]};
                     }
 #pragma unroll
@@ -284,14 +275,32 @@ __global__ void __launch_bounds__(WAVES * WAVE, 2) k_few_mx4(GmmArgs a, Mx4Args 
                             for (int j = 0; j < TN; ++j) mma_part(acc[i][j], fw[j], p[k], 0);
                     }
                 }
-            }
         };
-        few_walk<U, WAVES>(now, wave, steps, load_w, load_x, use);
+        for (int pass = 0; pass * WAVES * 4 < steps; ++pass) {
+            scales.store(s_scales[pass & 1]);
+            __syncthreads();
+            scales.next();
+            const int first = (pass * WAVES + wave) * 4;
+#pragma unroll
+            for (int i = 0; i < 4; i += U) {
+                const int t = first + i, t_next = i + U < 4 ? t + U : first + WAVES * 4;
+                if (t >= steps) break;
+                const uint8_t *words[TN];
+#pragma unroll
+                for (int j = 0; j < TN; ++j) words[j] = s_scales[pass & 1] + (j * 16 + r) * FewScales<TN, WAVES>::PITCH + (wave * 4 + i) * 4;
+                b.load_scales(words);
+                if (t + U <= whole) multiply(t, std::false_type{});
+                else multiply(t, std::true_type{});
+                if (t_next < steps) b.load(codes, t_next, g, m.blocks);
+            }
+        }
         few_meet<TM, TN, WAVES>(acc, rows, w.n0, a.n, s_sums, store);
     };
-    if (rows <= 16) tile(std::integral_constant<int, 1>{});
-    else if (rows <= 32) tile(std::integral_constant<int, 2>{});
-    else tile(std::integral_constant<int, 4>{});
+    if (ROWS == 16 || rows <= 16) tile(std::integral_constant<int, 1>{});
+    else if constexpr (ROWS >= 32) {
+        if (ROWS == 32 || rows <= 32) tile(std::integral_constant<int, 2>{});
+        else if constexpr (ROWS == 64) tile(std::integral_constant<int, 4>{});
+    }
 }
 
 template <class T, bool RCOL, int BM, int BN, int WAVES_M, int WAVES_N, bool ASYNC> hipError_t launch_tile(const GmmArgs &a, const Mx4Args &m, hipStream_t s)
@@ -310,12 +319,13 @@ template <class T, bool RCOL> hipError_t pick(const GmmArgs &a, const Mx4Args &m
     auto tiles = [&](int64_t bm, int64_t bn) { return (double)m_tiles(bm) * (double)((a.n + bn - 1) / bn); };
     if constexpr (!RCOL) {
         if (few(a)) {
-            const int columns = few_columns(a);
-            auto launch = [&](auto tn) {
-                hipLaunchKernelGGL((k_few_mx4<T, decltype(tn)::value, 8>), few_grid(a, decltype(tn)::value * 16), dim3(8 * WAVE), 0, s, a, m);
+            return launch_few(a, [&](auto rows, auto tn, auto waves) {
+                constexpr int ROWS = decltype(rows)::value, TN = decltype(tn)::value, WAVES = decltype(waves)::value;
+                const dim3 grid = few_grid(a, ROWS, TN * 16);
+            if (grid.x >= 1u << 23 || grid.y > 65535u) return TOO_MANY_TILES;
+            hipLaunchKernelGGL((k_few_mx4<T, ROWS, TN, WAVES>), grid, dim3(WAVES * WAVE), 0, s, a, m);
                 return hipGetLastError();
-            };
-            return columns == 4 ? launch(std::integral_constant<int, 4>{}) : columns == 2 ? launch(std::integral_constant<int, 2>{}) : launch(std::integral_constant<int, 1>{});
+            });
         }
     }
     if constexpr (std::is_same<T, bf16_t>::value) {

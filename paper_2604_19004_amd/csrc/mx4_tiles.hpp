@@ -105,63 +105,84 @@ __device__ __forceinline__ void store_tile(const GmmArgs &a, const RowsTile &w, 
     }
 }
 
-// Few rows: workgroup (x, y) has columns 16 TN x .. of the y-th tile of up to 64 rows of a group, as in k_few.  Its waves take every WAVES-th 128 numbers
+// Few rows: workgroup (x, y) has columns 16 TN x .. of the y-th tile of up to ROWS rows of a group, as in k_few.  Its waves take every WAVES-th 128 numbers
 // of c, a block of 32 of a line a lane, and their sums meet in LDS.
-constexpr int FEW_ROWS = 64;
-template <class O, int COLS> __device__ __forceinline__ bool few_rows_tile(const GmmArgs &a, RowsTile &w)
+template <class O, int ROWS, int COLS> __device__ __forceinline__ bool few_rows_tile(const GmmArgs &a, RowsTile &w)
 {
     int tiles = 0;
     w.n0 = (int)blockIdx.x * COLS;
     auto item_of = [&](int n) { tiles = n; return (int)blockIdx.y; };
-    if (find_tile(a, FEW_ROWS, item_of, w.group, w.m0, w.hi)) return true;
+    if (find_tile(a, ROWS, item_of, w.group, w.m0, w.hi)) return true;
     clear_outside<O>(a, w.n0, min((int64_t)COLS, a.n - w.n0), (int)blockIdx.y - tiles, (int)gridDim.y - tiles);
     return false;
 }
 
-// A block of each of TN lines of a matrix, and its scale.
-template <int TN> struct Mx4Blocks {
-    uint4 v[TN];
-    uint32_t s[TN];
-    __device__ __forceinline__ void load(const uint8_t *const (&codes)[TN], const uint8_t *const (&scales)[TN], int block)
+// U steps of 128 numbers of N lines: a block a lane and step (of 16 lanes' the group-th), and a word with the scales of a step's four blocks.
+template <int N, int U> struct Mx4Batch {
+    uint4 v[U][N];
+    uint32_t s[N][U];
+    // steps t .. t + U - 1 (blocks behind the end: the last one)
+    __device__ __forceinline__ void load(const uint8_t *const (&codes)[N], int t, int group, int blocks)
     {
 #pragma unroll
-        for (int j = 0; j < TN; ++j) {
-            v[j] = *reinterpret_cast<const uint4 *>(codes[j] + (int64_t)block * 16);
-            s[j] = scales[j][block];
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int j = 0; j < N; ++j) v[u][j] = *reinterpret_cast<const uint4 *>(codes[j] + (int64_t)min((t + u) * 4 + group, blocks - 1) * 16);
+    }
+    // scales[j]: where line j's words of the steps are (t a multiple of U: nothing is read behind a row's 16 bytes)
+    template <class P> __device__ __forceinline__ void load_scales(const P *const (&scales)[N])
+    {
+        using Words = std::conditional_t<U == 4, uint4, std::conditional_t<U == 2, uint2, uint32_t>>;
+#pragma unroll
+        for (int j = 0; j < N; ++j) {
+            const Words w = *reinterpret_cast<const Words *>(scales[j]);
+            __builtin_memcpy(s[j], &w, sizeof w);
         }
     }
-    // only the first `valid` numbers
-    __device__ __forceinline__ void end(int valid)
+    // only the first `valid` numbers of step u
+    __device__ __forceinline__ void end(int u, int valid)
     {
 #pragma unroll
-        for (int j = 0; j < TN; ++j) {
-            v[j] = make_uint4(mx4_first(v[j].x, valid), mx4_first(v[j].y, valid - 8), mx4_first(v[j].z, valid - 16), mx4_first(v[j].w, valid - 24));
-            s[j] = valid > 0 ? s[j] : 127u;
+        for (int j = 0; j < N; ++j) {
+            uint4 &w = v[u][j];
+            w = make_uint4(mx4_first(w.x, valid), mx4_first(w.y, valid - 8), mx4_first(w.z, valid - 16), mx4_first(w.w, valid - 24));
+            s[j][u] = valid > 0 ? s[j][u] : 0x7f7f7f7fu;
         }
     }
+    __device__ __forceinline__ uint32_t scale(int u, int j, int group) const { return s[j][u] >> 8 * group & 255u; }
 };
 
-// The walk of a wave over its steps of 128 numbers, U at a time, the matrix's blocks of the next ones under way meanwhile: first(t) loads those of step t
-// into `next` ahead of everything else, x(u, t) what they meet, use(u, t, end) multiplies; `end`: the step may reach behind the lines' end, and is then
-// told what is there by its blocks.
-template <int U, int WAVES, class Blocks, class LoadW, class LoadX, class Use>
-__device__ __forceinline__ void few_walk(Blocks (&now)[U], int wave, int steps, LoadW load_w, LoadX load_x, Use use)
-{
-    int t = wave;
-    for (; t + U * WAVES < steps; t += U * WAVES) {   // (all of these lie before the end)
-        Blocks next[U];
-        load_x(t, false);
-#pragma unroll
-        for (int u = 0; u < U; ++u) load_w(next[u], t + (U + u) * WAVES);
-        use(now, t, false);
-#pragma unroll
-        for (int u = 0; u < U; ++u) now[u] = next[u];
+// Few rows: the workgroup's 16 TN lines of the matrix go by in passes of four steps a wave.  Codes come straight into registers, 256 bytes of a line a wave.
+// Scales pass through LDS: read where they are needed, 8 bytes of a line here and 8 there, their lines of memory were fetched into the compute unit again and
+// again (96 rows of 16 experts, 4096 x 4096, rows in four bits: 45 us, and with all scales 1, 28).
+template <int TN, int WAVES> struct FewScales {
+    static constexpr int BYTES = WAVES * 16, PITCH = BYTES + 16, PIECES = TN * 16 * WAVES;   // of a line in a pass; in LDS, where 16 lines lie on different banks
+    static_assert(PIECES <= WAVES * WAVE, "a piece a thread");
+    const uint8_t *from;
+    int left;            // bytes from there to the line's end (of up to 16 more there is memory)
+    uint4 piece;
+    __device__ __forceinline__ FewScales(const uint8_t *scales, int64_t ld, int64_t n0, int64_t n, int blocks) : piece(make_uint4(0, 0, 0, 0))
+    {
+        const int tid = threadIdx.x, at = tid % WAVES * 16;
+        from = scales + min(n0 + tid / WAVES, n - 1) * ld + at;
+        left = tid < PIECES ? blocks - at : 0;
+        load();
     }
-    if (t < steps) {
-        load_x(t, true);
-        use(now, t, true);
+    __device__ __forceinline__ void load()
+    {
+        if (left > 0) piece = *reinterpret_cast<const uint4 *>(from);
     }
-}
+    __device__ __forceinline__ void store(uint8_t *lds) const
+    {
+        const int tid = threadIdx.x;
+        if (tid < PIECES) *reinterpret_cast<uint4 *>(lds + tid / WAVES * PITCH + tid % WAVES * 16) = piece;
+    }
+    __device__ __forceinline__ void next()
+    {
+        from += BYTES, left -= BYTES;
+        load();
+    }
+};
 
 // The waves' sums meet, 16 rows at a time; store(row, column, sum) is called once for each of the tile's.
 template <int TM, int TN, int WAVES, class Store>
@@ -186,21 +207,31 @@ __device__ __forceinline__ void few_meet(const f32x4 (&acc)[TM][TN], int rows, i
     }
 }
 constexpr int few_lds(int tn, int waves) { return waves * 16 * (tn * 16 + 4); }   // floats
-inline dim3 few_grid(const GmmArgs &a, int cols)
-{
-    return dim3((uint32_t)((a.n + cols - 1) / cols), (uint32_t)(a.rows / FEW_ROWS + std::min(a.groups, a.rows)) + 1);
-}
-
-// Columns of a workgroup, in sixteens.
-inline int few_columns(const GmmArgs &a)
-{
-    const int64_t tiles = std::min(a.groups, a.rows);
-    return tiles * ((a.n + 63) / 64) >= 512 ? 4 : tiles * ((a.n + 31) / 32) >= 512 ? 2 : 1;
-}
+// Whether rows are few, and calls launch(ROWS, TN, WAVES) as constants for how many, how many columns and how long rows.
 inline bool few(const GmmArgs &a)
 {
     const int64_t groups = std::min(a.groups, a.rows);
-    return groups > 0 && a.rows <= groups * 48 && a.n <= (1 << 20) && a.rows / FEW_ROWS + groups < 65535;
+    return groups > 0 && a.rows <= groups * 48 && a.n <= (1 << 20) && a.rows / 16 + groups < 65535;
+}
+inline dim3 few_grid(const GmmArgs &a, int rows, int cols)
+{
+    return dim3((uint32_t)((a.n + cols - 1) / cols), (uint32_t)(a.rows / rows + std::min(a.groups, a.rows)) + 1);
+}
+template <class Launch> hipError_t launch_few(const GmmArgs &a, Launch launch_)
+{
+    using std::integral_constant;
+    const int64_t groups = std::min(a.groups, a.rows);
+    auto launch = [&](auto rows, auto tn) {
+        if (a.c >= 4096) return launch_(rows, tn, integral_constant<int, 8>{});
+        return launch_(rows, tn, integral_constant<int, 4>{});
+    };
+    auto with_rows = [&](auto tn) {
+        if (a.rows <= groups * 10) return launch(integral_constant<int, 16>{}, tn);
+        return launch(integral_constant<int, 32>{}, tn);
+    };
+    if (a.rows > groups * 22) return launch(integral_constant<int, 64>{}, integral_constant<int, 2>{});   // (more columns leave no registers)
+    if (groups * ((a.n + 63) / 64) >= 512) return with_rows(integral_constant<int, 4>{});
+    return with_rows(integral_constant<int, 2>{});
 }
 
 }  // namespace

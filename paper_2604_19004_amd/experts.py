@@ -150,7 +150,7 @@ def _apart(t, name, step):
 class Mx4:
     """A matrix [rows, inner] or matrices [count, rows, inner] in microscaled four bits (e2m1 codes with an e8m0 scale for every 32 numbers of a row).  codes:
     uint8 [.., rows, 16 * blocks], two numbers a byte, the earlier one in the low half, rows at multiples of 16 bytes; scales: uint8 [.., rows, blocks up to
-    a multiple of 4] (those behind the blocks do not count), rows at multiples of 4 bytes; a number is its code's value times 2^(scale - 127), 255 makes a
+    a multiple of 16] (those behind the blocks do not count), rows at multiples of 16 bytes; a number is its code's value times 2^(scale - 127), 255 makes a
     block of NaN.  blocks = (inner + 31) // 32, and codes behind `inner` do not count.  Slices of the matrices or of rows are made from slices of both arrays."""
     codes: "object"
     scales: "object"
@@ -161,12 +161,12 @@ class Mx4:
         c, s, blocks = self.codes, self.scales, _blocks(self.inner)
         if c.dtype != torch.uint8 or s.dtype != torch.uint8 or c.dim() not in (2, 3) or s.dim() != c.dim() or c.shape[:-1] != s.shape[:-1]:
             raise ValueError(f"codes and scales must be uint8 [(count,) rows, bytes] of the same rows, not {c.dtype} {tuple(c.shape)} and {s.dtype} {tuple(s.shape)}")
-        if self.inner < 0 or c.shape[-1] != 16 * blocks or s.shape[-1] < blocks or s.shape[-1] % 4:
-            raise ValueError(f"rows of {self.inner} have {16 * blocks} bytes of codes and {blocks} scales up to a multiple of 4, not {c.shape[-1]} and {s.shape[-1]}")
+        if self.inner < 0 or c.shape[-1] != 16 * blocks or s.shape[-1] < blocks or s.shape[-1] % 16:
+            raise ValueError(f"rows of {self.inner} have {16 * blocks} bytes of codes and {blocks} scales up to a multiple of 16, not {c.shape[-1]} and {s.shape[-1]}")
         if c.device != s.device:
             raise ValueError(f"codes are on {c.device}, scales on {s.device}")
         ldc, sc = _apart(c, "codes", 16)
-        lds, ss = _apart(s, "scales", 4)
+        lds, ss = _apart(s, "scales", 16)
         count, rows = (1, c.shape[0]) if c.dim() == 2 else c.shape[:2]
         self.__dict__.update(_struct=ocean_mx4(count, rows, self.inner, _ptr(c), ldc, sc, _ptr(s), lds, ss))
 
@@ -176,7 +176,7 @@ class Mx4:
         import torch
         *many, inner = shape
         blocks = _blocks(inner)
-        width, up = 16 * blocks, (blocks + 3) // 4 * 4
+        width, up = 16 * blocks, (blocks + 15) // 16 * 16
         codes, scales = torch.empty((*many, width), dtype=torch.uint8, device=device), torch.empty((*many, up), dtype=torch.uint8, device=device)
         count, rows = many if len(many) == 2 else (1, many[0])
         q = object.__new__(cls)
@@ -200,8 +200,8 @@ class Mx4:
         if codes.dtype != torch.uint8 or scales.dtype != torch.uint8 or codes.dim() not in (2, 3) or codes.shape[:-1] != scales.shape[:-1] or \
                 codes.shape[-1] != 16 * blocks or scales.shape[-1] != blocks:
             raise ValueError(f"rows of {inner} have {16 * blocks} bytes of codes and {blocks} scales (uint8), not {tuple(codes.shape)} and {tuple(scales.shape)}")
-        if blocks % 4:
-            scales = torch.nn.functional.pad(scales, (0, 4 - blocks % 4))
+        if blocks % 16:
+            scales = torch.nn.functional.pad(scales, (0, 16 - blocks % 16))
         try:
             return cls(codes, scales, inner)
         except ValueError:

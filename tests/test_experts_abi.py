@@ -40,7 +40,7 @@ def test_struct_layouts_match_the_header(ex, tmp_path):
 
 
 def _four(ex, **change):
-    q = ex.ocean_mx4(2, 8, 64, 0x1000, 32, 256, 0x1000, 4, 32)
+    q = ex.ocean_mx4(2, 8, 64, 0x1000, 32, 256, 0x1000, 16, 128)
     for name, v in change.items():
         setattr(q, name, v)
     return q
@@ -54,17 +54,17 @@ def test_refusals_of_matrices_in_four_bits(ex):
     for call in calls:
         for q, word in ((None, "null"), (_four(ex, count=-1), "range"), (_four(ex, count=16385), "OCEAN_GROUPS_MAX"), (_four(ex, rows=1 << 31), "range"),
                         (_four(ex, inner=-3), "range"), (_four(ex, codes=0x1008), "aligned"), (_four(ex, ld_codes=40), "aligned"), (_four(ex, stride_codes=264), "aligned"),
-                        (_four(ex, scales=0x1002), "aligned"), (_four(ex, ld_scales=6), "aligned"), (_four(ex, stride_scales=34), "aligned"), (_four(ex, ld_codes=16), "stride"),
+                        (_four(ex, scales=0x1008), "aligned"), (_four(ex, ld_scales=24), "aligned"), (_four(ex, stride_scales=132), "aligned"), (_four(ex, ld_codes=16), "stride"),
                         (_four(ex, ld_scales=0), "stride"), (_four(ex, ld_codes=1 << 45), "2^46"), (_four(ex, ld_scales=1 << 45), "2^46"), (_four(ex, stride_codes=-16), "stride"),
                         (_four(ex, stride_scales=1 << 50), "stride"), (_four(ex, codes=None), "null"), (_four(ex, scales=None), "null")):
             assert call(b(q) if q else None) == 1 and word in lib.ocean_last_error().decode(), (word, lib.ocean_last_error())
-    for q in (_four(ex, stride_codes=240), _four(ex, stride_scales=28)):   # (read they may overlap)
+    for q in (_four(ex, stride_codes=240), _four(ex, stride_scales=112)):   # (read they may overlap)
         assert calls[0](b(q)) == 1 and "overlap" in lib.ocean_last_error().decode()
     q = _four(ex)
     for rc, word in ((lambda: lib.ocean_mx4_quantize(0x1000, 0, 64, 512, b(q), None), "dtype"), (lambda: lib.ocean_mx4_quantize(0x1000, 1, 63, 512, b(q), None), "stride"),
                      (lambda: lib.ocean_mx4_quantize(0x1001, 1, 64, 512, b(q), None), "aligned"), (lambda: lib.ocean_mx4_quantize(None, 1, 64, 512, b(q), None), "null"),
                      (lambda: lib.ocean_mx4_dequantize(b(q), 1, 0x1000, 64, 500, None), "overlap"),
-                     (lambda: lib.ocean_mx4_quantize(0x1000, 1, 64, 512, b(_four(ex, rows=1 << 30, stride_codes=1 << 35, stride_scales=1 << 32)), None), "2^31")):
+                     (lambda: lib.ocean_mx4_quantize(0x1000, 1, 64, 512, b(_four(ex, rows=1 << 30, stride_codes=1 << 35, stride_scales=1 << 34)), None), "2^31")):
         assert rc() == 1 and word in lib.ocean_last_error().decode(), (word, lib.ocean_last_error())
 
 
@@ -77,6 +77,8 @@ def test_refusals_of_products(ex):
                      (lambda: product(b(g), 1, 0x1000, 63, b(q), 0, 0x1000, 8, None), "stride"), (lambda: product(b(g), 1, 0x1000, 64, b(q), 0, 0x1000, 7, None), "stride"),
                      (lambda: product(b(g), 1, 0x1000, 7, b(q), 1, 0x1000, 64, None), "stride"), (lambda: product(b(g), 1, 0x1000, 8, b(q), 1, 0x1000, 63, None), "stride"),
                      (lambda: product(b(g), 1, None, 64, b(q), 0, 0x1000, 8, None), "null"), (lambda: product(b(g), 2, 0x1001, 64, b(q), 0, 0x1000, 8, None), "aligned"),
+                     (lambda: product(b(g), 1, 0x1000, 64, b(_four(ex, ld_codes=1 << 23)), 0, 0x1000, 8, None), "2^23"),
+                     (lambda: both(b(g), b(x), b(_four(ex, ld_scales=1 << 23)), 2, 0x1000, 8, None), "2^23"),
                      (lambda: both(b(g), None, b(q), 2, 0x1000, 8, None), "null"), (lambda: both(b(g), b(x), None, 2, 0x1000, 8, None), "null"),
                      (lambda: both(b(g), b(_four(ex, count=1, rows=9)), b(q), 2, 0x1000, 8, None), "x_rows"),
                      (lambda: both(b(g), b(_four(ex, count=1, rows=10, inner=63)), b(q), 2, 0x1000, 8, None), "inner"),
@@ -85,8 +87,8 @@ def test_refusals_of_products(ex):
         assert rc() == 1 and word in lib.ocean_last_error().decode(), (word, lib.ocean_last_error())
     n = 1 << 23   # more tiles than a launch takes
     wide = ex.ocean_groups(n, 1, 0x1000, None, n)
-    tall = ex.ocean_mx4(1, n, 64, 0x1000, 32, 0, 0x1000, 4, 0)
-    rows = ex.ocean_mx4(1, n, 64, 0x1000, 32, 0, 0x1000, 4, 0)
+    tall = ex.ocean_mx4(1, n, 64, 0x1000, 32, 0, 0x1000, 16, 0)
+    rows = ex.ocean_mx4(1, n, 64, 0x1000, 32, 0, 0x1000, 16, 0)
     for rc in (lambda d: product(b(wide), d, 0x1000, 64, b(tall), 0, 0x1000, n, None), lambda d: both(b(wide), b(rows), b(tall), d, 0x1000, n, None)):
         for dtype in (1, 2, 3):
             assert rc(dtype) == 1 and "tiles" in lib.ocean_last_error().decode()
@@ -103,7 +105,9 @@ def test_refusals_of_the_balance(ex):
     forward, backward = lib.ocean_route_balance, lib.ocean_route_balance_backward
     none = ex.ocean_routing(10, 4, 2, 0, 0x1000, 0x1000, 0x1000, None, 0x1000, 0x1000)
     bare = ex.ocean_routing(10, 4, 2, 0, 0x1000, 0x1000, None, 0x1000, 0x1000, 0x1000)
-    for rc, word in ((lambda: forward(None, 0x1000, 1, 4, b(out), 0x1000, need, None), "null"), (lambda: forward(b(r), 0x1000, 0, 4, b(out), 0x1000, need, None), "dtype"),
+    for rc, word in ((lambda: forward(b(r), 0x1000, 1, 1 << 23, b(out), 0x1000, need, None), "2^23"),
+                     (lambda: backward(b(out), b(r), 0x1000, 1, 4, 0x1000, None, 1, 0x1000, 1 << 23, None), "2^23"),
+                     (lambda: forward(None, 0x1000, 1, 4, b(out), 0x1000, need, None), "null"), (lambda: forward(b(r), 0x1000, 0, 4, b(out), 0x1000, need, None), "dtype"),
                      (lambda: forward(b(none), 0x1000, 1, 4, b(out), 0x1000, need, None), "expert_ptr"), (lambda: forward(b(r), 0x1000, 1, 3, b(out), 0x1000, need, None), "stride"),
                      (lambda: forward(b(r), None, 1, 4, b(out), 0x1000, need, None), "null"), (lambda: forward(b(r), 0x1000, 1, 4, None, 0x1000, need, None), "balance"),
                      (lambda: forward(b(r), 0x1000, 1, 4, b(ex.ocean_balance(0x1000, None, 0x1000, 0x1000)), 0x1000, need, None), "balance"),
@@ -121,18 +125,18 @@ def test_matrices_in_four_bits_without_a_gpu(ex):
     import pickle
     import torch
     u8 = torch.uint8
-    codes, scales = torch.zeros(3, 10, 48, dtype=u8), torch.zeros(3, 10, 4, dtype=u8)
+    codes, scales = torch.zeros(3, 10, 48, dtype=u8), torch.zeros(3, 10, 16, dtype=u8)
     q = ex.Mx4(codes, scales, 70)
     assert q.shape == (3, 10, 70) and ex.Mx4(codes[0], scales[0], 96).shape == (10, 96)
     for c in (copy.deepcopy(q), pickle.loads(pickle.dumps(q))):
         assert c.shape == q.shape and c._struct.codes == c.codes.data_ptr() != q.codes.data_ptr()
     s = ex.Mx4(codes[1:, 2:], scales[1:, 2:], 70)._struct
-    assert (s.count, s.rows, s.inner, s.ld_codes, s.stride_codes, s.ld_scales, s.stride_scales) == (2, 8, 70, 48, 480, 4, 40)
-    assert s.codes == codes.data_ptr() + 480 + 96 and s.scales == scales.data_ptr() + 40 + 8
+    assert (s.count, s.rows, s.inner, s.ld_codes, s.stride_codes, s.ld_scales, s.stride_scales) == (2, 8, 70, 48, 480, 16, 160)
+    assert s.codes == codes.data_ptr() + 480 + 96 and s.scales == scales.data_ptr() + 160 + 32
     for bad in (lambda: ex.Mx4(codes, scales, 64), lambda: ex.Mx4(codes, scales, 97), lambda: ex.Mx4(codes, scales[..., :3], 70), lambda: ex.Mx4(codes.int(), scales, 70),
                 lambda: ex.Mx4(codes, scales[:2], 70), lambda: ex.Mx4(codes[0, 0], scales[0, 0], 70), lambda: ex.Mx4(codes[..., 8:40], scales, 64),
                 lambda: ex.Mx4(torch.zeros(3, 10, 49, dtype=u8)[..., :48], scales, 70),
-                lambda: ex.Mx4(codes, torch.zeros(3, 10, 8, dtype=u8)[..., 2:6], 70)):
+                lambda: ex.Mx4(codes, torch.zeros(3, 10, 32, dtype=u8)[..., 8:24], 70)):
         with pytest.raises(ValueError):
             bad()
     p = ex.Mx4.laid_out(torch.zeros(3, 10, 49, dtype=u8)[..., :48], torch.ones(3, 10, 3, dtype=u8), 70)
@@ -147,7 +151,7 @@ def test_calls_on_the_cpu_raise(ex):
     if torch.cuda.is_available():
         pytest.skip("a GPU is present")
     x = torch.zeros(4, 64)
-    q = ex.Mx4(torch.zeros(2, 8, 32, dtype=torch.uint8), torch.zeros(2, 8, 4, dtype=torch.uint8), 64)
+    q = ex.Mx4(torch.zeros(2, 8, 32, dtype=torch.uint8), torch.zeros(2, 8, 16, dtype=torch.uint8), 64)
     for call in (lambda: ex.mx4_quantize(x), lambda: ex.mx4_dequantize(q), lambda: ex.grouped_matmul_mx4(x, q, torch.zeros(3, dtype=torch.int64))):
         with pytest.raises((RuntimeError, ValueError)):
             call()

@@ -98,11 +98,11 @@ def test_strides_and_what_lies_beside(ex):
             held = torch.full((3, 10, 77 + extra + off), float("nan"), dtype=dtype, device="cuda")
             held[..., off:off + 77] = x
             codes = torch.full((3, 12, 16 * 5), 9, dtype=torch.uint8, device="cuda")
-            scales = torch.full((3, 11, 12), 9, dtype=torch.uint8, device="cuda")
-            q = ex.mx4_quantize(held[..., off:off + 77], out=ex.Mx4(codes[:, 1:11, 16:64], scales[:, 1:, 4:8], 77))
+            scales = torch.full((3, 11, 48), 9, dtype=torch.uint8, device="cuda")
+            q = ex.mx4_quantize(held[..., off:off + 77], out=ex.Mx4(codes[:, 1:11, 16:64], scales[:, 1:, 16:32], 77))
             assert torch.equal(q.codes, want.codes) and torch.equal(q.scales, want.scales)
             codes[:, 1:11, 16:64] = 9
-            scales[:, 1:, 4:8] = 9
+            scales[:, 1:, 16:32] = 9
             assert bool((codes == 9).all()) and bool((scales == 9).all())
             out = torch.full((3, 10, 77 + extra + off), 7.0, dtype=dtype, device="cuda")
             ex.mx4_dequantize(want, out=out[..., off:off + 77])
@@ -181,7 +181,7 @@ def test_refusals(ex):
     for call in (lambda: ex.mx4_quantize(x.T), lambda: ex.mx4_quantize(x[0]), lambda: ex.mx4_quantize(x[:5], out=q), lambda: ex.mx4_quantize(x.cpu()),
                  lambda: ex.mx4_dequantize(q, out=torch.empty(6, 63, device="cuda")), lambda: ex.mx4_dequantize(q, torch.float16, out=torch.empty(6, 64, device="cuda")),
                  lambda: ex.mx4_dequantize(q, out=torch.empty(6, 64)),
-                 lambda: ex.mx4_quantize(x.expand(2, 6, 64), out=ex.Mx4(q.codes.expand(2, 6, 32), q.scales.expand(2, 6, 4), 64))):
+                 lambda: ex.mx4_quantize(x.expand(2, 6, 64), out=ex.Mx4(q.codes.expand(2, 6, 32), q.scales.expand(2, 6, 16), 64))):
         with pytest.raises((ValueError, RuntimeError)):
             call()
     with pytest.raises(TypeError):

@@ -48,7 +48,7 @@ def _four(ex, gen, *shape, spread=3, pitch=0):
     inner = shape[-1]
     blocks = (inner + 31) // 32
     codes = torch.randint(0, 256, (*shape[:-1], blocks * 16), generator=gen).to(torch.uint8)
-    scales = torch.randint(0, 256, (*shape[:-1], (blocks + 3) // 4 * 4 + pitch), generator=gen).to(torch.uint8)
+    scales = torch.randint(0, 256, (*shape[:-1], (blocks + 15) // 16 * 16 + pitch), generator=gen).to(torch.uint8)
     scales[..., :blocks] = (127 - spread + torch.randint(0, 2 * spread + 1, (*shape[:-1], blocks), generator=gen)).to(torch.uint8)
     return ex.Mx4(codes.cuda(), scales.cuda(), inner), X.values(X.unpack(codes.numpy()), scales[..., :blocks].numpy().astype(np.int64), inner)
 
@@ -180,9 +180,9 @@ def test_small_inner_products_beside_large_ones(ex):
     g = torch.Generator().manual_seed(9)
     for sizes, N in (([4], 40), ([300], 300)):
         codes = torch.randint(0, 256, (1, N, 64), generator=g).to(torch.uint8)
-        scales = torch.full((1, N, 4), 127, dtype=torch.uint8)
+        scales = torch.full((1, N, 16), 127, dtype=torch.uint8)
         scales[:, :, 0], scales[:, :, 1], scales[:, :, 2] = 160, 100, 80
-        w, value = ex.Mx4(codes.cuda(), scales.cuda(), 128), X.values(X.unpack(codes.numpy()), scales.numpy().astype(np.int64), 128)
+        w, value = ex.Mx4(codes.cuda(), scales.cuda(), 128), X.values(X.unpack(codes.numpy()), scales[..., :4].numpy().astype(np.int64), 128)
         x = _rand(g, sum(sizes), 128, dtype="float16")
         x[:, :32], x[:, 96:] = 0, 0
         x[:, 32:64] *= 1000
@@ -298,9 +298,9 @@ def test_strides_and_alignment(ex, dtype):
             return big[..., off:off + t.shape[-1]]
 
         codes = torch.full((3, N + 2, 16 * 7), 255, dtype=torch.uint8, device="cuda")
-        scales = torch.full((3, N + 1, 16), 255, dtype=torch.uint8, device="cuda")
-        codes[:, 1:-1, 16:96], scales[:, 1:, 4:12] = w.codes, w.scales
-        v = ex.Mx4(codes[:, 1:-1, 16:96], scales[:, 1:, 4:12], K)
+        scales = torch.full((3, N + 1, 48), 255, dtype=torch.uint8, device="cuda")
+        codes[:, 1:-1, 16:96], scales[:, 1:, 16:32] = w.codes, w.scales
+        v = ex.Mx4(codes[:, 1:-1, 16:96], scales[:, 1:, 16:32], K)
         for off, extra in ((8, 64), (1, 3), (4, 12), (0, 1), (2, 66)):
             out = torch.full((S, N + extra), 7.0, device="cuda", dtype=x.dtype)
             ex.grouped_matmul_mx4(held(x, off, extra), v, ptr, out=out[:, off:off + N])
