@@ -35,6 +35,23 @@ template <class T> __device__ __forceinline__ void mx4_widen(uint32_t codes, flo
     pair(std::integral_constant<int, 3>{});
 }
 
+// The same as a fragment of the matrix instructions; float16 has all numbers whose scale is not far (below).
+template <class T> __device__ __forceinline__ Frag<T> mx4_fragment(uint32_t codes, float scale)
+{
+    if constexpr (std::is_same<T, f16_t>::value) {
+        const mx_f16x2 a = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(codes, scale, 0), b = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(codes, scale, 1),
+                       c = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(codes, scale, 2), d = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(codes, scale, 3);
+        return f16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
+    } else {
+        bf16_t e[8];
+        mx4_widen<bf16_t>(codes, scale, e);
+        return bf16x8{e[0], e[1], e[2], e[3], e[4], e[5], e[6], e[7]};
+    }
+}
+// Whether float16 does not hold numbers of this scale: 6 * 2^(s - 127) is beyond it from 141 on, 2^(s - 128) is below its 2^-24 up to 103.  Numbers of scales up to
+// 51 count as 0 there: 2^31 products of them with float16 numbers come to less than half its least number.  (255 stays NaN.)
+__device__ __forceinline__ bool mx4_far(uint32_t s) { return (s > 140u && s != 255u) || (s > 51u && s < 104u); }
+
 // And back.
 template <class T> __device__ __forceinline__ uint32_t mx4_narrow(const T (&x)[8], float scale)
 {

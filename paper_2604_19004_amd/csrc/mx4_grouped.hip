@@ -1,7 +1,8 @@
 // Products of ragged groups of rows with their group's matrix in four bits, rows in their own type.
 //
-// Every number of four bits is a bfloat16 number, every float16 number the sum of two and every single precision number of three: so all products are
-// made by the bfloat16 matrix instructions, x in 1, 2 or 3 parts (exactly: single precision at a third of their rate is three times that of its own).
+// Every number of four bits is a bfloat16 number, every float16 number the sum of two and every single precision number of three: so all products can be
+// made by the bfloat16 matrix instructions, x in 1, 2 or 3 parts (exactly: single precision at a third of their rate is three times that of its own).  float16 goes
+// through its own as long as it holds the matrix's numbers (mx4_far), and through two parts where it does not.
 #include "mx4_tiles.hpp"
 
 namespace ocean {
@@ -32,15 +33,40 @@ template <class T> __device__ __forceinline__ void split(const T (&x)[8], bf16x8
     }
 }
 
-// A tile: x straight to LDS (bfloat16, whole pieces) or through registers, where it is split; the matrix's codes through registers, where they are widened.
+// Whether a tile has a scale that float16 does not take; every thread calls it.
+template <bool RCOL, int BN, int THREADS> __device__ __forceinline__ bool any_far(const Mx4Args &m, const uint8_t *scales, int n0, int64_t n, int depth)
+{
+    bool far = false;
+    if constexpr (RCOL) {   // (BN / 32 blocks of every line)
+        constexpr int BLOCKS = BN / MX4_BLOCK;
+        const int block = min(n0 / MX4_BLOCK + (int)threadIdx.x % BLOCKS, m.blocks - 1);
+#pragma unroll 4
+        for (int c = threadIdx.x / BLOCKS; c < depth; c += THREADS / BLOCKS) far |= mx4_far(scales[c * m.ld_scales + block]);
+    } else {
+        constexpr int EACH = 8;   // threads a line
+        for (int i = threadIdx.x / EACH; i < min((int64_t)BN, n - n0); i += THREADS / EACH)
+#pragma unroll 2
+            for (int b = threadIdx.x % EACH * 16; b < m.blocks; b += EACH * 16) {
+                const uint4 v = *reinterpret_cast<const uint4 *>(scales + (n0 + i) * m.ld_scales + b);
+                const uint32_t words[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+                for (int k = 0; k < 16; ++k) far |= b + k < m.blocks && mx4_far(words[k / 4] >> k % 4 * 8 & 255u);
+            }
+    }
+    return __syncthreads_or(far);
+}
+
+// A tile: x straight to LDS (16 bits, whole pieces) or through registers, where single precision is split; the matrix's codes through registers, where they are widened.
 template <class T, bool RCOL, int BM, int BN, int WAVES_M, int WAVES_N, bool ASYNC>
 __global__ void __launch_bounds__(WAVES_M * WAVES_N * WAVE, 2) k_gmm_mx4(GmmArgs a, Mx4Args m, int nt)
 {
-    constexpr int THREADS = WAVES_M * WAVES_N * WAVE, WM = BM / WAVES_M, WN = BN / WAVES_N, TM = WM / 16, TN = WN / 16, PARTS = PARTS_OF<T>;
-    constexpr int STEP_C = STEP<bf16_t>;
+    constexpr int THREADS = WAVES_M * WAVES_N * WAVE, WM = BM / WAVES_M, WN = BN / WAVES_N, TM = WM / 16, TN = WN / 16, PARTS = sizeof(T) == 4 ? 3 : 1;
+    using S = std::conditional_t<sizeof(T) == 4, bf16_t, T>;   // what LDS holds (float16 with far scales: of the matrix, bfloat16)
+    constexpr bool HALF = std::is_same<T, f16_t>::value;
+    constexpr int STEP_C = STEP<S>;
     static_assert(!ASYNC || PARTS == 1, "parts are made in registers");
-    using TL = Tile<bf16_t, false, false, BM, THREADS, LINE>;
-    using TR = Tile<bf16_t, RCOL, !RCOL, BN, THREADS, LINE>;
+    using TL = Tile<S, false, false, BM, THREADS, LINE>;
+    using TR = Tile<S, RCOL, !RCOL, BN, THREADS, LINE>;
     constexpr int BUFFER = PARTS * TL::BYTES + TR::BYTES;
     // A thread's share of the matrix's step: E numbers of a line side by side, in one block.
     constexpr int E = BN * STEP_C / THREADS, WORDS = E / 8, A_LINE = (RCOL ? BN : STEP_C) / E;
@@ -77,124 +103,153 @@ __global__ void __launch_bounds__(WAVES_M * WAVES_N * WAVE, 2) k_gmm_mx4(GmmArgs
         scale_off = (uint32_t)n * (uint32_t)m.ld_scales + part * E / MX4_BLOCK;
     }
 
-    struct Raw { uint4 v[sizeof(T) / 2]; };
-    Raw kept[ASYNC ? 1 : TL::LOADS];
-    uint32_t kept_codes[WORDS], kept_scale = 0;
-    // Workgroups begin at different steps and go round, so that they don't all read lines that begin in the same memory channels; what is left
-    // of the lines behind whole steps comes last.
-    const int whole = depth / STEP_C, turn = whole == 0 ? 0 : (w.n0 / BN + w.group * 5) % whole;
-    auto at = [&](int t) { return t == whole ? t : t + turn >= whole ? t + turn - whole : t + turn; };
-    auto fetch = [&](int t_) {
-        const int t = at(t_), c0 = t * STEP_C, left = min(STEP_C, depth - c0);
-        const bool there = RCOL ? line < left : c0 + part * E < m.blocks * MX4_BLOCK;
-        const Memory code_memory = memory_at(RCOL ? codes + (int64_t)c0 * m.ld_codes : codes), scale_memory = memory_at(RCOL ? scales + (int64_t)c0 * m.ld_scales : scales);
-        const uint32_t code_at = there ? code_off : NOWHERE, scale_at = there ? scale_off : NOWHERE;   // (zeros: a code of 0 is 0 at any scale but NaN)
-        if constexpr (WORDS == 4) {
-            const u32x4 v = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(code_memory, code_at, RCOL ? 0 : c0 / 2, 0));
+    // (float16 with far scales is a walk of its own: beside the other one, its registers would be that one's too)
+    auto run = [&](auto far) {
+        constexpr bool WIDE = decltype(far)::value;
+        struct Raw { uint4 v[sizeof(T) / 2]; };
+        Raw kept[ASYNC ? 1 : TL::LOADS];
+        uint32_t kept_codes[WORDS], kept_scale = 0;
+        // Workgroups begin at different steps and go round, so that they don't all read lines that begin in the same memory channels; what is left
+        // of the lines behind whole steps comes last.
+        const int whole = depth / STEP_C, turn = whole == 0 ? 0 : (w.n0 / BN + w.group * 5) % whole;
+        auto at = [&](int t) { return t == whole ? t : t + turn >= whole ? t + turn - whole : t + turn; };
+        auto fetch = [&](int t_) {
+            const int t = at(t_), c0 = t * STEP_C, left = min(STEP_C, depth - c0);
+            const bool there = RCOL ? line < left : c0 + part * E < m.blocks * MX4_BLOCK;
+            const Memory code_memory = memory_at(RCOL ? codes + (int64_t)c0 * m.ld_codes : codes), scale_memory = memory_at(RCOL ? scales + (int64_t)c0 * m.ld_scales : scales);
+            const uint32_t code_at = there ? code_off : NOWHERE, scale_at = there ? scale_off : NOWHERE;   // (zeros: a code of 0 is 0 at any scale but NaN)
+            if constexpr (WORDS == 4) {
+                const u32x4 v = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(code_memory, code_at, RCOL ? 0 : c0 / 2, 0));
 #pragma unroll
-            for (int j = 0; j < 4; ++j) kept_codes[j] = v[j];
-        } else {
-            const auto v = __builtin_amdgcn_raw_buffer_load_b64(code_memory, code_at, RCOL ? 0 : c0 / 2, 0);
-            kept_codes[0] = v[0], kept_codes[1] = v[1];
-        }
-        kept_scale = __builtin_amdgcn_raw_buffer_load_b8(scale_memory, scale_at, RCOL ? 0 : c0 / MX4_BLOCK, 0);
-        if constexpr (ASYNC) {
-            char *to = lds + (t_ & 1) * BUFFER + wave * (WAVE * 16);
-#pragma unroll
-            for (int i = 0; i < TL::LOADS; ++i)
-                memory_to_lds<16>(x_memory, TL::piece_of(tid, i) * 8 < left ? off[i] : NOWHERE, (uint32_t)c0 * 2, to + i * THREADS * 16);
-        } else {
-            const T *x = static_cast<const T *>(a.l) + c0;
-#pragma unroll
-            for (int i = 0; i < TL::LOADS; ++i) {
-                const T *p = x + row[i] + TL::piece_of(tid, i) * 8;
-                const int valid = left - TL::piece_of(tid, i) * 8;
-#pragma unroll
-                for (int j = 0; j < (int)sizeof(T) / 2; ++j)
-                    kept[i].v[j] = left == STEP_C ? load_any(reinterpret_cast<const char *>(p + j * PIECE<T>)) : load_piece(p + j * PIECE<T>, valid - j * PIECE<T>);
+                for (int j = 0; j < 4; ++j) kept_codes[j] = v[j];
+            } else {
+                const auto v = __builtin_amdgcn_raw_buffer_load_b64(code_memory, code_at, RCOL ? 0 : c0 / 2, 0);
+                kept_codes[0] = v[0], kept_codes[1] = v[1];
             }
-        }
-    };
-    auto stash = [&](int t_) {
-        char *to = lds + (t_ & 1) * BUFFER;
-        if constexpr (!ASYNC) {
+            kept_scale = __builtin_amdgcn_raw_buffer_load_b8(scale_memory, scale_at, RCOL ? 0 : c0 / MX4_BLOCK, 0);
+            if constexpr (ASYNC) {
+                char *to = lds + (t_ & 1) * BUFFER + wave * (WAVE * 16);
 #pragma unroll
-            for (int i = 0; i < TL::LOADS; ++i) {
-                bf16x8 p[PARTS];
-                split<T>(__builtin_bit_cast(decltype(Vec<T, 8>{}), kept[i]).e, p);
+                for (int i = 0; i < TL::LOADS; ++i)
+                    memory_to_lds<16>(x_memory, TL::piece_of(tid, i) * 8 < left ? off[i] : NOWHERE, (uint32_t)c0 * 2, to + i * THREADS * 16);
+            } else {
+                const T *x = static_cast<const T *>(a.l) + c0;
 #pragma unroll
-                for (int k = 0; k < PARTS; ++k) *reinterpret_cast<bf16x8 *>(to + k * TL::BYTES + (i * THREADS + tid) * 16) = p[k];
+                for (int i = 0; i < TL::LOADS; ++i) {
+                    const T *p = x + row[i] + TL::piece_of(tid, i) * 8;
+                    const int valid = left - TL::piece_of(tid, i) * 8;
+#pragma unroll
+                    for (int j = 0; j < (int)sizeof(T) / 2; ++j)
+                        kept[i].v[j] = left == STEP_C ? load_any(reinterpret_cast<const char *>(p + j * PIECE<T>)) : load_piece(p + j * PIECE<T>, valid - j * PIECE<T>);
+                }
             }
-        }
-        if constexpr (!RCOL) {
-            const int valid = depth - (at(t_) * STEP_C + part * E);
-            if (valid < E) {   // (codes behind the end meet zeros of x, but may be infinite numbers)
+        };
+        auto stash = [&](int t_) {
+            char *to = lds + (t_ & 1) * BUFFER;
+            if constexpr (!ASYNC) {
 #pragma unroll
-                for (int j = 0; j < WORDS; ++j) kept_codes[j] = mx4_first(kept_codes[j], valid - j * 8);
+                for (int i = 0; i < TL::LOADS; ++i) {
+                    if constexpr (PARTS == 1) {
+                        *reinterpret_cast<uint4 *>(to + (i * THREADS + tid) * 16) = kept[i].v[0];
+                    } else {
+                        bf16x8 p[PARTS];
+                        split<T>(__builtin_bit_cast(decltype(Vec<T, 8>{}), kept[i]).e, p);
+#pragma unroll
+                        for (int k = 0; k < PARTS; ++k) *reinterpret_cast<bf16x8 *>(to + k * TL::BYTES + (i * THREADS + tid) * 16) = p[k];
+                    }
+                }
             }
-        }
-        const int swizzle = RCOL ? col_xor<bf16_t, TR::PIECES>(line) : row_xor<!RCOL, TR::PIECES>(line);
-        char *to_line = to + PARTS * TL::BYTES + line * TR::PIECES * 16;
-        const float scale = mx4_scale(kept_scale);
+            if constexpr (!RCOL) {
+                const int valid = depth - (at(t_) * STEP_C + part * E);
+                if (valid < E) {   // (codes behind the end meet zeros of x, but may be infinite numbers)
 #pragma unroll
-        for (int j = 0; j < WORDS; ++j) {
-            bf16_t v[8];
-            mx4_widen<bf16_t>(kept_codes[j], scale, v);
-            *reinterpret_cast<bf16x8 *>(to_line + ((part * WORDS + j) ^ swizzle) * 16) = bf16x8{v[0], v[1], v[2], v[3], v[4], v[5], v[6], v[7]};
-        }
-    };
+                    for (int j = 0; j < WORDS; ++j) kept_codes[j] = mx4_first(kept_codes[j], valid - j * 8);
+                }
+            }
+            const int swizzle = RCOL ? col_xor<S, TR::PIECES>(line) : row_xor<!RCOL, TR::PIECES>(line);
+            char *to_line = to + PARTS * TL::BYTES + line * TR::PIECES * 16;
+            const float scale = mx4_scale(kept_scale);
+            auto widen = [&](auto type) {
+                using W = decltype(type);
+#pragma unroll
+                for (int j = 0; j < WORDS; ++j)
+                    *reinterpret_cast<Frag<W> *>(to_line + ((part * WORDS + j) ^ swizzle) * 16) = mx4_fragment<W>(kept_codes[j], scale);
+            };
+            widen(std::conditional_t<WIDE, bf16_t, S>{});
+        };
 
-    const uint32_t at_l = TL::place(wm), at_r = TR::place(wn);
-    f32x4 acc[TM][TN] = {};
-    // (single precision: the sums of 256 products are put aside, as in k_gmm)
-    constexpr bool ASIDE = sizeof(T) == 4;
-    f32x4 sums[ASIDE ? TM : 1][ASIDE ? TN : 1] = {};
-    auto put_aside = [&] {
+        const uint32_t at_l = TL::place(wm), at_r = TR::place(wn);
+        f32x4 acc[TM][TN] = {};
+        // (single precision: the sums of 256 products are put aside, as in k_gmm)
+        constexpr bool ASIDE = sizeof(T) == 4;
+        f32x4 sums[ASIDE ? TM : 1][ASIDE ? TN : 1] = {};
+        auto put_aside = [&] {
+            if constexpr (ASIDE) {
+#pragma unroll
+                for (int i = 0; i < TM; ++i)
+#pragma unroll
+                    for (int j = 0; j < TN; ++j) {
+                        sums[i][j] += acc[i][j];
+                        acc[i][j] = f32x4{};
+                    }
+            }
+        };
+        auto multiply = [&](int buffer) {
+            const char *from = lds + buffer * BUFFER;
+            auto half = [&](auto h) {
+                Frag<S> fr[TN], fl[TM];
+                TR::template read<decltype(h)::value>(from + PARTS * TL::BYTES, at_r, fr);
+#pragma unroll
+                for (int p = PARTS - 1; p >= 0; --p) {
+                    TL::template read<decltype(h)::value>(from + p * TL::BYTES, at_l, fl);
+                    if constexpr (WIDE) {
+#pragma unroll
+                        for (int i = 0; i < TM; ++i) {
+                            bf16x8 x[PARTS_OF<f16_t>];
+                            split<f16_t>(__builtin_bit_cast(decltype(Vec<f16_t, 8>{}), fl[i]).e, x);
+#pragma unroll
+                            for (int k = PARTS_OF<f16_t> - 1; k >= 0; --k)
+#pragma unroll
+                                for (int j = 0; j < TN; ++j) mma_part(acc[i][j], __builtin_bit_cast(bf16x8, fr[j]), x[k], 0);
+                            __builtin_amdgcn_sched_barrier(0);   // (one after the other: this is not to cost the other path registers)
+                        }
+                    } else {
+                        mma<S>(acc, fr, fl);
+                    }
+                }
+            };
+            half(std::integral_constant<int, 0>{});
+            half(std::integral_constant<int, 1>{});
+        };
+        if (steps > 0) {
+            fetch(0);
+            stash(0);
+        }
+        for (int t = 0; t < steps; ++t) {
+            asm volatile("" ::: "memory");
+            __builtin_amdgcn_s_waitcnt(0x0070);   // vmcnt(0), lgkmcnt(0): this wave's part of the step is in LDS, and what it read of the step before has come
+            __builtin_amdgcn_s_barrier();
+            asm volatile("" ::: "memory");
+            if (t + 1 < steps) fetch(t + 1);
+            multiply(t & 1);
+            if (ASIDE && t % 4 == 3) put_aside();
+            if (t + 1 < steps) stash(t + 1);
+        }
         if constexpr (ASIDE) {
 #pragma unroll
             for (int i = 0; i < TM; ++i)
 #pragma unroll
-                for (int j = 0; j < TN; ++j) {
-                    sums[i][j] += acc[i][j];
-                    acc[i][j] = f32x4{};
-                }
+                for (int j = 0; j < TN; ++j) acc[i][j] += sums[i][j];
         }
+        store_tile<T, BM, BN, WAVES_M, WAVES_N, !RCOL, sizeof(lds)>(a, w, acc, lds);
     };
-    auto multiply = [&](int buffer) {
-        const char *from = lds + buffer * BUFFER;
-        auto half = [&](auto h) {
-            Frag<bf16_t> fr[TN], fl[TM];
-            TR::template read<decltype(h)::value>(from + PARTS * TL::BYTES, at_r, fr);
-#pragma unroll
-            for (int p = PARTS - 1; p >= 0; --p) {
-                TL::template read<decltype(h)::value>(from + p * TL::BYTES, at_l, fl);
-                mma<bf16_t>(acc, fr, fl);
-            }
-        };
-        half(std::integral_constant<int, 0>{});
-        half(std::integral_constant<int, 1>{});
-    };
-    if (steps > 0) {
-        fetch(0);
-        stash(0);
+    if constexpr (HALF) {
+        if (any_far<RCOL, BN, THREADS>(m, m.scales + w.group * m.stride_scales, w.n0, a.n, depth)) {
+            run(std::true_type{});
+            return;
+        }
     }
-    for (int t = 0; t < steps; ++t) {
-        asm volatile("" ::: "memory");
-        __builtin_amdgcn_s_waitcnt(0x0070);   // vmcnt(0), lgkmcnt(0): this wave's part of the step is in LDS, and what it read of the step before has come
-        __builtin_amdgcn_s_barrier();
-        asm volatile("" ::: "memory");
-        if (t + 1 < steps) fetch(t + 1);
-        multiply(t & 1);
-        if (ASIDE && t % 4 == 3) put_aside();
-        if (t + 1 < steps) stash(t + 1);
-    }
-    if constexpr (ASIDE) {
-#pragma unroll
-        for (int i = 0; i < TM; ++i)
-#pragma unroll
-            for (int j = 0; j < TN; ++j) acc[i][j] += sums[i][j];
-    }
-    store_tile<T, BM, BN, WAVES_M, WAVES_N, !RCOL, sizeof(lds)>(a, w, acc, lds);
+    run(std::false_type{});
 }
 
 // Few rows: the matrix is read once, straight into registers.  A lane's 32 numbers of c are those of its block, in four matrix instructions; x is read
@@ -231,15 +286,15 @@ __global__ void __launch_bounds__(WAVES * WAVE, 2) k_few_mx4(GmmArgs a, Mx4Args 
         for (int i = 0; i < TM; ++i) x[i] = static_cast<const T *>(a.l) + max(s_row[min(i * 16 + r, rows - 1)], (int64_t)0) * a.ldl + g * MX4_BLOCK;
         f32x4 acc[TM][TN] = {};
         struct Eight { uint4 v[sizeof(T) / 2]; };
-        // U steps from t0 on; END: some of them may reach behind the lines' end.
-        auto multiply = [&](int t0, auto end) {
-            constexpr bool END = decltype(end)::value;
+        // U steps from t0 on.  ANY: some of them may reach behind the lines' end, and float16 goes in parts.
+        auto multiply = [&](int t0, auto any) {
+            constexpr bool ANY = decltype(any)::value;
+            using W = std::conditional_t<!ANY && sizeof(T) == 2, T, bf16_t>;   // (what the matrix's numbers become)
             Eight xs[U][TM][4];
 #pragma unroll
             for (int u = 0; u < U; ++u) {
-                const T *at = nullptr;
                 int valid = MX4_BLOCK;
-                if constexpr (END) {
+                if constexpr (ANY) {
                     valid = t0 + u < steps ? (int)max(min(a.c - ((int64_t)(t0 + u) * 128 + g * MX4_BLOCK), (int64_t)MX4_BLOCK), (int64_t)0) : 0;
                     b.end(u, valid);
                 }
@@ -249,31 +304,35 @@ __global__ void __launch_bounds__(WAVES * WAVE, 2) k_few_mx4(GmmArgs a, Mx4Args 
                     for (int q = 0; q < 4; ++q)
 #pragma unroll
                         for (int p = 0; p < (int)sizeof(T) / 2; ++p) {
-                            at = x[i] + (int64_t)(t0 + u) * 128 + q * 8 + p * PIECE<T>;
-                            xs[u][i][q].v[p] = END ? load_piece(at, valid - q * 8 - p * PIECE<T>) : load_any(reinterpret_cast<const char *>(at));
+                            const T *at = x[i] + (int64_t)(t0 + u) * 128 + q * 8 + p * PIECE<T>;
+                            xs[u][i][q].v[p] = ANY ? load_piece(at, valid - q * 8 - p * PIECE<T>) : load_any(reinterpret_cast<const char *>(at));
                         }
             }
 #pragma unroll
             for (int u = 0; u < U; ++u)
 #pragma unroll
                 for (int q = 0; q < 4; ++q) {
-                    Frag<bf16_t> fw[TN];
+                    Frag<W> fw[TN];
 #pragma unroll
                     for (int j = 0; j < TN; ++j) {
                         const uint4 &v = b.v[u][j];
-                        bf16_t e[8];
-                        mx4_widen<bf16_t>(q == 0 ? v.x : q == 1 ? v.y : q == 2 ? v.z : v.w, mx4_scale(b.scale(u, j, g)), e);
-                        fw[j] = bf16x8{e[0], e[1], e[2], e[3], e[4], e[5], e[6], e[7]};
+                        fw[j] = mx4_fragment<W>(q == 0 ? v.x : q == 1 ? v.y : q == 2 ? v.z : v.w, mx4_scale(b.scale(u, j, g)));
                     }
 #pragma unroll
                     for (int i = 0; i < TM; ++i) {
-                        bf16x8 p[PARTS];
-                        split<T>(__builtin_bit_cast(decltype(Vec<T, 8>{}), xs[u][i][q]).e, p);
+                        if constexpr (std::is_same<T, W>::value) {
 #pragma unroll
-                        for (int k = PARTS - 1; k >= 0; --k)
+                            for (int j = 0; j < TN; ++j) mma_part(acc[i][j], fw[j], __builtin_bit_cast(Frag<W>, xs[u][i][q].v[0]), 0);
+                        } else {
+                            bf16x8 p[PARTS];
+                            split<T>(__builtin_bit_cast(decltype(Vec<T, 8>{}), xs[u][i][q]).e, p);
 #pragma unroll
-                            for (int j = 0; j < TN; ++j) mma_part(acc[i][j], fw[j], p[k], 0);
+                            for (int k = PARTS - 1; k >= 0; --k)
+#pragma unroll
+                                for (int j = 0; j < TN; ++j) mma_part(acc[i][j], fw[j], p[k], 0);
+                        }
                     }
+                    if (ANY) __builtin_amdgcn_sched_barrier(0);   // (so that this takes no more registers than the other one)
                 }
         };
         for (int pass = 0; pass * WAVES * 4 < steps; ++pass) {
@@ -289,7 +348,15 @@ __global__ void __launch_bounds__(WAVES * WAVE, 2) k_few_mx4(GmmArgs a, Mx4Args 
 #pragma unroll
                 for (int j = 0; j < TN; ++j) words[j] = s_scales[pass & 1] + (j * 16 + r) * FewScales<TN, WAVES>::PITCH + (wave * 4 + i) * 4;
                 b.load_scales(words);
-                if (t + U <= whole) multiply(t, std::false_type{});
+                bool far = false;
+                if constexpr (std::is_same<T, f16_t>::value) {
+#pragma unroll
+                    for (int u = 0; u < U; ++u)
+#pragma unroll
+                        for (int j = 0; j < TN; ++j) far |= mx4_far(b.scale(u, j, g));
+                    far = __any(far);
+                }
+                if (t + U <= whole && !far) multiply(t, std::false_type{});
                 else multiply(t, std::true_type{});
                 if (t_next < steps) b.load(codes, t_next, g, m.blocks);
             }
@@ -328,7 +395,7 @@ template <class T, bool RCOL> hipError_t pick(const GmmArgs &a, const Mx4Args &m
             });
         }
     }
-    if constexpr (std::is_same<T, bf16_t>::value) {
+    if constexpr (sizeof(T) == 2) {
         if (straight) {
             if (tiles(128, 128) >= 512 && launches<GM_ROWS>(a, 256, 256, 512)) return launch_tile<T, RCOL, 256, 256, 2, 4, true>(a, m, s);
             if (tiles(64, 64) >= 512 || !launches<GM_ROWS>(a, 64, 64, 256)) return launch_tile<T, RCOL, 128, 128, 2, 2, true>(a, m, s);
@@ -355,7 +422,7 @@ hipError_t launch_grouped_mx4(const ocean_groups &g, int dtype, const void *x, i
     const Mx4Args m = mx4_args(w);
     // (the rows of a tile lie within 256 lines, gathered ones anywhere in x)
     // (whole pieces: a piece of x lies before its row's end or behind it)
-    const bool straight = dtype == OCEAN_BF16 && pieces_aligned(x, ldx, 0, 2) && inner % 8 == 0 && offsets_fit(g.row_index ? std::max<int64_t>(g.x_rows, 256) : 256, ldx, 2);
+    const bool straight = dtype != OCEAN_F32 && pieces_aligned(x, ldx, 0, 2) && inner % 8 == 0 && offsets_fit(g.row_index ? std::max<int64_t>(g.x_rows, 256) : 256, ldx, 2);
     return with_type(dtype, [&](auto t) {
         using T = decltype(t);
         return transposed ? pick<T, true>(a, m, straight, s) : pick<T, false>(a, m, straight, s);
