@@ -4,14 +4,14 @@
 
 namespace ocean {
 
-// (codes as bytes: a tile's step of 128 bytes is 256 numbers of c, a fragment of 16 bytes one block)
+// (codes as bytes: 64 bytes of a line are 128 numbers of c, a fragment of 16 bytes one block)
 template <> struct FragOf<uint8_t> { using type = u32x4; };
 
 namespace {
 
 typedef int i32x8 __attribute__((ext_vector_type(8)));
 
-constexpr int STEP_BLOCKS = LINE / 16, HALF_BLOCKS = STEP_BLOCKS / 2;   // blocks of a line in a step, in a matrix instruction
+constexpr int MMA_BLOCKS = 4, STEP_BLOCKS = LINE / 16;   // blocks of a line in a matrix instruction, in a step
 
 __device__ __forceinline__ void mma_mx4(f32x4 &acc, u32x4 a, uint32_t scale_a, u32x4 b, uint32_t scale_b)
 {
@@ -26,15 +26,19 @@ __device__ __forceinline__ u32x4 first_codes(u32x4 v, int valid)
     return v;
 }
 
+// A tile, STAGES steps of 128 bytes of c (256 numbers) of both operands in LDS, and the scales of the periods of two steps that they belong to: 16
+// bytes of a line at a time (4 bytes a step, each a line of memory looked up, cost more than the codes: 32668 rows of 4096 by eight 8192 x 4096 746 us).
 template <class O, int BM, int BN, int WAVES_M, int WAVES_N, int STAGES>
 __global__ void __launch_bounds__(WAVES_M * WAVES_N * WAVE, 2) k_gmm_mx4_mx4(GmmArgs a, Mx4Args x, Mx4Args m, int nt)
 {
     constexpr int THREADS = WAVES_M * WAVES_N * WAVE, WM = BM / WAVES_M, WN = BN / WAVES_N, TM = WM / 16, TN = WN / 16;
     using TL = Tile<uint8_t, false, false, BM, THREADS, LINE>;
     using TR = Tile<uint8_t, false, true, BN, THREADS, LINE>;
-    constexpr int LINES = BM + BN, WORDS = 2 * LINES, SCALE_LOADS = WORDS / THREADS, CODES = TL::BYTES + TR::BYTES, BUFFER = CODES + WORDS * 4;
-    static_assert(WORDS % THREADS == 0, "whole words of scales a thread");
-    __shared__ __align__(16) char lds[STAGES * BUFFER];
+    constexpr int LINES = BM + BN, CODES = TL::BYTES + TR::BYTES, PERIODS = STAGES / 2 + 1, PERIOD_BLOCKS = 2 * STEP_BLOCKS;
+    static_assert(STAGES % 2 == 0 && (LINES % THREADS == 0 || THREADS % LINES == 0), "as many scales a period for all waves");
+    constexpr int SCALE_LOADS = LINES > THREADS ? LINES / THREADS : 1;
+    __shared__ __align__(16) char lds[STAGES * CODES];
+    __shared__ __align__(16) uint32_t s_scales[PERIODS][LINES][4];   // lines of x, then of the matrix
     RowsTile w;
     if (!rows_tile<O>(a, BM, BN, nt, w)) return;
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid / WAVE), lane = lane_id(), r = lane % 16, g = lane / 16;
@@ -49,31 +53,34 @@ __global__ void __launch_bounds__(WAVES_M * WAVES_N * WAVE, 2) k_gmm_mx4_mx4(Gmm
     for (int i = 0; i < TL::LOADS; ++i) off_l[i] = (uint32_t)(tile_row(a, w, TL::line_of(tid, i)) - first) * (uint32_t)x.ld_codes + TL::piece_of(tid, i) * 16;
 #pragma unroll
     for (int i = 0; i < TR::LOADS; ++i) off_r[i] = (uint32_t)min(TR::line_of(tid, i), (int)a.n - 1 - w.n0) * (uint32_t)m.ld_codes + TR::piece_of(tid, i) * 16;
-    // Scales lie in LDS as [half of the step][line of x, then of the matrix], a word of four blocks each; a wave's words are all of one operand and half.
+    // (a wave's lines are all of one operand; where there are more threads than lines, some load the same)
     const uint8_t *l_scales = x.scales + first * x.ld_scales, *r_scales = w_scales + (int64_t)w.n0 * m.ld_scales;
 #pragma unroll
     for (int i = 0; i < SCALE_LOADS; ++i) {
         const int line = (i * THREADS + tid) % LINES;
         off_s[i] = line < BM ? (uint32_t)(tile_row(a, w, line) - first) * (uint32_t)x.ld_scales : (uint32_t)min(line - BM, (int)a.n - 1 - w.n0) * (uint32_t)m.ld_scales;
     }
-    // (the order of the steps is that of k_gmm_mx4)
-    const int whole = (int)(a.c / (STEP_BLOCKS * MX4_BLOCK)), turn = whole == 0 ? 0 : (w.n0 / BN + w.group * 5) % whole;
-    auto at = [&](int t) { return t == whole ? t : t + turn >= whole ? t + turn - whole : t + turn; };
-    auto fetch = [&](int t_, int buffer) {
-        const int t = at(t_), left = depth - t * LINE;
-        char *to = lds + buffer * BUFFER, *to_wave = to + wave * (WAVE * 16);
+    // (the order of the steps is that of k_gmm_mx4, by periods)
+    const int whole = (int)(a.c / (STEP_BLOCKS * MX4_BLOCK)), periods = whole / 2, turn = periods == 0 ? 0 : (w.n0 / BN + w.group * 5) % periods;
+    auto period = [&](int p) { return p >= periods ? p : p + turn >= periods ? p + turn - periods : p + turn; };
+    // (in `parts` parts, the part-th now)
+    auto fetch = [&](int t_, int buffer, auto part_, auto parts_) {
+        constexpr int PART = decltype(part_)::value, PARTS = decltype(parts_)::value;
+        const int p = period(t_ / 2), t = p * 2 + t_ % 2, left = depth - t * LINE;
+        char *to = lds + buffer * CODES + wave * (WAVE * 16);
+        if (PART == 0 && t_ % 2 == 0) {
 #pragma unroll
-        for (int i = 0; i < TL::LOADS; ++i)
-            memory_to_lds<16>(l_codes, TL::piece_of(tid, i) * 16 < left ? off_l[i] : NOWHERE, t * LINE, to_wave + i * THREADS * 16);
-#pragma unroll
-        for (int i = 0; i < TR::LOADS; ++i)
-            memory_to_lds<16>(r_codes, TR::piece_of(tid, i) * 16 < left ? off_r[i] : NOWHERE, t * LINE, to_wave + TL::BYTES + i * THREADS * 16);
-#pragma unroll
-        for (int i = 0; i < SCALE_LOADS; ++i) {
-            const int word = i * THREADS + wave * WAVE, half = word / LINES, block = t * STEP_BLOCKS + half * HALF_BLOCKS;
-            const Memory scales = memory_at(word % LINES < BM ? l_scales : r_scales);
-            memory_to_lds<4>(scales, block < m.blocks ? off_s[i] : NOWHERE, block, to + CODES + word * 4);
+            for (int i = 0; i < SCALE_LOADS; ++i) {
+                const int line = (i * THREADS + wave * WAVE) % LINES;
+                memory_to_lds<16>(memory_at(line < BM ? l_scales : r_scales), off_s[i], p * PERIOD_BLOCKS, reinterpret_cast<char *>(s_scales[t_ / 2 % PERIODS][line]));
+            }
         }
+#pragma unroll
+        for (int i = TL::LOADS * PART / PARTS; i < TL::LOADS * (PART + 1) / PARTS; ++i)
+            memory_to_lds<16>(l_codes, TL::piece_of(tid, i) * 16 < left ? off_l[i] : NOWHERE, t * LINE, to + i * THREADS * 16);
+#pragma unroll
+        for (int i = TR::LOADS * PART / PARTS; i < TR::LOADS * (PART + 1) / PARTS; ++i)
+            memory_to_lds<16>(r_codes, TR::piece_of(tid, i) * 16 < left ? off_r[i] : NOWHERE, t * LINE, to + TL::BYTES + i * THREADS * 16);
     };
 
     // The end of the lines: of this thread's pieces, codes of x behind it become 0 and scales of blocks behind it 1 (an empty block's could be NaN).
@@ -86,9 +93,12 @@ __global__ void __launch_bounds__(WAVES_M * WAVES_N * WAVE, 2) k_gmm_mx4_mx4(Gmm
         }
 #pragma unroll
         for (int i = 0; i < SCALE_LOADS; ++i) {
-            const int word = i * THREADS + tid, there = m.blocks - (t * STEP_BLOCKS + word / LINES * HALF_BLOCKS);
-            uint32_t *scales = reinterpret_cast<uint32_t *>(buffer + CODES + word * 4);
-            if (there < HALF_BLOCKS) *scales = there <= 0 ? 0x7f7f7f7fu : (*scales & ((1u << 8 * there) - 1u)) | 0x7f7f7f7fu << 8 * there;
+            uint32_t *scales = s_scales[t / 2 % PERIODS][(i * THREADS + tid) % LINES];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const int there = m.blocks - (t / 2 * PERIOD_BLOCKS + k * MMA_BLOCKS);
+                if (there < MMA_BLOCKS) scales[k] = there <= 0 ? 0x7f7f7f7fu : (scales[k] & ((1u << 8 * there) - 1u)) | 0x7f7f7f7fu << 8 * there;
+            }
         }
         __builtin_amdgcn_s_waitcnt(0xc07f);   // lgkmcnt(0)
     };
@@ -97,10 +107,10 @@ __global__ void __launch_bounds__(WAVES_M * WAVES_N * WAVE, 2) k_gmm_mx4_mx4(Gmm
     f32x4 acc[TM][TN] = {};
     // A step in portions: 128 numbers of c of all the wave's columns and AT_ONCE of its 16s of rows, the next portion's reads under way meanwhile (all at once
     // don't fit the registers beside the sums).
-    constexpr int AT_ONCE = TM < 4 ? TM : 4, PER_HALF = TM / AT_ONCE, PORTIONS = 2 * PER_HALF;
-    auto multiply = [&](int buffer) {
-        const char *from = lds + buffer * BUFFER;
-        const uint32_t *scales = reinterpret_cast<const uint32_t *>(from + CODES);
+    constexpr int AT_ONCE = TM < 4 ? TM : 4, PER_HALF = TM / AT_ONCE, PORTIONS = 2 * PER_HALF, LOAD_PARTS = 1;
+    auto multiply = [&](int t, int buffer, auto load) {
+        const char *from = lds + buffer * CODES;
+        const uint32_t *scales = s_scales[t / 2 % PERIODS][0] + t % 2 * 2;
         u32x4 fr[2][TN], fl[2][AT_ONCE];
         uint32_t sr[2][TN], sl[2][AT_ONCE];
         auto read = [&](auto portion) {
@@ -108,16 +118,17 @@ __global__ void __launch_bounds__(WAVES_M * WAVES_N * WAVE, 2) k_gmm_mx4_mx4(Gmm
             if constexpr (i0 == 0) {
                 TR::template read<h>(from + TL::BYTES, at_r, fr[h]);
 #pragma unroll
-                for (int j = 0; j < TN; ++j) sr[h][j] = scales[h * LINES + BM + wn + tile_line<true>(j, r)] >> (8 * g);
+                for (int j = 0; j < TN; ++j) sr[h][j] = scales[(BM + wn + tile_line<true>(j, r)) * 4 + h] >> (8 * g);
             }
             TL::template read<h>(from + tile_line<false>(i0, 0) * LINE, at_l, fl[p & 1]);
 #pragma unroll
-            for (int i = 0; i < AT_ONCE; ++i) sl[p & 1][i] = scales[h * LINES + wm + tile_line<false>(i0 + i, r)] >> (8 * g);
+            for (int i = 0; i < AT_ONCE; ++i) sl[p & 1][i] = scales[(wm + tile_line<false>(i0 + i, r)) * 4 + h] >> (8 * g);
         };
         auto portion = [&](auto portion) {
             constexpr int p = decltype(portion)::value, h = p / PER_HALF, i0 = p % PER_HALF * AT_ONCE;
             if constexpr (p < PORTIONS) {
                 if constexpr (p + 1 < PORTIONS) read(std::integral_constant<int, p + 1>{});
+                if constexpr (p < LOAD_PARTS) load(std::integral_constant<int, p>{});
 #pragma unroll
                 for (int i = 0; i < AT_ONCE; ++i)
 #pragma unroll
@@ -133,22 +144,23 @@ __global__ void __launch_bounds__(WAVES_M * WAVES_N * WAVE, 2) k_gmm_mx4_mx4(Gmm
     };
 #pragma unroll
     for (int t = 0; t < STAGES - 1; ++t)
-        if (t < steps) fetch(t, t);
+        if (t < steps) fetch(t, t, std::integral_constant<int, 0>{}, std::integral_constant<int, 1>{});
     int buffer = 0;
     for (int t = 0; t < steps; ++t) {
         // This wave's part of the step is in LDS (loads come back in order: all but those of later steps), and what it read of the step before has
         // come; then everyone's is, and nobody reads the buffer of the step before any more.
-        constexpr int LATER = (STAGES - 2) * (TL::LOADS + TR::LOADS + SCALE_LOADS);
+        constexpr int LATER = (STAGES - 2) * (TL::LOADS + TR::LOADS) + (STAGES - 2) / 2 * SCALE_LOADS;
         static_assert(LATER < 64, "what the counter holds");
         asm volatile("" ::: "memory");
         if (t + STAGES - 2 < steps) __builtin_amdgcn_s_waitcnt(0x0070 | (LATER & 15) | (LATER >> 4) << 14);
         else __builtin_amdgcn_s_waitcnt(0x0070);
         asm volatile("" ::: "memory");
-        if (t == whole) end_lines(t, lds + buffer * BUFFER);
+        if (t == whole) end_lines(t, lds + buffer * CODES);
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
-        if (t + STAGES - 1 < steps) fetch(t + STAGES - 1, buffer == 0 ? STAGES - 1 : buffer - 1);   // (in place of the step before)
-        multiply(buffer);
+        multiply(t, buffer, [&](auto part) {   // (in place of the step before)
+            if (t + STAGES - 1 < steps) fetch(t + STAGES - 1, buffer == 0 ? STAGES - 1 : buffer - 1, part, std::integral_constant<int, LOAD_PARTS>{});
+        });
         buffer = buffer + 1 == STAGES ? 0 : buffer + 1;
     }
     store_tile<O, BM, BN, WAVES_M, WAVES_N, true, sizeof(lds)>(a, w, acc, lds);

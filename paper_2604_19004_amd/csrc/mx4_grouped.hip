@@ -194,32 +194,48 @@ __global__ void __launch_bounds__(WAVES_M * WAVES_N * WAVE, 2) k_gmm_mx4(GmmArgs
                     }
             }
         };
-        auto multiply = [&](int buffer) {
+        // A step in portions: half of its c, one part of x and AT_ONCE of the wave's 16s of rows, the next portion's reads under way meanwhile; load() brings the next
+        // step on its way behind the first reads (before them, the waves wait for its addresses to be taken).
+        constexpr int AT_ONCE = TM < 4 ? TM : 4, PER_PART = TM / AT_ONCE, PER_HALF = PARTS * PER_PART, PORTIONS = 2 * PER_HALF;
+        auto multiply = [&](int buffer, auto load) {
             const char *from = lds + buffer * BUFFER;
-            auto half = [&](auto h) {
-                Frag<S> fr[TN], fl[TM];
-                TR::template read<decltype(h)::value>(from + PARTS * TL::BYTES, at_r, fr);
+            Frag<S> fr[2][TN], fl[2][AT_ONCE];
+            auto read = [&](auto portion) {
+                constexpr int q = decltype(portion)::value, h = q / PER_HALF, p = PARTS - 1 - q % PER_HALF / PER_PART, i0 = q % PER_PART * AT_ONCE;
+                if constexpr (q % PER_HALF == 0) TR::template read<h>(from + PARTS * TL::BYTES, at_r, fr[h]);
+                TL::template read<h>(from + p * TL::BYTES + tile_line<false>(i0, 0) * LINE, at_l, fl[q & 1]);
+            };
+            auto portion = [&](auto portion) {
+                constexpr int q = decltype(portion)::value, h = q / PER_HALF, i0 = q % PER_PART * AT_ONCE;
+                if constexpr (q < PORTIONS) {
+                    if constexpr (q + 1 < PORTIONS) read(std::integral_constant<int, q + 1>{});
+                    if constexpr (q == 0) load();
 #pragma unroll
-                for (int p = PARTS - 1; p >= 0; --p) {
-                    TL::template read<decltype(h)::value>(from + p * TL::BYTES, at_l, fl);
-                    if constexpr (WIDE) {
-#pragma unroll
-                        for (int i = 0; i < TM; ++i) {
+                    for (int i = 0; i < AT_ONCE; ++i) {
+                        if constexpr (WIDE) {
                             bf16x8 x[PARTS_OF<f16_t>];
-                            split<f16_t>(__builtin_bit_cast(decltype(Vec<f16_t, 8>{}), fl[i]).e, x);
+                            split<f16_t>(__builtin_bit_cast(decltype(Vec<f16_t, 8>{}), fl[q & 1][i]).e, x);
 #pragma unroll
                             for (int k = PARTS_OF<f16_t> - 1; k >= 0; --k)
 #pragma unroll
-                                for (int j = 0; j < TN; ++j) mma_part(acc[i][j], __builtin_bit_cast(bf16x8, fr[j]), x[k], 0);
-                            __builtin_amdgcn_sched_barrier(0);   // (one after the other: this is not to cost the other path registers)
+                                for (int j = 0; j < TN; ++j) mma_part(acc[i0 + i][j], __builtin_bit_cast(bf16x8, fr[h][j]), x[k], 0);
+                            __builtin_amdgcn_sched_barrier(0);   // (one after the other: registers)
+                        } else {
+#pragma unroll
+                            for (int j = 0; j < TN; ++j) mma_part(acc[i0 + i][j], fr[h][j], fl[q & 1][i], 0);
                         }
-                    } else {
-                        mma<S>(acc, fr, fl);
                     }
+                    __builtin_amdgcn_sched_barrier(0);
                 }
             };
-            half(std::integral_constant<int, 0>{});
-            half(std::integral_constant<int, 1>{});
+            read(std::integral_constant<int, 0>{});
+            portion(std::integral_constant<int, 0>{});
+            portion(std::integral_constant<int, 1>{});
+            portion(std::integral_constant<int, 2>{});
+            portion(std::integral_constant<int, 3>{});
+            portion(std::integral_constant<int, 4>{});
+            portion(std::integral_constant<int, 5>{});
+            static_assert(PORTIONS <= 6);
         };
         if (steps > 0) {
             fetch(0);
@@ -230,8 +246,9 @@ __global__ void __launch_bounds__(WAVES_M * WAVES_N * WAVE, 2) k_gmm_mx4(GmmArgs
             __builtin_amdgcn_s_waitcnt(0x0070);   // vmcnt(0), lgkmcnt(0): this wave's part of the step is in LDS, and what it read of the step before has come
             __builtin_amdgcn_s_barrier();
             asm volatile("" ::: "memory");
-            if (t + 1 < steps) fetch(t + 1);
-            multiply(t & 1);
+            multiply(t & 1, [&] {
+                if (t + 1 < steps) fetch(t + 1);
+            });
             if (ASIDE && t % 4 == 3) put_aside();
             if (t + 1 < steps) stash(t + 1);
         }
