@@ -167,87 +167,68 @@ __global__ void __launch_bounds__(WAVES_M * WAVES_N * WAVE, 2) k_gmm_mx4_mx4(Gmm
 }
 
 // Few rows: the matrix is read once, straight into registers, a block and its scale a lane.
-template <class O, int ROWS, int TN, int WAVES>
+template <class O, int TN, int WAVES>
 __global__ void __launch_bounds__(WAVES * WAVE, 2) k_few_mx4_mx4(GmmArgs a, Mx4Args x, Mx4Args m)
 {
+    constexpr int ROWS = 16, U = TN == 2 ? 4 : 2;
     __shared__ __align__(16) float s_sums[few_lds(TN, WAVES)];
     __shared__ __align__(16) uint8_t s_scales[2][TN * 16 * FewScales<TN, WAVES>::PITCH];
-    __shared__ int64_t s_row[ROWS];
     RowsTile w;
     if (!few_rows_tile<O, ROWS, TN * 16>(a, w)) return;
     const int lane = lane_id(), r = lane % 16, g = lane / 16, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE);
+    const int whole = (int)(a.c / 128), steps = (int)((a.c + 127) / 128), rows = min(ROWS, w.hi - w.m0);
     const uint8_t *codes[TN];
 #pragma unroll
     for (int j = 0; j < TN; ++j) codes[j] = m.codes + w.group * m.stride_codes + min(w.n0 + j * 16 + r, (int)a.n - 1) * m.ld_codes;
-    const int whole = (int)(a.c / 128), steps = (int)((a.c + 127) / 128), rows = min(ROWS, w.hi - w.m0);
-    O *out = static_cast<O *>(a.out);
-    auto store = [&](int row, int64_t col, float v) { out[(int64_t)(w.m0 + row) * a.ldo + col] = (O)(s_row[row] < 0 ? 0.0f : v); };
-    auto tile = [&](auto tm) {
-        constexpr int TM = decltype(tm)::value, U = TN == 2 && TM <= 2 ? 4 : 2;
-        // (on their way while the rows are found)
-        FewScales<TN, WAVES> scales(m.scales + w.group * m.stride_scales, m.ld_scales, w.n0, a.n, m.blocks);
-        Mx4Batch<TN, U> b;
-        if (steps > 0) b.load(codes, min(wave * 4, steps - 1), g, m.blocks);
-        if ((int)threadIdx.x < rows) {
-            const int64_t row = a.index ? a.index[w.m0 + threadIdx.x] : w.m0 + threadIdx.x;
-            s_row[threadIdx.x] = (uint64_t)row < (uint64_t)a.index_rows ? row : -1;
-        }
-        __syncthreads();
-        const uint8_t *x_codes[TM], *x_scales[TM];
+    // (on their way while the row is found)
+    FewScales<TN, WAVES> scales(m.scales + w.group * m.stride_scales, m.ld_scales, w.n0, a.n, m.blocks);
+    Mx4Batch<TN, U> b;
+    if (steps > 0) b.load(codes, min(wave * 4, steps - 1), g, m.blocks);
+    const int slot = w.m0 + min(r, rows - 1);
+    const int64_t number = a.index ? a.index[slot] : slot, row = (uint64_t)number < (uint64_t)a.index_rows ? number : 0;   // (0: its result is replaced by 0)
+    const uint8_t *x_codes[1] = {x.codes + row * x.ld_codes}, *x_scales = x.scales + row * x.ld_scales;
+    f32x4 acc[1][TN] = {};
+    // U steps from t0 on; END: some of them may reach behind the lines' end.
+    auto multiply = [&](int t0, auto end) {
+        Mx4Batch<1, U> xs;
+        xs.load(x_codes, t0, g, m.blocks);
+        const uint8_t *words[1] = {x_scales + (int64_t)t0 * 4};
+        xs.load_scales(words);
 #pragma unroll
-        for (int i = 0; i < TM; ++i) {
-            const int64_t row = max(s_row[min(i * 16 + r, rows - 1)], (int64_t)0);
-            x_codes[i] = x.codes + row * x.ld_codes;
-            x_scales[i] = x.scales + row * x.ld_scales;
-        }
-        f32x4 acc[TM][TN] = {};
-        // U steps from t0 on; END: some of them may reach behind the lines' end.
-        auto multiply = [&](int t0, auto end) {
-            Mx4Batch<TM, U> xs;
-            xs.load(x_codes, t0, g, m.blocks);
-            const uint8_t *words[TM];
-#pragma unroll
-            for (int i = 0; i < TM; ++i) words[i] = x_scales[i] + (int64_t)t0 * 4;
-            xs.load_scales(words);
-#pragma unroll
-            for (int u = 0; u < U; ++u) {
-                if constexpr (decltype(end)::value) {
-                    const int valid = t0 + u < steps ? (int)max(min(a.c - ((int64_t)(t0 + u) * 128 + g * MX4_BLOCK), (int64_t)MX4_BLOCK), (int64_t)0) : 0;
-                    b.end(u, valid);
-                    xs.end(u, valid);
-                }
-#pragma unroll
-                for (int i = 0; i < TM; ++i)
-#pragma unroll
-                    for (int j = 0; j < TN; ++j)
-                        mma_mx4(acc[i][j], __builtin_bit_cast(u32x4, b.v[u][j]), b.s[j][u] >> 8 * g, __builtin_bit_cast(u32x4, xs.v[u][i]), xs.s[i][u] >> 8 * g);
+        for (int u = 0; u < U; ++u) {
+            if constexpr (decltype(end)::value) {
+                const int valid = t0 + u < steps ? (int)max(min(a.c - ((int64_t)(t0 + u) * 128 + g * MX4_BLOCK), (int64_t)MX4_BLOCK), (int64_t)0) : 0;
+                b.end(u, valid);
+                xs.end(u, valid);
             }
-        };
-        for (int pass = 0; pass * WAVES * 4 < steps; ++pass) {
-            scales.store(s_scales[pass & 1]);
-            __syncthreads();
-            scales.next();
-            const int first = (pass * WAVES + wave) * 4;
 #pragma unroll
-            for (int i = 0; i < 4; i += U) {
-                const int t = first + i, t_next = i + U < 4 ? t + U : first + WAVES * 4;
-                if (t >= steps) break;
-                const uint8_t *words[TN];
-#pragma unroll
-                for (int j = 0; j < TN; ++j) words[j] = s_scales[pass & 1] + (j * 16 + r) * FewScales<TN, WAVES>::PITCH + (wave * 4 + i) * 4;
-                b.load_scales(words);
-                if (t + U <= whole) multiply(t, std::false_type{});
-                else multiply(t, std::true_type{});
-                if (t_next < steps) b.load(codes, t_next, g, m.blocks);
-            }
+            for (int j = 0; j < TN; ++j)
+                mma_mx4(acc[0][j], __builtin_bit_cast(u32x4, b.v[u][j]), b.s[j][u] >> 8 * g, __builtin_bit_cast(u32x4, xs.v[u][0]), xs.s[0][u] >> 8 * g);
         }
-        few_meet<TM, TN, WAVES>(acc, rows, w.n0, a.n, s_sums, store);
     };
-    if (ROWS == 16 || rows <= 16) tile(std::integral_constant<int, 1>{});
-    else if constexpr (ROWS >= 32) {
-        if (ROWS == 32 || rows <= 32) tile(std::integral_constant<int, 2>{});
-        else if constexpr (ROWS == 64) tile(std::integral_constant<int, 4>{});
+    for (int pass = 0; pass * WAVES * 4 < steps; ++pass) {
+        scales.store(s_scales[pass & 1]);
+        __syncthreads();
+        scales.next();
+        const int first = (pass * WAVES + wave) * 4;
+#pragma unroll
+        for (int i = 0; i < 4; i += U) {
+            const int t = first + i, t_next = i + U < 4 ? t + U : first + WAVES * 4;
+            if (t >= steps) break;
+            const uint8_t *words[TN];
+#pragma unroll
+            for (int j = 0; j < TN; ++j) words[j] = s_scales[pass & 1] + (j * 16 + r) * FewScales<TN, WAVES>::PITCH + (wave * 4 + i) * 4;
+            b.load_scales(words);
+            if (t + U <= whole) multiply(t, std::false_type{});
+            else multiply(t, std::true_type{});
+            if (t_next < steps) b.load(codes, t_next, g, m.blocks);
+        }
     }
+    O *out = static_cast<O *>(a.out);
+    few_meet<1, TN, WAVES>(acc, rows, w.n0, a.n, s_sums, [&](int i, int64_t col, float v) {
+        const int64_t of = a.index ? a.index[w.m0 + i] : w.m0 + i;
+        out[(int64_t)(w.m0 + i) * a.ldo + col] = (O)((uint64_t)of < (uint64_t)a.index_rows ? v : 0.0f);
+    });
 }
 
 template <class O, int BM, int BN, int WAVES_M, int WAVES_N, int STAGES> hipError_t launch_tile(const GmmArgs &a, const Mx4Args &x, const Mx4Args &m, hipStream_t s)
@@ -261,24 +242,25 @@ template <class O, int BM, int BN, int WAVES_M, int WAVES_N, int STAGES> hipErro
 
 template <class O> hipError_t pick(const GmmArgs &a, const Mx4Args &x, const Mx4Args &m, hipStream_t s)
 {
+    // Up to 12 rows a group by themselves (us here and in tiles: 16 groups of 6 rows, 4096 x 4096, 25 and 28, eight of 8 15 and 16, of 16 19 and 16), and what
+    // tiles do not reach: 256 lines of the matrix and the rows of x that they gather, by 32-bit offsets.
     const int64_t groups = std::min(a.groups, a.rows);
-    auto m_tiles = [&](int64_t bm) { return std::max(groups, a.rows / bm + groups / 2); };
-    auto tiles = [&](int64_t bm, int64_t bn) { return (double)m_tiles(bm) * (double)((a.n + bn - 1) / bn); };
-    // (tiles reach 256 lines of the matrix and the rows of x that they gather by 32-bit offsets)
     const bool reached = offsets_fit(a.index ? std::max<int64_t>(a.index_rows, 256) : 256, std::max(x.ld_codes, x.ld_scales), 1);
-    if (few(a) || !reached) {
-        return launch_few(a, [&](auto rows, auto tn, auto waves) {
-            constexpr int ROWS = decltype(rows)::value, TN = decltype(tn)::value, WAVES = decltype(waves)::value;
-            const dim3 grid = few_grid(a, ROWS, TN * 16);
-            if (grid.x >= 1u << 23 || grid.y > 65535u) return TOO_MANY_TILES;
-            hipLaunchKernelGGL((k_few_mx4_mx4<O, ROWS, TN, WAVES>), grid, dim3(WAVES * WAVE), 0, s, a, x, m);
+    const bool few = groups > 0 && a.rows <= groups * 12 && a.n <= (1 << 20) && a.rows / 16 + groups < 65535;
+    if (few || !reached)
+        return with_columns_and_waves(a, [&](auto tn, auto waves) {
+            constexpr int TN = decltype(tn)::value, WAVES = decltype(waves)::value;
+            const dim3 grid = few_grid(a, 16, TN * 16);
+            if (grid.x >= 1u << 22 || grid.y > 65535u) return TOO_MANY_TILES;
+            hipLaunchKernelGGL((k_few_mx4_mx4<O, TN, WAVES>), grid, dim3(WAVES * WAVE), 0, s, a, x, m);
             return hipGetLastError();
         });
-    }
-    if constexpr (sizeof(O) == 2)   // (results of 32 bits do not fit the operands' place in LDS)
-        if (tiles(128, 128) >= 512 && launches<GM_ROWS>(a, 256, 256, 512)) return launch_tile<O, 256, 256, 2, 4, 2>(a, x, m, s);
-    if (tiles(64, 64) >= 512 || !launches<GM_ROWS>(a, 64, 64, 256)) return launch_tile<O, 128, 128, 2, 2, 2>(a, x, m, s);
-    return launch_tile<O, 64, 64, 4, 1, 4>(a, x, m, s);
+    constexpr TileTimes TIMES = {12.5, 3.5, 0.0248, 26, 19.5, 41, 32};
+    const int lines = pick_lines(a, TIMES, sizeof(O) == 2);   // (results of 32 bits do not fit the operands' place in LDS)
+    if (lines == 64) return launch_tile<O, 64, 64, 4, 1, 4>(a, x, m, s);
+    if constexpr (sizeof(O) == 2)
+        if (lines == 256) return launch_tile<O, 256, 256, 2, 4, 2>(a, x, m, s);
+    return launch_tile<O, 128, 128, 2, 2, 2>(a, x, m, s);
 }
 
 }  // namespace

@@ -57,7 +57,8 @@ template <bool RCOL, int BN, int THREADS> __device__ __forceinline__ bool any_fa
 }
 
 // A tile: x straight to LDS (16 bits, whole pieces) or through registers, where single precision is split; the matrix's codes through registers, where they are widened.
-template <class T, bool RCOL, int BM, int BN, int WAVES_M, int WAVES_N, bool ASYNC>
+// STAGES steps of x are in LDS, and as many of the matrix under way in registers or widened: the next one, or in small tiles, which wait for memory, three.
+template <class T, bool RCOL, int BM, int BN, int WAVES_M, int WAVES_N, bool ASYNC, int STAGES>
 __global__ void __launch_bounds__(WAVES_M * WAVES_N * WAVE, 2) k_gmm_mx4(GmmArgs a, Mx4Args m, int nt)
 {
     constexpr int THREADS = WAVES_M * WAVES_N * WAVE, WM = BM / WAVES_M, WN = BN / WAVES_N, TM = WM / 16, TN = WN / 16, PARTS = sizeof(T) == 4 ? 3 : 1;
@@ -67,11 +68,13 @@ __global__ void __launch_bounds__(WAVES_M * WAVES_N * WAVE, 2) k_gmm_mx4(GmmArgs
     static_assert(!ASYNC || PARTS == 1, "parts are made in registers");
     using TL = Tile<S, false, false, BM, THREADS, LINE>;
     using TR = Tile<S, RCOL, !RCOL, BN, THREADS, LINE>;
-    constexpr int BUFFER = PARTS * TL::BYTES + TR::BYTES;
+    constexpr int X_BYTES = PARTS * TL::BYTES;
+    static_assert(STAGES == 2 || (STAGES == 4 && ASYNC), "through registers: one step ahead");
     // A thread's share of the matrix's step: E numbers of a line side by side, in one block.
     constexpr int E = BN * STEP_C / THREADS, WORDS = E / 8, A_LINE = (RCOL ? BN : STEP_C) / E;
     static_assert(E == 16 || E == 32, "part of a block");
-    __shared__ __align__(16) char lds[2 * BUFFER];
+    __shared__ __align__(16) char lds[STAGES * X_BYTES + 2 * TR::BYTES];
+    char *const lds_r = lds + STAGES * X_BYTES;
     RowsTile w;
     if (!rows_tile<T>(a, BM, BN, nt, w)) return;
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid / WAVE);
@@ -108,27 +111,31 @@ __global__ void __launch_bounds__(WAVES_M * WAVES_N * WAVE, 2) k_gmm_mx4(GmmArgs
         constexpr bool WIDE = decltype(far)::value;
         struct Raw { uint4 v[sizeof(T) / 2]; };
         Raw kept[ASYNC ? 1 : TL::LOADS];
-        uint32_t kept_codes[WORDS], kept_scale = 0;
+        uint32_t kept_codes[STAGES][WORDS], kept_scale[STAGES];   // step t's in t % STAGES
         // Workgroups begin at different steps and go round, so that they don't all read lines that begin in the same memory channels; what is left
         // of the lines behind whole steps comes last.
         const int whole = depth / STEP_C, turn = whole == 0 ? 0 : (w.n0 / BN + w.group * 5) % whole;
         auto at = [&](int t) { return t == whole ? t : t + turn >= whole ? t + turn - whole : t + turn; };
-        auto fetch = [&](int t_) {
-            const int t = at(t_), c0 = t * STEP_C, left = min(STEP_C, depth - c0);
-            const bool there = RCOL ? line < left : c0 + part * E < m.blocks * MX4_BLOCK;
+        auto scale_place = [&](int c0) -> uint32_t { return RCOL ? scale_off : scale_off + c0 / MX4_BLOCK; };
+        // (steps that are not there are fetched as zeros, from no memory, so that every step has as many loads)
+        auto fetch = [&](int t_, auto slot_) {
+            constexpr int slot = decltype(slot_)::value;
+            const int t = t_ < steps ? at(t_) : 0, c0 = t * STEP_C, left = t_ < steps ? min(STEP_C, depth - c0) : 0;
+            const bool there = RCOL ? line < left : t_ < steps && c0 + part * E < m.blocks * MX4_BLOCK;
             const Memory code_memory = memory_at(RCOL ? codes + (int64_t)c0 * m.ld_codes : codes), scale_memory = memory_at(RCOL ? scales + (int64_t)c0 * m.ld_scales : scales);
-            const uint32_t code_at = there ? code_off : NOWHERE, scale_at = there ? scale_off : NOWHERE;   // (zeros: a code of 0 is 0 at any scale but NaN)
+            // (zeros: a code of 0 is 0 at any scale but NaN.  The scale as its word: a byte would be widened, and waited for, where it is loaded)
+            const uint32_t code_at = there ? code_off : NOWHERE, scale_at = there ? scale_place(c0) & ~3u : NOWHERE;
             if constexpr (WORDS == 4) {
                 const u32x4 v = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(code_memory, code_at, RCOL ? 0 : c0 / 2, 0));
 #pragma unroll
-                for (int j = 0; j < 4; ++j) kept_codes[j] = v[j];
+                for (int j = 0; j < 4; ++j) kept_codes[slot][j] = v[j];
             } else {
                 const auto v = __builtin_amdgcn_raw_buffer_load_b64(code_memory, code_at, RCOL ? 0 : c0 / 2, 0);
-                kept_codes[0] = v[0], kept_codes[1] = v[1];
+                kept_codes[slot][0] = v[0], kept_codes[slot][1] = v[1];
             }
-            kept_scale = __builtin_amdgcn_raw_buffer_load_b8(scale_memory, scale_at, RCOL ? 0 : c0 / MX4_BLOCK, 0);
+            kept_scale[slot] = __builtin_amdgcn_raw_buffer_load_b32(scale_memory, scale_at, 0, 0);
             if constexpr (ASYNC) {
-                char *to = lds + (t_ & 1) * BUFFER + wave * (WAVE * 16);
+                char *to = lds + slot * X_BYTES + wave * (WAVE * 16);
 #pragma unroll
                 for (int i = 0; i < TL::LOADS; ++i)
                     memory_to_lds<16>(x_memory, TL::piece_of(tid, i) * 8 < left ? off[i] : NOWHERE, (uint32_t)c0 * 2, to + i * THREADS * 16);
@@ -144,9 +151,10 @@ __global__ void __launch_bounds__(WAVES_M * WAVES_N * WAVE, 2) k_gmm_mx4(GmmArgs
                 }
             }
         };
-        auto stash = [&](int t_) {
-            char *to = lds + (t_ & 1) * BUFFER;
+        auto stash = [&](int t_, auto slot_) {
+            constexpr int slot = decltype(slot_)::value;
             if constexpr (!ASYNC) {
+                char *to = lds + slot * X_BYTES;
 #pragma unroll
                 for (int i = 0; i < TL::LOADS; ++i) {
                     if constexpr (PARTS == 1) {
@@ -159,21 +167,18 @@ __global__ void __launch_bounds__(WAVES_M * WAVES_N * WAVE, 2) k_gmm_mx4(GmmArgs
                     }
                 }
             }
-            if constexpr (!RCOL) {
-                const int valid = depth - (at(t_) * STEP_C + part * E);
-                if (valid < E) {   // (codes behind the end meet zeros of x, but may be infinite numbers)
+            uint32_t (&words)[WORDS] = kept_codes[slot];
+            if (!RCOL && t_ == whole) {   // (codes behind the lines' end meet zeros of x, but may be infinite numbers)
 #pragma unroll
-                    for (int j = 0; j < WORDS; ++j) kept_codes[j] = mx4_first(kept_codes[j], valid - j * 8);
-                }
+                for (int j = 0; j < WORDS; ++j) words[j] = mx4_first(words[j], depth - (t_ * STEP_C + part * E + j * 8));
             }
             const int swizzle = RCOL ? col_xor<S, TR::PIECES>(line) : row_xor<!RCOL, TR::PIECES>(line);
-            char *to_line = to + PARTS * TL::BYTES + line * TR::PIECES * 16;
-            const float scale = mx4_scale(kept_scale);
+            char *to_line = lds_r + slot % 2 * TR::BYTES + line * TR::PIECES * 16;
+            const float scale = mx4_scale(kept_scale[slot] >> scale_place(at(t_) * STEP_C) % 4 * 8 & 255u);
             auto widen = [&](auto type) {
                 using W = decltype(type);
 #pragma unroll
-                for (int j = 0; j < WORDS; ++j)
-                    *reinterpret_cast<Frag<W> *>(to_line + ((part * WORDS + j) ^ swizzle) * 16) = mx4_fragment<W>(kept_codes[j], scale);
+                for (int j = 0; j < WORDS; ++j) *reinterpret_cast<Frag<W> *>(to_line + ((part * WORDS + j) ^ swizzle) * 16) = mx4_fragment<W>(words[j], scale);
             };
             widen(std::conditional_t<WIDE, bf16_t, S>{});
         };
@@ -197,12 +202,12 @@ __global__ void __launch_bounds__(WAVES_M * WAVES_N * WAVE, 2) k_gmm_mx4(GmmArgs
         // A step in portions: half of its c, one part of x and AT_ONCE of the wave's 16s of rows, the next portion's reads under way meanwhile; load() brings the next
         // step on its way behind the first reads (before them, the waves wait for its addresses to be taken).
         constexpr int AT_ONCE = TM < 4 ? TM : 4, PER_PART = TM / AT_ONCE, PER_HALF = PARTS * PER_PART, PORTIONS = 2 * PER_HALF;
-        auto multiply = [&](int buffer, auto load) {
-            const char *from = lds + buffer * BUFFER;
+        auto multiply = [&](int slot, auto load) {
+            const char *from = lds + slot * X_BYTES, *from_r = lds_r + slot % 2 * TR::BYTES;
             Frag<S> fr[2][TN], fl[2][AT_ONCE];
             auto read = [&](auto portion) {
                 constexpr int q = decltype(portion)::value, h = q / PER_HALF, p = PARTS - 1 - q % PER_HALF / PER_PART, i0 = q % PER_PART * AT_ONCE;
-                if constexpr (q % PER_HALF == 0) TR::template read<h>(from + PARTS * TL::BYTES, at_r, fr[h]);
+                if constexpr (q % PER_HALF == 0) TR::template read<h>(from_r, at_r, fr[h]);
                 TL::template read<h>(from + p * TL::BYTES + tile_line<false>(i0, 0) * LINE, at_l, fl[q & 1]);
             };
             auto portion = [&](auto portion) {
@@ -237,20 +242,35 @@ __global__ void __launch_bounds__(WAVES_M * WAVES_N * WAVE, 2) k_gmm_mx4(GmmArgs
             portion(std::integral_constant<int, 5>{});
             static_assert(PORTIONS <= 6);
         };
-        if (steps > 0) {
-            fetch(0);
-            stash(0);
-        }
-        for (int t = 0; t < steps; ++t) {
-            asm volatile("" ::: "memory");
-            __builtin_amdgcn_s_waitcnt(0x0070);   // vmcnt(0), lgkmcnt(0): this wave's part of the step is in LDS, and what it read of the step before has come
-            __builtin_amdgcn_s_barrier();
-            asm volatile("" ::: "memory");
-            multiply(t & 1, [&] {
-                if (t + 1 < steps) fetch(t + 1);
+        using std::integral_constant;
+        auto each_slot = [&](auto f) {
+            f(integral_constant<int, 0>{});
+            f(integral_constant<int, 1>{});
+            if constexpr (STAGES == 4) {
+                f(integral_constant<int, 2>{});
+                f(integral_constant<int, 3>{});
+            }
+        };
+        each_slot([&](auto slot) {
+            if constexpr (decltype(slot)::value < STAGES - 1) fetch(decltype(slot)::value, slot);
+        });
+        stash(0, integral_constant<int, 0>{});
+        for (int t0 = 0; t0 < steps; t0 += STAGES) {
+            each_slot([&](auto slot_) {
+                constexpr int slot = decltype(slot_)::value, NEXT = (slot + 1) % STAGES, LAST = (slot + STAGES - 1) % STAGES;
+                const int t = t0 + slot;   // (up to STAGES - 1 steps are not there: zeros, and no branch for which registers of loads under way would be moved)
+                // This wave's part of the step is in LDS (loads come back in order: all but those of the steps behind it), and what it read of the step before
+                // has come; then everyone's is, and nobody reads the places of the step before any more.
+                constexpr int LATER = (STAGES - 2) * (2 + (ASYNC ? TL::LOADS : 0));
+                static_assert(LATER < 16, "what the counter's low bits hold");
+                asm volatile("" ::: "memory");
+                __builtin_amdgcn_s_waitcnt(0x0070 | LATER);
+                __builtin_amdgcn_s_barrier();
+                asm volatile("" ::: "memory");
+                multiply(slot, [&] { fetch(t + STAGES - 1, integral_constant<int, LAST>{}); });
+                if (ASIDE && t % 4 == 3) put_aside();
+                stash(t + 1, integral_constant<int, NEXT>{});
             });
-            if (ASIDE && t % 4 == 3) put_aside();
-            if (t + 1 < steps) stash(t + 1);
         }
         if constexpr (ASIDE) {
 #pragma unroll
@@ -387,40 +407,50 @@ __global__ void __launch_bounds__(WAVES * WAVE, 2) k_few_mx4(GmmArgs a, Mx4Args 
     }
 }
 
-template <class T, bool RCOL, int BM, int BN, int WAVES_M, int WAVES_N, bool ASYNC> hipError_t launch_tile(const GmmArgs &a, const Mx4Args &m, hipStream_t s)
+template <class T, bool RCOL, int BM, int BN, int WAVES_M, int WAVES_N, bool ASYNC, int STAGES = 2> hipError_t launch_tile(const GmmArgs &a, const Mx4Args &m, hipStream_t s)
 {
     const Grid g = grid_of<GM_ROWS>(a, BM, BN);
     constexpr int threads = WAVES_M * WAVES_N * WAVE;
     if (g.blocks * threads >= (1ll << 32)) return TOO_MANY_TILES;
-    hipLaunchKernelGGL((k_gmm_mx4<T, RCOL, BM, BN, WAVES_M, WAVES_N, ASYNC>), dim3((uint32_t)g.blocks), dim3(threads), 0, s, a, m, (int)g.nt);
+    hipLaunchKernelGGL((k_gmm_mx4<T, RCOL, BM, BN, WAVES_M, WAVES_N, ASYNC, STAGES>), dim3((uint32_t)g.blocks), dim3(threads), 0, s, a, m, (int)g.nt);
     return hipGetLastError();
+}
+
+// Rows are few where the matrix's bytes are the time: up to 20 a group, and up to 64 where there are not enough groups and columns for the chip (4096 x 4096, us in k_few_mx4
+// and in tiles: eight groups of 8 rows 21 and 35, of 16 25 and 35, of 24 45 and 35; one group of 16 12 and 25, of 40 17 and 24, of 64 21 and 24).
+bool few_rows(const GmmArgs &a)
+{
+    const int64_t groups = std::min(a.groups, a.rows);
+    return groups > 0 && a.rows <= groups * (fills_chip(a) ? 20 : 64) && a.n <= (1 << 20) && a.rows / 16 + groups < 65535;
 }
 
 template <class T, bool RCOL> hipError_t pick(const GmmArgs &a, const Mx4Args &m, bool straight, hipStream_t s)
 {
-    const int64_t groups = std::min(a.groups, a.rows);
-    auto m_tiles = [&](int64_t bm) { return std::max(groups, a.rows / bm + groups / 2); };
-    auto tiles = [&](int64_t bm, int64_t bn) { return (double)m_tiles(bm) * (double)((a.n + bn - 1) / bn); };
     if constexpr (!RCOL) {
-        if (few(a)) {
-            return launch_few(a, [&](auto rows, auto tn, auto waves) {
+        if (few_rows(a)) {
+            auto launch = [&](auto rows, auto tn, auto waves) {
                 constexpr int ROWS = decltype(rows)::value, TN = decltype(tn)::value, WAVES = decltype(waves)::value;
-                const dim3 grid = few_grid(a, ROWS, TN * 16);
-            if (grid.x >= 1u << 23 || grid.y > 65535u) return TOO_MANY_TILES;
-            hipLaunchKernelGGL((k_few_mx4<T, ROWS, TN, WAVES>), grid, dim3(WAVES * WAVE), 0, s, a, m);
+                hipLaunchKernelGGL((k_few_mx4<T, ROWS, TN, WAVES>), few_grid(a, ROWS, TN * 16), dim3(WAVES * WAVE), 0, s, a, m);
                 return hipGetLastError();
+            };
+            using std::integral_constant;
+            const int64_t groups = std::min(a.groups, a.rows);
+            return with_columns_and_waves(a, [&](auto tn, auto waves) {
+                if (a.rows <= groups * 10) return launch(integral_constant<int, 16>{}, tn, waves);
+                if (a.rows <= groups * 22) return launch(integral_constant<int, 32>{}, tn, waves);
+                return launch(integral_constant<int, 64>{}, integral_constant<int, 2>{}, waves);   // (more columns leave no registers; here they are 2)
             });
         }
     }
-    if constexpr (sizeof(T) == 2) {
-        if (straight) {
-            if (tiles(128, 128) >= 512 && launches<GM_ROWS>(a, 256, 256, 512)) return launch_tile<T, RCOL, 256, 256, 2, 4, true>(a, m, s);
-            if (tiles(64, 64) >= 512 || !launches<GM_ROWS>(a, 64, 64, 256)) return launch_tile<T, RCOL, 128, 128, 2, 2, true>(a, m, s);
-            return launch_tile<T, RCOL, 64, 64, 4, 1, true>(a, m, s);
-        }
+    // (single precision: tiles of 128 x 128 take 367 us for 2048 rows of 4096, 4096 columns, of 64 x 64 369, and 185 and 105 for 512)
+    if constexpr (sizeof(T) == 4) return launch_tile<T, RCOL, 64, 64, 4, 1, false>(a, m, s);
+    else {
+        constexpr TileTimes TIMES = {26, 10, 0.0555, 74, 50, 104, 92};
+        const int lines = pick_lines(a, TIMES, straight);
+        if (!straight) return lines == 64 ? launch_tile<T, RCOL, 64, 64, 4, 1, false>(a, m, s) : launch_tile<T, RCOL, 128, 128, 2, 2, false>(a, m, s);
+        if (lines == 64) return launch_tile<T, RCOL, 64, 64, 4, 1, true, 4>(a, m, s);
+        return lines == 128 ? launch_tile<T, RCOL, 128, 128, 2, 2, true>(a, m, s) : launch_tile<T, RCOL, 256, 256, 2, 4, true>(a, m, s);
     }
-    if (tiles(64, 64) >= 512 || !launches<GM_ROWS>(a, 64, 64, 256)) return launch_tile<T, RCOL, 128, 128, 2, 2, false>(a, m, s);
-    return launch_tile<T, RCOL, 64, 64, 4, 1, false>(a, m, s);
 }
 
 }  // namespace

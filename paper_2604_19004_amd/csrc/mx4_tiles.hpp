@@ -207,31 +207,53 @@ __device__ __forceinline__ void few_meet(const f32x4 (&acc)[TM][TN], int rows, i
     }
 }
 constexpr int few_lds(int tn, int waves) { return waves * 16 * (tn * 16 + 4); }   // floats
-// Whether rows are few, and calls launch(ROWS, TN, WAVES) as constants for how many, how many columns and how long rows.
-inline bool few(const GmmArgs &a)
-{
-    const int64_t groups = std::min(a.groups, a.rows);
-    return groups > 0 && a.rows <= groups * 48 && a.n <= (1 << 20) && a.rows / 16 + groups < 65535;
-}
 inline dim3 few_grid(const GmmArgs &a, int rows, int cols)
 {
     return dim3((uint32_t)((a.n + cols - 1) / cols), (uint32_t)(a.rows / rows + std::min(a.groups, a.rows)) + 1);
 }
-template <class Launch> hipError_t launch_few(const GmmArgs &a, Launch launch_)
+// Columns of a workgroup of few rows, and its waves: calls launch(TN, WAVES) as constants.  64 columns where that leaves two workgroups a compute unit, else 32; short
+// lines in fewer waves.
+inline bool fills_chip(const GmmArgs &a) { return std::min(a.groups, a.rows) * ((a.n + 63) / 64) >= 512; }
+template <class Launch> hipError_t with_columns_and_waves(const GmmArgs &a, Launch launch)
 {
     using std::integral_constant;
+    auto with_waves = [&](auto tn) {
+        if (a.c >= 4096) return launch(tn, integral_constant<int, 8>{});
+        return launch(tn, integral_constant<int, 4>{});
+    };
+    if (fills_chip(a)) return with_waves(integral_constant<int, 4>{});
+    return with_waves(integral_constant<int, 2>{});
+}
+
+// Which tiles: those that take the least by what was measured at c = 4096, us for n of them: of 64 x 64 one a compute unit, or so much for all and each; of
+// 128 x 128 by rounds of two a compute unit, of 256 x 256 of one, and for a last round that is half full or less.
+struct TileTimes { double small, small_all, small_each, middle, middle_half, large, large_least; };
+inline double small_time(const TileTimes &t, double n) { return n <= 256 ? t.small : t.small_all + t.small_each * n; }
+inline double middle_time(const TileTimes &t, double n)
+{
+    const double whole = (double)(int64_t)(n / 512), rest = n - whole * 512;
+    return whole * t.middle + (rest > 256 ? t.middle : rest > 0 ? t.middle_half : 0.0);
+}
+inline double large_time(const TileTimes &t, double n)
+{
+    const double whole = (double)(int64_t)(n / 256), rest = n - whole * 256;
+    return whole * t.large + (rest > 0 ? t.large_least + (t.large - t.large_least) * rest / 256 : 0.0);
+}
+// The tile's lines (256 only if `large`), among those that one launch has; 0: none does.
+inline int pick_lines(const GmmArgs &a, const TileTimes &t, bool large)
+{
     const int64_t groups = std::min(a.groups, a.rows);
-    auto launch = [&](auto rows, auto tn) {
-        if (a.c >= 4096) return launch_(rows, tn, integral_constant<int, 8>{});
-        return launch_(rows, tn, integral_constant<int, 4>{});
+    // (a group's last tile is half full on the average)
+    auto tiles = [&](int64_t b) { return (double)std::max(groups, a.rows / b + groups / 2) * (double)((a.n + b - 1) / b); };
+    double best = 1e300;
+    int lines = 0;
+    auto offer = [&](int b, int threads, double time) {
+        if (time < best && launches<GM_ROWS>(a, b, b, threads)) best = time, lines = b;
     };
-    auto with_rows = [&](auto tn) {
-        if (a.rows <= groups * 10) return launch(integral_constant<int, 16>{}, tn);
-        return launch(integral_constant<int, 32>{}, tn);
-    };
-    if (a.rows > groups * 22) return launch(integral_constant<int, 64>{}, integral_constant<int, 2>{});   // (more columns leave no registers)
-    if (groups * ((a.n + 63) / 64) >= 512) return with_rows(integral_constant<int, 4>{});
-    return with_rows(integral_constant<int, 2>{});
+    offer(64, 256, small_time(t, tiles(64)));
+    offer(128, 256, middle_time(t, tiles(128)));
+    if (large) offer(256, 512, large_time(t, tiles(256)));
+    return lines;
 }
 
 }  // namespace
