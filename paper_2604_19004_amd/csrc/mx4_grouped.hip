@@ -272,6 +272,9 @@ __global__ void __launch_bounds__(WAVES_M * WAVES_N * WAVE, 2) k_gmm_mx4(GmmArgs
                 stash(t + 1, integral_constant<int, NEXT>{});
             });
         }
+        asm volatile("" ::: "memory");
+        __builtin_amdgcn_s_waitcnt(0x0f70);   // vmcnt(0): steps that are not there also write their zeros to LDS, where the results go now
+        asm volatile("" ::: "memory");
         if constexpr (ASIDE) {
 #pragma unroll
             for (int i = 0; i < TM; ++i)

@@ -389,3 +389,94 @@ def test_refusals(ex):
     for call in (lambda: f(x.double(), w, ptr), lambda: f(q, w, ptr, dtype=torch.float64)):
         with pytest.raises(TypeError):
             call()
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16", "float16"])
+def test_sizes_that_take_each_tile(ex, dtype):
+    """Of 64 x 64, 128 x 128 and 256 x 256 (16 bits), with lines of whole pieces and without, forward and across, lengths of one step to several and odd ones."""
+    for K, N in ((264, 2000), (2000, 264), (1999, 264), (320, 2049), (64, 2560), (2560, 64), (63, 130), (192, 1000), (40, 72)):
+        _compare(ex, [1500, 0, 1600], K, N, dtype, K + N, rows_of_x=700)
+    _compare(ex, [3000, 3100, 2900, 3300], 2304, 96, dtype, 11)
+    _compare(ex, [65, 130, 40], 72, 200, dtype, 12)
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16", "float16"])
+def test_all_rows_in_one_of_many_groups(ex, dtype):
+    """Where groups are few rows on the average, one that has them all is shared out in tiles of few rows."""
+    _compare(ex, [0] * 7 + [600] + [0] * 60, 200, 136, dtype, 13, rows_of_x=90)
+    _compare(ex, [1] * 20 + [150] + [0] * 9 + [17] * 3, 330, 72, dtype, 14)
+
+
+def test_float16_at_the_ends_of_its_range(ex):
+    """Scales at which float16 just holds the matrix's numbers, subnormal ones among them, one step beyond it, zeros at scale 0, and one far scale in a matrix of near ones."""
+    import torch
+    g = torch.Generator().manual_seed(15)
+    for sizes, K, N in (([9], 96, 40), ([200, 130], 96, 150), ([700, 900], 264, 2000)):
+        S, E = sum(sizes), len(sizes)
+        blocks = (K + 31) // 32
+        for low, high in ((104, 112), (103, 106), (138, 140), (140, 142), (90, 150)):
+            codes = torch.randint(0, 256, (E, N, blocks * 16), generator=g).to(torch.uint8)
+            scales = torch.zeros(E, N, 16, dtype=torch.uint8)
+            scales[..., :blocks] = torch.randint(low, high + 1, (E, N, blocks), generator=g).to(torch.uint8)
+            codes[:, 3, :16], scales[:, 3, 0] = 0, 0                  # zeros, whatever the scale
+            scales[E - 1, N - 1, 1] = 60 if low < 120 else 150          # (beyond float16, in the last tile)
+            w, value = ex.Mx4(codes.cuda(), scales.cuda(), K), X.values(X.unpack(codes.numpy()), scales[..., :blocks].numpy().astype(np.int64), K)
+            # rows that keep the results within float16
+            x = (torch.randn(S, K, generator=g) * (2.0 ** -14 if low >= 120 or high >= 150 else 8.0)).half()
+            dy = (torch.randn(S, N, generator=g) * (2.0 ** -14 if low >= 120 or high >= 150 else 8.0)).half()
+            ptr = _ptr(sizes)
+            want, mag = O.grouped(_np(ptr), _np(x), value)
+            with np.errstate(over="ignore"):
+                ok = np.abs(want) < 60000
+            got = ex.grouped_matmul_mx4(x.cuda(), w, ptr.cuda())
+            assert np.all(np.abs(_np(got) - want)[ok] <= (2 * (K + 2) * 2.0 ** -24 * mag + EPS["float16"] * np.abs(want) + TINY["float16"])[ok])
+            want, mag = O.grouped(_np(ptr), _np(dy), value.transpose(0, 2, 1))
+            ok = np.abs(want) < 60000
+            got = ex.grouped_matmul_mx4(dy.cuda(), w, ptr.cuda(), transposed=True)
+            assert np.all(np.abs(_np(got) - want)[ok] <= (2 * (N + 2) * 2.0 ** -24 * mag + EPS["float16"] * np.abs(want) + TINY["float16"])[ok])
+
+
+def test_codes_and_scales_behind_the_end_do_not_count(ex):
+    """The same numbers with other bytes behind `inner`, forward, across and with rows in four bits: the same bits."""
+    import torch
+    g = torch.Generator().manual_seed(16)
+    for sizes, K, N in (([3, 9], 70, 50), ([300, 400], 1000, 300), ([40], 4100, 40), ([900], 33, 500)):
+        ptr = _ptr(sizes).cuda()
+        a = ex.mx4_quantize(torch.randn(len(sizes), N, K, generator=g).cuda())
+        q = ex.mx4_quantize(torch.randn(sum(sizes), K, generator=g).cuda())
+        x, dy = torch.randn(sum(sizes), K, generator=g).bfloat16().cuda(), torch.randn(sum(sizes), N, generator=g).bfloat16().cuda()
+
+        def other(m):
+            codes, scales = m.codes.clone(), m.scales.clone()
+            codes[..., (K + 1) // 2:] = 0xff if K % 2 == 0 else codes[..., (K + 1) // 2:]
+            if K % 2:
+                codes[..., K // 2] |= 0xf0
+                codes[..., K // 2 + 1:] = 0x77
+            scales[..., (K + 31) // 32:] = 255
+            return ex.Mx4(codes, scales, K)
+
+        b, p = other(a), other(q)
+        assert torch.equal(ex.grouped_matmul_mx4(x, a, ptr), ex.grouped_matmul_mx4(x, b, ptr))
+        assert torch.equal(ex.grouped_matmul_mx4(dy, a, ptr, transposed=True), ex.grouped_matmul_mx4(dy, b, ptr, transposed=True))
+        assert torch.equal(ex.grouped_matmul_mx4(q, a, ptr), ex.grouped_matmul_mx4(p, b, ptr))
+
+
+def test_two_streams_at_once(ex):
+    import torch
+    g = torch.Generator().manual_seed(17)
+    ptr = _ptr([400, 500]).cuda()
+    w, _ = _four(ex, g, 2, 300, 520)
+    xs = [_rand(g, 900, 520, dtype="bfloat16").cuda() for _ in range(2)]
+    want = [(ex.grouped_matmul_mx4(x, w, ptr), ex.grouped_matmul_mx4(ex.mx4_quantize(x), w, ptr)) for x in xs]
+    streams = [torch.cuda.Stream() for _ in xs]
+    got = [[], []]
+    for s in streams:
+        s.wait_stream(torch.cuda.current_stream())
+    for _ in range(5):
+        for i, (s, x) in enumerate(zip(streams, xs)):
+            got[i].append((ex.grouped_matmul_mx4(x, w, ptr, stream=s), ex.grouped_matmul_mx4(ex.mx4_quantize(x, stream=s), w, ptr, stream=s)))
+    for s in streams:
+        torch.cuda.current_stream().wait_stream(s)
+    for i in range(2):
+        for pair in got[i]:
+            assert all(torch.equal(a, b) for a, b in zip(pair, want[i]))
