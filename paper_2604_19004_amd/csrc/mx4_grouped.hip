@@ -32,6 +32,27 @@ template <class T> __device__ __forceinline__ void split(const T (&x)[8], bf16x8
         }
     }
 }
+// The same in 4 operations a number and one a pair and part, where this is the time: numbers that are not finite, whose rest is NaN, are looked for with one more,
+// and then it goes the other way (in tiles, 2048 rows by eight 4096 x 4096: 380 us and 340; beside few rows the branch costs more than it saves).
+__device__ __forceinline__ void split_finite(const float (&x)[8], bf16x8 (&out)[3])
+{
+    uint32_t words[3][4];
+    float other = 0.0f;
+#pragma unroll
+    for (int k = 0; k < 8; k += 2) {
+        float left[2] = {x[k], x[k + 1]};
+        other = fmaf(left[1], 0.0f, fmaf(left[0], 0.0f, other));
+#pragma unroll
+        for (int p = 0; p < 3; ++p) {
+            words[p][k / 2] = __builtin_amdgcn_perm(__float_as_uint(left[1]), __float_as_uint(left[0]), 0x07060302);
+#pragma unroll
+            for (int i = 0; i < 2; ++i) left[i] -= __uint_as_float(__float_as_uint(left[i]) & 0xffff0000u);
+        }
+    }
+#pragma unroll
+    for (int p = 0; p < 3; ++p) out[p] = __builtin_bit_cast(bf16x8, words[p]);
+    if (other != other) split<float>(x, out);
+}
 
 // Whether a tile has a scale that float16 does not take; every thread calls it.
 template <bool RCOL, int BN, int THREADS> __device__ __forceinline__ bool any_far(const Mx4Args &m, const uint8_t *scales, int n0, int64_t n, int depth)
@@ -57,7 +78,8 @@ template <bool RCOL, int BN, int THREADS> __device__ __forceinline__ bool any_fa
 }
 
 // A tile: x straight to LDS (16 bits, whole pieces) or through registers, where single precision is split; the matrix's codes through registers, where they are widened.
-// STAGES steps of x are in LDS, and as many of the matrix under way in registers or widened: the next one, or in small tiles, which wait for memory, three.
+// STAGES steps are under way, in LDS or registers: the next one, or in small tiles, which wait for memory, three (512 rows of 4095 by 4095 x 4096, bfloat16, through
+// registers: 58 us and 50).
 template <class T, bool RCOL, int BM, int BN, int WAVES_M, int WAVES_N, bool ASYNC, int STAGES>
 __global__ void __launch_bounds__(WAVES_M * WAVES_N * WAVE, 2) k_gmm_mx4(GmmArgs a, Mx4Args m, int nt)
 {
@@ -68,13 +90,13 @@ __global__ void __launch_bounds__(WAVES_M * WAVES_N * WAVE, 2) k_gmm_mx4(GmmArgs
     static_assert(!ASYNC || PARTS == 1, "parts are made in registers");
     using TL = Tile<S, false, false, BM, THREADS, LINE>;
     using TR = Tile<S, RCOL, !RCOL, BN, THREADS, LINE>;
-    constexpr int X_BYTES = PARTS * TL::BYTES;
-    static_assert(STAGES == 2 || (STAGES == 4 && ASYNC), "through registers: one step ahead");
+    constexpr int X_BYTES = PARTS * TL::BYTES, X_STEPS = ASYNC ? STAGES : 2;
+    static_assert(STAGES == 2 || STAGES == 4, "the loop's steps");
     // A thread's share of the matrix's step: E numbers of a line side by side, in one block.
     constexpr int E = BN * STEP_C / THREADS, WORDS = E / 8, A_LINE = (RCOL ? BN : STEP_C) / E;
     static_assert(E == 16 || E == 32, "part of a block");
-    __shared__ __align__(16) char lds[STAGES * X_BYTES + 2 * TR::BYTES];
-    char *const lds_r = lds + STAGES * X_BYTES;
+    __shared__ __align__(16) char lds[X_STEPS * X_BYTES + 2 * TR::BYTES];
+    char *const lds_r = lds + X_STEPS * X_BYTES;
     RowsTile w;
     if (!rows_tile<T>(a, BM, BN, nt, w)) return;
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid / WAVE);
@@ -110,7 +132,7 @@ __global__ void __launch_bounds__(WAVES_M * WAVES_N * WAVE, 2) k_gmm_mx4(GmmArgs
     auto run = [&](auto far) {
         constexpr bool WIDE = decltype(far)::value;
         struct Raw { uint4 v[sizeof(T) / 2]; };
-        Raw kept[ASYNC ? 1 : TL::LOADS];
+        Raw kept[ASYNC ? 1 : STAGES][ASYNC ? 1 : TL::LOADS];
         uint32_t kept_codes[STAGES][WORDS], kept_scale[STAGES];   // step t's in t % STAGES
         // Workgroups begin at different steps and go round, so that they don't all read lines that begin in the same memory channels; what is left
         // of the lines behind whole steps comes last.
@@ -147,21 +169,21 @@ __global__ void __launch_bounds__(WAVES_M * WAVES_N * WAVE, 2) k_gmm_mx4(GmmArgs
                     const int valid = left - TL::piece_of(tid, i) * 8;
 #pragma unroll
                     for (int j = 0; j < (int)sizeof(T) / 2; ++j)
-                        kept[i].v[j] = left == STEP_C ? load_any(reinterpret_cast<const char *>(p + j * PIECE<T>)) : load_piece(p + j * PIECE<T>, valid - j * PIECE<T>);
+                        kept[slot][i].v[j] = left == STEP_C ? load_any(reinterpret_cast<const char *>(p + j * PIECE<T>)) : load_piece(p + j * PIECE<T>, valid - j * PIECE<T>);
                 }
             }
         };
         auto stash = [&](int t_, auto slot_) {
             constexpr int slot = decltype(slot_)::value;
             if constexpr (!ASYNC) {
-                char *to = lds + slot * X_BYTES;
+                char *to = lds + slot % X_STEPS * X_BYTES;
 #pragma unroll
                 for (int i = 0; i < TL::LOADS; ++i) {
                     if constexpr (PARTS == 1) {
-                        *reinterpret_cast<uint4 *>(to + (i * THREADS + tid) * 16) = kept[i].v[0];
+                        *reinterpret_cast<uint4 *>(to + (i * THREADS + tid) * 16) = kept[slot][i].v[0];
                     } else {
                         bf16x8 p[PARTS];
-                        split<T>(__builtin_bit_cast(decltype(Vec<T, 8>{}), kept[i]).e, p);
+                        split_finite(__builtin_bit_cast(decltype(Vec<T, 8>{}), kept[slot][i]).e, p);
 #pragma unroll
                         for (int k = 0; k < PARTS; ++k) *reinterpret_cast<bf16x8 *>(to + k * TL::BYTES + (i * THREADS + tid) * 16) = p[k];
                     }
@@ -203,7 +225,7 @@ __global__ void __launch_bounds__(WAVES_M * WAVES_N * WAVE, 2) k_gmm_mx4(GmmArgs
         // step on its way behind the first reads (before them, the waves wait for its addresses to be taken).
         constexpr int AT_ONCE = TM < 4 ? TM : 4, PER_PART = TM / AT_ONCE, PER_HALF = PARTS * PER_PART, PORTIONS = 2 * PER_HALF;
         auto multiply = [&](int slot, auto load) {
-            const char *from = lds + slot * X_BYTES, *from_r = lds_r + slot % 2 * TR::BYTES;
+            const char *from = lds + slot % X_STEPS * X_BYTES, *from_r = lds_r + slot % 2 * TR::BYTES;
             Frag<S> fr[2][TN], fl[2][AT_ONCE];
             auto read = [&](auto portion) {
                 constexpr int q = decltype(portion)::value, h = q / PER_HALF, p = PARTS - 1 - q % PER_HALF / PER_PART, i0 = q % PER_PART * AT_ONCE;
@@ -255,23 +277,35 @@ __global__ void __launch_bounds__(WAVES_M * WAVES_N * WAVE, 2) k_gmm_mx4(GmmArgs
             if constexpr (decltype(slot)::value < STAGES - 1) fetch(decltype(slot)::value, slot);
         });
         stash(0, integral_constant<int, 0>{});
-        for (int t0 = 0; t0 < steps; t0 += STAGES) {
-            each_slot([&](auto slot_) {
+        // This wave's part of the step is in LDS (loads come back in order: all but those of the steps behind it), and what it read of the step before
+        // has come; then everyone's is, and nobody reads the places of the step before any more.
+        auto meet = [&](auto later) {
+            constexpr int LATER = decltype(later)::value;
+            static_assert(LATER < 16, "what the counter's low bits hold");
+            asm volatile("" ::: "memory");
+            __builtin_amdgcn_s_waitcnt(ASYNC ? 0x0070 | LATER : 0xc07f);   // (registers are waited for where they are used)
+            __builtin_amdgcn_s_barrier();
+            asm volatile("" ::: "memory");
+        };
+        int t0 = 0;
+        for (; t0 + STAGES <= steps; t0 += STAGES)
+            each_slot([&](auto slot_) {   // (the last ones fetch steps that are not there: zeros, and no branch for which registers of loads under way would be moved)
                 constexpr int slot = decltype(slot_)::value, NEXT = (slot + 1) % STAGES, LAST = (slot + STAGES - 1) % STAGES;
-                const int t = t0 + slot;   // (up to STAGES - 1 steps are not there: zeros, and no branch for which registers of loads under way would be moved)
-                // This wave's part of the step is in LDS (loads come back in order: all but those of the steps behind it), and what it read of the step before
-                // has come; then everyone's is, and nobody reads the places of the step before any more.
-                constexpr int LATER = (STAGES - 2) * (2 + (ASYNC ? TL::LOADS : 0));
-                static_assert(LATER < 16, "what the counter's low bits hold");
-                asm volatile("" ::: "memory");
-                __builtin_amdgcn_s_waitcnt(0x0070 | LATER);
-                __builtin_amdgcn_s_barrier();
-                asm volatile("" ::: "memory");
+                const int t = t0 + slot;
+                meet(integral_constant<int, (STAGES - 2) * (2 + (ASYNC ? TL::LOADS : 0))>{});
                 multiply(slot, [&] { fetch(t + STAGES - 1, integral_constant<int, LAST>{}); });
                 if (ASIDE && t % 4 == 3) put_aside();
                 stash(t + 1, integral_constant<int, NEXT>{});
             });
-        }
+        each_slot([&](auto slot_) {   // (fewer than STAGES are left, and all of them are under way)
+            constexpr int slot = decltype(slot_)::value;
+            if constexpr (slot < STAGES - 1)
+                if (t0 + slot < steps) {
+                    meet(integral_constant<int, 0>{});
+                    multiply(slot, [] {});
+                    stash(t0 + slot + 1, integral_constant<int, slot + 1>{});
+                }
+        });
         asm volatile("" ::: "memory");
         __builtin_amdgcn_s_waitcnt(0x0f70);   // vmcnt(0): steps that are not there also write their zeros to LDS, where the results go now
         asm volatile("" ::: "memory");
@@ -445,12 +479,13 @@ template <class T, bool RCOL> hipError_t pick(const GmmArgs &a, const Mx4Args &m
             });
         }
     }
-    // (single precision: tiles of 128 x 128 take 367 us for 2048 rows of 4096, 4096 columns, of 64 x 64 369, and 185 and 105 for 512)
-    if constexpr (sizeof(T) == 4) return launch_tile<T, RCOL, 64, 64, 4, 1, false>(a, m, s);
+    // (single precision, 4096 columns and c = 4096: tiles of 128 x 128 were as fast for 2048 rows as those of 64 x 64, 367 us and 369, and slower for 512, 185 and 105;
+    // these take 340 and 93 since)
+    if constexpr (sizeof(T) == 4) return launch_tile<T, RCOL, 64, 64, 4, 1, false, 4>(a, m, s);
     else {
         constexpr TileTimes TIMES = {26, 10, 0.0555, 74, 50, 104, 92};
         const int lines = pick_lines(a, TIMES, straight);
-        if (!straight) return lines == 64 ? launch_tile<T, RCOL, 64, 64, 4, 1, false>(a, m, s) : launch_tile<T, RCOL, 128, 128, 2, 2, false>(a, m, s);
+        if (!straight) return lines == 64 ? launch_tile<T, RCOL, 64, 64, 4, 1, false, 4>(a, m, s) : launch_tile<T, RCOL, 128, 128, 2, 2, false>(a, m, s);
         if (lines == 64) return launch_tile<T, RCOL, 64, 64, 4, 1, true, 4>(a, m, s);
         return lines == 128 ? launch_tile<T, RCOL, 128, 128, 2, 2, true>(a, m, s) : launch_tile<T, RCOL, 256, 256, 2, 4, true>(a, m, s);
     }
