@@ -53,12 +53,13 @@ __global__ void __launch_bounds__(WAVES_M * WAVES_N * WAVE, 2) k_gmm_mx4_mx4(Gmm
     for (int i = 0; i < TL::LOADS; ++i) off_l[i] = (uint32_t)(tile_row(a, w, TL::line_of(tid, i)) - first) * (uint32_t)x.ld_codes + TL::piece_of(tid, i) * 16;
 #pragma unroll
     for (int i = 0; i < TR::LOADS; ++i) off_r[i] = (uint32_t)min(TR::line_of(tid, i), (int)a.n - 1 - w.n0) * (uint32_t)m.ld_codes + TR::piece_of(tid, i) * 16;
-    // (a wave's lines are all of one operand; where there are more threads than lines, some load the same)
+    // (a wave's lines are all of one operand; where there are more threads than lines, some load the same.  The matrix's lie as a wave takes them, 16 side by side: as
+    // 1 line in 4, 16 bytes each, they met on the same banks, a third of the cycles that LDS was used)
     const uint8_t *l_scales = x.scales + first * x.ld_scales, *r_scales = w_scales + (int64_t)w.n0 * m.ld_scales;
 #pragma unroll
     for (int i = 0; i < SCALE_LOADS; ++i) {
         const int line = (i * THREADS + tid) % LINES;
-        off_s[i] = line < BM ? (uint32_t)(tile_row(a, w, line) - first) * (uint32_t)x.ld_scales : (uint32_t)min(line - BM, (int)a.n - 1 - w.n0) * (uint32_t)m.ld_scales;
+        off_s[i] = line < BM ? (uint32_t)(tile_row(a, w, line) - first) * (uint32_t)x.ld_scales : (uint32_t)min(tile_line<true>((line - BM) / 16, line % 16), (int)a.n - 1 - w.n0) * (uint32_t)m.ld_scales;
     }
     // (the order of the steps is that of k_gmm_mx4, by periods)
     const int whole = (int)(a.c / (STEP_BLOCKS * MX4_BLOCK)), periods = whole / 2, turn = periods == 0 ? 0 : (w.n0 / BN + w.group * 5) % periods;
@@ -118,7 +119,7 @@ __global__ void __launch_bounds__(WAVES_M * WAVES_N * WAVE, 2) k_gmm_mx4_mx4(Gmm
             if constexpr (i0 == 0) {
                 TR::template read<h>(from + TL::BYTES, at_r, fr[h]);
 #pragma unroll
-                for (int j = 0; j < TN; ++j) sr[h][j] = scales[(BM + wn + tile_line<true>(j, r)) * 4 + h] >> (8 * g);
+                for (int j = 0; j < TN; ++j) sr[h][j] = scales[(BM + wn + j * 16 + r) * 4 + h] >> (8 * g);
             }
             TL::template read<h>(from + tile_line<false>(i0, 0) * LINE, at_l, fl[p & 1]);
 #pragma unroll
