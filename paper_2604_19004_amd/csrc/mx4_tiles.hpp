@@ -211,18 +211,17 @@ inline dim3 few_grid(const GmmArgs &a, int rows, int cols)
 {
     return dim3((uint32_t)((a.n + cols - 1) / cols), (uint32_t)(a.rows / rows + std::min(a.groups, a.rows)) + 1);
 }
-// Columns of a workgroup of few rows, and its waves: calls launch(TN, WAVES) as constants.  64 columns where that leaves two workgroups a compute unit, else 32; short
-// lines in fewer waves.
-inline bool fills_chip(const GmmArgs &a) { return std::min(a.groups, a.rows) * ((a.n + 63) / 64) >= 512; }
+// Columns of a workgroup of few rows, and its waves: calls launch(TN, WAVES) as constants.  64 columns where that leaves two workgroups a compute unit, else 32; eight
+// waves to a long line where there are fewer workgroups than that all the same, else four (rows of bfloat16, us with four and eight: one group of 8 rows, 8192 x 4096,
+// 14.4 and 11.4, one row, 28000 x 8192, 34 and 29; two groups of one row, 4096 x 8192, 11.6 and 12.5, sixteen of four, 4096 x 4096, 31 and 35).
+inline int64_t few_columns(const GmmArgs &a, int cols) { return std::min(a.groups, a.rows) * ((a.n + cols - 1) / cols); }
+inline bool fills_chip(const GmmArgs &a) { return few_columns(a, 64) >= 512; }
 template <class Launch> hipError_t with_columns_and_waves(const GmmArgs &a, Launch launch)
 {
     using std::integral_constant;
-    auto with_waves = [&](auto tn) {
-        if (a.c >= 4096) return launch(tn, integral_constant<int, 8>{});
-        return launch(tn, integral_constant<int, 4>{});
-    };
-    if (fills_chip(a)) return with_waves(integral_constant<int, 4>{});
-    return with_waves(integral_constant<int, 2>{});
+    if (fills_chip(a)) return launch(integral_constant<int, 4>{}, integral_constant<int, 4>{});
+    if (a.c < 4096 || few_columns(a, 32) >= 512) return launch(integral_constant<int, 2>{}, integral_constant<int, 4>{});
+    return launch(integral_constant<int, 2>{}, integral_constant<int, 8>{});
 }
 
 // Which tiles: those that take the least by what was measured at c = 4096, us for n of them: of 64 x 64 one a compute unit, or so much for all and each; of
