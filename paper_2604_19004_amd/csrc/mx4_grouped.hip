@@ -454,7 +454,7 @@ template <class T, bool RCOL, int BM, int BN, int WAVES_M, int WAVES_N, bool ASY
 }
 
 // Rows are few where the matrix's bytes are the time: up to 20 a group, and up to 64 where there are not enough groups and columns for the chip (4096 x 4096, us in k_few_mx4
-// and in tiles: eight groups of 8 rows 21 and 35, of 16 25 and 35, of 24 45 and 35; one group of 16 12 and 25, of 40 17 and 24, of 64 21 and 24).
+// and in tiles: eight groups of 8 rows 19 and 35, of 16 22 and 35, of 24 45 and 35; one group of 16 12 and 25, of 40 17 and 24, of 64 21 and 24).
 bool few_rows(const GmmArgs &a)
 {
     const int64_t groups = std::min(a.groups, a.rows);

@@ -151,7 +151,7 @@ class Mx4:
     """A matrix [rows, inner] or matrices [count, rows, inner] in microscaled four bits (e2m1 codes with an e8m0 scale for every 32 numbers of a row).  codes:
     uint8 [.., rows, 16 * blocks], two numbers a byte, the earlier one in the low half, rows at multiples of 16 bytes; scales: uint8 [.., rows, blocks up to
     a multiple of 16] (those behind the blocks do not count), rows at multiples of 16 bytes; a number is its code's value times 2^(scale - 127), 255 makes a
-    block of NaN.  blocks = (inner + 31) // 32, and codes behind `inner` do not count.  Slices of the matrices or of rows are made from slices of both arrays."""
+    block of NaN.  blocks = (inner + 31) // 32, and codes behind `inner` do not count; shape is ((count,) rows, inner).  Slices of the matrices or of rows are made from slices of both arrays."""
     codes: "object"
     scales: "object"
     inner: int
@@ -168,7 +168,7 @@ class Mx4:
         ldc, sc = _apart(c, "codes", 16)
         lds, ss = _apart(s, "scales", 16)
         count, rows = (1, c.shape[0]) if c.dim() == 2 else c.shape[:2]
-        self.__dict__.update(_struct=ocean_mx4(count, rows, self.inner, _ptr(c), ldc, sc, _ptr(s), lds, ss))
+        self.__dict__.update(shape=(*c.shape[:-1], self.inner), _struct=ocean_mx4(count, rows, self.inner, _ptr(c), ldc, sc, _ptr(s), lds, ss))
 
     @classmethod
     def _made(cls, shape, device):
@@ -180,17 +180,13 @@ class Mx4:
         codes, scales = torch.empty((*many, width), dtype=torch.uint8, device=device), torch.empty((*many, up), dtype=torch.uint8, device=device)
         count, rows = many if len(many) == 2 else (1, many[0])
         q = object.__new__(cls)
-        q.__dict__.update(codes=codes, scales=scales, inner=inner,
+        q.__dict__.update(codes=codes, scales=scales, inner=inner, shape=(*many, inner),
                           _struct=ocean_mx4(count, rows, inner, _ptr(codes), width, rows * width, _ptr(scales), up, rows * up))
         return q
 
     def __reduce__(self):
         """Copies and pickles are made of the fields: the struct holds pointers to this one's arrays."""
         return Mx4, (self.codes, self.scales, self.inner)
-
-    @property
-    def shape(self):
-        return (*self.codes.shape[:-1], self.inner)
 
     @classmethod
     def laid_out(cls, codes, scales, inner: int) -> "Mx4":
@@ -247,9 +243,10 @@ def mx4_dequantize(q: Mx4, dtype=None, *, out=None, stream=None):
     code = _code(dtype)
     s, here = _at(dev, stream, q.codes, q.scales, out)
     with here:
-        out = _output(out, q.shape, q.codes.new_empty(0, dtype=dtype))
-        if out.dtype != dtype or out.device != dev:
-            raise ValueError(f"out is {out.dtype} on {out.device}, not {dtype} on {dev}")
+        if out is None:
+            out = torch.empty(q.shape, dtype=dtype, device=dev)
+        elif tuple(out.shape) != q.shape or out.dtype != dtype or out.device != dev:
+            raise ValueError(f"out must be {q.shape} {dtype} on {dev}, not {tuple(out.shape)} {out.dtype} on {out.device}")
         ld, stride = _cube(out, "out")
         _b._check(lib.ocean_mx4_dequantize(C.byref(q._struct), code, _ptr(out), ld, stride, s))
     return out
@@ -262,7 +259,10 @@ def grouped_matmul_mx4(x, w: Mx4, expert_ptr, *, rows=None, transposed: bool = F
     import torch
     lib = load()
     if len(w.shape) != 3:
-        raise ValueError(f"w must be [experts, outer, inner], not {tuple(w.shape)}")
+        raise ValueError(f"w must be [experts, outer, inner], not {w.shape}")
+    count, outer, inner = w.shape
+    if transposed:
+        outer, inner = inner, outer
     four = isinstance(x, Mx4)
     first = x.codes if four else x
     dev = first.device
@@ -277,8 +277,7 @@ def grouped_matmul_mx4(x, w: Mx4, expert_ptr, *, rows=None, transposed: bool = F
         dtype = x.dtype
     code = _code(dtype)
     g = _groups(first, expert_ptr, rows)
-    outer, inner = (w.shape[2], w.shape[1]) if transposed else (w.shape[1], w.shape[2])
-    if w.shape[0] != g.experts or inner != x.shape[1] or w.codes.device != dev:
+    if count != g.experts or inner != x.shape[1] or w.codes.device != dev:
         raise ValueError(f"w is {w.shape}{' (transposed)' if transposed else ''} on {w.codes.device}: not {g.experts} matrices for rows of {x.shape[1]} on {dev}")
     held = (x.codes, x.scales) if four else (x,)
     s, here = _at(dev, stream, *held, w.codes, w.scales, expert_ptr, rows, out)
