@@ -47,7 +47,6 @@ template <class T, int G, int NV> __device__ __forceinline__ void offsets_of(uin
 #pragma unroll
     for (int i = 0; i < NV; ++i) at[i] = i * G + sub < experts ? (uint32_t)((row * ld + i * G + sub) * (int64_t)sizeof(T)) : NOWHERE;
 }
-template <class T> using Bits = std::conditional_t<sizeof(T) == 4, uint32_t, uint16_t>;
 template <class T> __device__ __forceinline__ T load_one(Memory m, uint32_t at)
 {
     if constexpr (sizeof(T) == 4) return __builtin_bit_cast(T, (uint32_t)__builtin_amdgcn_raw_buffer_load_b32(m, at, 0, 0));
@@ -98,7 +97,8 @@ __device__ __forceinline__ float row_softmax(const T (&row)[NV], const uint32_t 
     return there ? sum : 0.0f;
 }
 
-// G lanes share a row and keep their columns' sums over all rows that they see; those of a workgroup meet in LDS in a fixed order.
+// G lanes share a row and keep their columns' sums over all rows that they see; those of a workgroup meet in LDS in a fixed order.  65536 rows of 100, f32: 9.6 us for
+// 26 MB, of which 856 instructions a wave, four waves to a SIMD, are 6.
 template <class T, int G, int NV>
 __global__ void __launch_bounds__(SUM_TPB) k_balance(const T *logits, int64_t ld, int64_t tokens, int experts, BalanceSpace w)
 {
@@ -168,7 +168,7 @@ template <class V> __device__ __forceinline__ V wave_total(V v)
     return v;
 }
 
-// The workgroups' sums together, in 64 bits: 1024 / experts threads an expert, each every so many workgroups.  A chain of two trips to memory and three barriers.
+// The workgroups' sums together, in 64 bits: 1024 / experts threads an expert, each every so many workgroups.  A chain of two trips to memory and three barriers, 5 to 6 us.
 __global__ void __launch_bounds__(FINISH_TPB) k_balance_finish(const int64_t *expert_ptr, int experts, int blocks, BalanceSpace w, ocean_balance out)
 {
     constexpr int WAVES = FINISH_TPB / WAVE, DEEP = 32;
@@ -226,7 +226,7 @@ __global__ void __launch_bounds__(FINISH_TPB) k_balance_finish(const int64_t *ex
 }
 
 // dl_c = p_c (a (f_c - sum f p) + b lse) with f the experts' shares of the entries, a = dloss[0] experts / rows and b = 2 dloss[1] / rows; with `dval` what
-// k_route_backward gives beside it.
+// k_route_backward gives beside it.  65536 rows of 100, k 8, f32: 21 us for 59 MB (4.9 at the rate of a copy would be 12); 1315 instructions a wave are 12 of them.
 template <class T, int G, int NV, bool WEIGHTS>
 __global__ void __launch_bounds__(TPB) k_balance_backward(ocean_balance b, ocean_routing r, const float *dloss, const float *dval, const T *logits,
                                                           int64_t ld, int normalize, T *dlogits, int64_t ldd)

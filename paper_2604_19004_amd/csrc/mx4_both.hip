@@ -28,6 +28,8 @@ __device__ __forceinline__ u32x4 first_codes(u32x4 v, int valid)
 
 // A tile, STAGES steps of 128 bytes of c (256 numbers) of both operands in LDS, and the scales of the periods of two steps that they belong to: 16
 // bytes of a line at a time (4 bytes a step, each a line of memory looked up, cost more than the codes: 32668 rows of 4096 by eight 8192 x 4096 746 us).
+// There now 650 to 690 us, 3.2 to 3.4 PFLOP/s; matrix cores are busy 43 %, LDS 34 %.  A step is a chain: without its loads it would be a sixth shorter, with a quarter of its
+// products a quarter, and a tile's 16 steps have a beginning and an end that nothing overlaps, as one workgroup fills a compute unit's LDS.
 template <class O, int BM, int BN, int WAVES_M, int WAVES_N, int STAGES>
 __global__ void __launch_bounds__(WAVES_M * WAVES_N * WAVE, 2) k_gmm_mx4_mx4(GmmArgs a, Mx4Args x, Mx4Args m, int nt)
 {

@@ -79,7 +79,8 @@ template <bool RCOL, int BN, int THREADS> __device__ __forceinline__ bool any_fa
 
 // A tile: x straight to LDS (16 bits, whole pieces) or through registers, where single precision is split; the matrix's codes through registers, where they are widened.
 // STAGES steps are under way, in LDS or registers: the next one, or in small tiles, which wait for memory, three (512 rows of 4095 by 4095 x 4096, bfloat16, through
-// registers: 58 us and 50).
+// registers: 58 us and 50).  Large ones are bound by the matrix cores under the card's power: 32668 rows by eight 8192 x 4096, bf16, 1811 us, 1210 TFLOP/s; small and short
+// ones by the way of a step, which has loads, LDS and matrix cores one after the other.
 template <class T, bool RCOL, int BM, int BN, int WAVES_M, int WAVES_N, bool ASYNC, int STAGES>
 __global__ void __launch_bounds__(WAVES_M * WAVES_N * WAVE, 2) k_gmm_mx4(GmmArgs a, Mx4Args m, int nt)
 {
@@ -327,7 +328,8 @@ __global__ void __launch_bounds__(WAVES_M * WAVES_N * WAVE, 2) k_gmm_mx4(GmmArgs
 }
 
 // Few rows: the matrix is read once, straight into registers.  A lane's 32 numbers of c are those of its block, in four matrix instructions; x is read
-// to match.
+// to match.  Bound by the matrix's bytes: sixteen groups of 4 rows, 4096 x 4096, 31 us, 4.6 TB/s; two of one row, 8192 x 4096, 11.3 us, 3.2 TB/s, where the beginning is a third.
+// Two steps under way a wave: with one 16 and 36 us, with four, or registers cut to four waves a SIMD, 12 and 31, 15 and 40.
 template <class T, int ROWS, int TN, int WAVES>
 __global__ void __launch_bounds__(WAVES * WAVE, 2) k_few_mx4(GmmArgs a, Mx4Args m)
 {
