@@ -75,18 +75,18 @@ int ocean_mx4_dequantize(const ocean_mx4 *q, int32_t dtype, void *out, int64_t l
 /*
  * As ocean_grouped_matmul, with matrices in four bits: y[s] = x[row(s)] * W_e^T for the rows of group e (transposed == 0; x: x_rows x w->inner, y: rows x
  * w->rows), or y[s] = x[row(s)] * W_e (transposed != 0; x: x_rows x w->rows, y: rows x w->inner), which is the gradient of x's rows.
- * w->count is the groups' `experts`, and its row strides are below 2^23.  The matrices' numbers are taken as they are, x's too: as the type they have, float16 where the matrices' numbers are beyond it and
- * single precision as the exact sum of two and three bfloat16 numbers (what is left of a number below 2^-133 is not kept).
- * Beside float16 rows, matrices' numbers of scales up to 51 (below 2^-73) count as 0, also where x is infinite.
+ * w->count is the groups' `experts`, and its row strides are below 2^23.  The matrices' numbers are taken as they are, x's too: in the type they have, or, float16
+ * where the matrices' numbers are beyond it and single precision, as the exact sum of two and three bfloat16 numbers (what is left of a number below 2^-133 is not kept).
+ * Beside float16 rows, matrices' numbers of scales up to 51 (below 2^-73) may count as 0, also where x is infinite.
  * One launch has fewer than 2^32 threads.  In tiles of 256 x 256 that is 2^23 (16 bits, rows at 16 bytes), of 128 x 128 2^24 (16 bits), of 64 x 64 2^24 (single precision),
  * those that groups' last tiles add among them: what has more is refused.
  */
 int ocean_grouped_matmul_mx4(const ocean_groups *g, int32_t dtype, const void *x, int64_t ld_x, const ocean_mx4 *w, int32_t transposed, void *y,
                              int64_t ld_y, ocean_stream_t stream);
 
-/* The same with x in four bits too (one matrix, x->count == 1, x->rows == x_rows, x->inner == w->inner); y has type dtype.  (Tiles as above, of 256 x 256 for results of 16
- * bits.)  Codes or scales of x that span 4 GB or more and
- * are gathered go 16 rows at a time: there rows / 16 + groups may be up to 65533 and w->rows below 2^27, and more is refused. */
+/* The same with x in four bits too (one matrix, x->count == 1, x->rows == x_rows, x->inner == w->inner); y has type dtype.  (Tiles as above, of 256 x 256
+ * for results of 16 bits.)  Codes or scales of x that span 4 GB or more and are gathered go 16 rows at a time: there rows / 16 + groups may be up to 65533 and w->rows
+ * below 2^27, and more is refused. */
 int ocean_grouped_matmul_mx4_mx4(const ocean_groups *g, const ocean_mx4 *x, const ocean_mx4 *w, int32_t dtype, void *y, int64_t ld_y,
                                  ocean_stream_t stream);
 
