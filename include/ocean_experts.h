@@ -41,7 +41,8 @@ int ocean_route_balance(const ocean_routing *r, const void *logits, int32_t dtyp
  * Gradient of the logits from that of the losses, dloss[2].  counts count as constants; counts and rows of `b` are read (those of all
  * devices, where a program has added them up), its loss and prob are not (they may be NULL).
  * dval: NULL, or tokens * k gradients of the routing's weights: what ocean_route_backward gives for them (normalize as there; reads row_ptr,
- * col_idx and val) is added before the one rounding to the logits' type.  Masked logits get 0.
+ * col_idx and val; the columns of a row differ, as ocean_route makes them) is added before the one rounding to the logits' type.
+ * Masked logits get 0.
  */
 int ocean_route_balance_backward(const ocean_balance *b, const ocean_routing *r, const void *logits, int32_t dtype, int64_t ld, const float *dloss,
                                  const float *dval, int32_t normalize, void *dlogits, int64_t ld_dlogits, ocean_stream_t stream);
