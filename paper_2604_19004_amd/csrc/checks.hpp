@@ -11,11 +11,15 @@ namespace {
 
 inline int bad(const char *msg) { return set_error(OCEAN_EINVAL, msg); }
 
-inline int launched(hipError_t e, const char *what)
+// (header: where the sizes of the operator stand)
+inline int launched(hipError_t e, const char *what, const char *header)
 {
     if (e == hipSuccess) return OCEAN_OK;
-    if (e == TOO_MANY_TILES) return bad("the result has more tiles than one launch takes (see the sizes in ocean_routed.h)");
     char msg[256];
+    if (e == TOO_MANY_TILES) {
+        std::snprintf(msg, sizeof msg, "the result has more tiles than one launch takes (see the sizes in %s)", header);
+        return bad(msg);
+    }
     std::snprintf(msg, sizeof msg, "%s: %s", what, hipGetErrorString(e));
     return set_error(OCEAN_EHIP, msg);
 }

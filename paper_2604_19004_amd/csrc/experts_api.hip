@@ -4,6 +4,8 @@
 
 using namespace ocean;
 
+static constexpr char HEADER[] = "ocean_experts.h";
+
 namespace {
 
 // Null where the matrices are fine (their places, and that rows and matrices that are written lie apart).
@@ -72,7 +74,7 @@ int ocean_route_balance(const ocean_routing *r, const void *logits, int32_t dtyp
     if (!out || !out->loss || !out->counts || !out->prob || !out->rows) return bad("the balance or an array of it is null");
     if (!workspace || !aligned(workspace, 256) || workspace_bytes < balance_workspace(r->tokens, r->experts))
         return bad("workspace is null, not aligned to 256 bytes or smaller than ocean_route_balance_workspace");
-    return launched(launch_balance(*r, logits, dtype, ld, *out, workspace, static_cast<hipStream_t>(stream)), "ocean_route_balance");
+    return launched(launch_balance(*r, logits, dtype, ld, *out, workspace, static_cast<hipStream_t>(stream)), "ocean_route_balance", HEADER);
 }
 
 int ocean_route_balance_backward(const ocean_balance *b, const ocean_routing *r, const void *logits, int32_t dtype, int64_t ld, const float *dloss,
@@ -85,19 +87,19 @@ int ocean_route_balance_backward(const ocean_balance *b, const ocean_routing *r,
     REFUSE(logits_fault(logits, r, ld, dtype));
     REFUSE(logits_fault(dlogits, r, ld_dlogits, dtype));
     return launched(launch_balance_backward(*b, *r, logits, dtype, ld, dloss, dval, normalize != 0, dlogits, ld_dlogits, static_cast<hipStream_t>(stream)),
-                    "ocean_route_balance_backward");
+                    "ocean_route_balance_backward", HEADER);
 }
 
 int ocean_mx4_quantize(const void *x, int32_t dtype, int64_t ld_x, int64_t stride_x, const ocean_mx4 *q, ocean_stream_t stream)
 {
     REFUSE(converted_fault(q, x, dtype, ld_x, stride_x, true));
-    return launched(launch_mx4_quantize(x, dtype, ld_x, stride_x, *q, static_cast<hipStream_t>(stream)), "ocean_mx4_quantize");
+    return launched(launch_mx4_quantize(x, dtype, ld_x, stride_x, *q, static_cast<hipStream_t>(stream)), "ocean_mx4_quantize", HEADER);
 }
 
 int ocean_mx4_dequantize(const ocean_mx4 *q, int32_t dtype, void *out, int64_t ld_out, int64_t stride_out, ocean_stream_t stream)
 {
     REFUSE(converted_fault(q, out, dtype, ld_out, stride_out, false));
-    return launched(launch_mx4_dequantize(*q, dtype, out, ld_out, stride_out, static_cast<hipStream_t>(stream)), "ocean_mx4_dequantize");
+    return launched(launch_mx4_dequantize(*q, dtype, out, ld_out, stride_out, static_cast<hipStream_t>(stream)), "ocean_mx4_dequantize", HEADER);
 }
 
 int ocean_grouped_matmul_mx4(const ocean_groups *g, int32_t dtype, const void *x, int64_t ld_x, const ocean_mx4 *w, int32_t transposed, void *y,
@@ -108,7 +110,7 @@ int ocean_grouped_matmul_mx4(const ocean_groups *g, int32_t dtype, const void *x
     REFUSE(product_fault(w, g));
     REFUSE(matrix_fault(x, g->x_rows, transposed ? w->rows : w->inner, ld_x, dtype));
     REFUSE(matrix_fault(y, g->rows, transposed ? w->inner : w->rows, ld_y, dtype));
-    return launched(launch_grouped_mx4(*g, dtype, x, ld_x, *w, transposed != 0, y, ld_y, static_cast<hipStream_t>(stream)), "ocean_grouped_matmul_mx4");
+    return launched(launch_grouped_mx4(*g, dtype, x, ld_x, *w, transposed != 0, y, ld_y, static_cast<hipStream_t>(stream)), "ocean_grouped_matmul_mx4", HEADER);
 }
 
 int ocean_grouped_matmul_mx4_mx4(const ocean_groups *g, const ocean_mx4 *x, const ocean_mx4 *w, int32_t dtype, void *y, int64_t ld_y,
@@ -120,7 +122,7 @@ int ocean_grouped_matmul_mx4_mx4(const ocean_groups *g, const ocean_mx4 *x, cons
     REFUSE(product_fault(w, g));
     if (x->count != 1 || x->rows != g->x_rows || x->inner != w->inner) return bad("x must be one matrix of x_rows rows with the matrices' inner");
     REFUSE(matrix_fault(y, g->rows, w->rows, ld_y, dtype));
-    return launched(launch_grouped_mx4_mx4(*g, *x, *w, dtype, y, ld_y, static_cast<hipStream_t>(stream)), "ocean_grouped_matmul_mx4_mx4");
+    return launched(launch_grouped_mx4_mx4(*g, *x, *w, dtype, y, ld_y, static_cast<hipStream_t>(stream)), "ocean_grouped_matmul_mx4_mx4", HEADER);
 }
 
 }  // extern "C"

@@ -3,6 +3,8 @@
 
 using namespace ocean;
 
+static constexpr char HEADER[] = "ocean_routed.h";
+
 extern "C" {
 
 size_t ocean_route_workspace(int64_t tokens, int64_t experts, int32_t k)
@@ -20,7 +22,7 @@ int ocean_route(const void *logits, int32_t dtype, int64_t ld, int32_t normalize
     const size_t need = route_workspace(out->tokens, out->experts, out->k);
     if (need > 0 && (!workspace || !aligned(workspace, 256) || workspace_bytes < need))
         return bad("workspace is null, not aligned to 256 bytes or smaller than ocean_route_workspace");
-    return launched(launch_route(logits, dtype, ld, normalize != 0, *out, workspace, static_cast<hipStream_t>(stream)), "ocean_route");
+    return launched(launch_route(logits, dtype, ld, normalize != 0, *out, workspace, static_cast<hipStream_t>(stream)), "ocean_route", HEADER);
 }
 
 int ocean_route_backward(const ocean_routing *r, const float *dval, const void *logits, int32_t dtype, int64_t ld, int32_t normalize,
@@ -32,7 +34,7 @@ int ocean_route_backward(const ocean_routing *r, const float *dval, const void *
     if (!normalize) REFUSE(matrix_fault(logits, r->tokens, r->experts, ld, dtype));
     REFUSE(matrix_fault(dlogits, r->tokens, r->experts, ld_dlogits, dtype));
     return launched(launch_route_backward(*r, dval, logits, dtype, ld, normalize != 0, dlogits, ld_dlogits, static_cast<hipStream_t>(stream)),
-                    "ocean_route_backward");
+                    "ocean_route_backward", HEADER);
 }
 
 int ocean_combine(const ocean_routing *r, const void *y, int32_t dtype, int64_t width, int64_t ld_y, void *out, int64_t ld_out,
@@ -43,7 +45,7 @@ int ocean_combine(const ocean_routing *r, const void *y, int32_t dtype, int64_t 
     if (r->tokens > 0 && !r->slot) return bad("slot is null");
     REFUSE(matrix_fault(y, r->tokens * r->k, width, ld_y, dtype));
     REFUSE(matrix_fault(out, r->tokens, width, ld_out, dtype));
-    return launched(launch_combine(*r, y, dtype, width, ld_y, out, ld_out, static_cast<hipStream_t>(stream)), "ocean_combine");
+    return launched(launch_combine(*r, y, dtype, width, ld_y, out, ld_out, static_cast<hipStream_t>(stream)), "ocean_combine", HEADER);
 }
 
 int ocean_combine_backward(const ocean_routing *r, const void *dout, int64_t ld_dout, const void *y, int64_t ld_y, int32_t dtype,
@@ -56,7 +58,7 @@ int ocean_combine_backward(const ocean_routing *r, const void *dout, int64_t ld_
     if (dval) REFUSE(matrix_fault(y, r->tokens * r->k, width, ld_y, dtype));
     REFUSE(matrix_fault(dy, r->tokens * r->k, width, ld_dy, dtype));
     return launched(launch_combine_backward(*r, dout, ld_dout, y, ld_y, dtype, width, dy, ld_dy, dval, static_cast<hipStream_t>(stream)),
-                    "ocean_combine_backward");
+                    "ocean_combine_backward", HEADER);
 }
 
 int ocean_grouped_matmul(const ocean_groups *g, int32_t dtype, int64_t inner, int64_t outer, const void *x, int64_t ld_x, const void *w,
@@ -68,7 +70,7 @@ int ocean_grouped_matmul(const ocean_groups *g, int32_t dtype, int64_t inner, in
     REFUSE(matrices_fault(w, g->experts, stride_w, transposed ? inner : outer, transposed ? outer : inner, ld_w, dtype, false));
     REFUSE(matrix_fault(y, g->rows, outer, ld_y, dtype));
     return launched(launch_grouped_matmul(*g, dtype, inner, outer, x, ld_x, w, ld_w, stride_w, transposed != 0, y, ld_y,
-                                          static_cast<hipStream_t>(stream)), "ocean_grouped_matmul");
+                                          static_cast<hipStream_t>(stream)), "ocean_grouped_matmul", HEADER);
 }
 
 int ocean_grouped_weight_grad(const ocean_groups *g, int32_t dtype, int64_t inner, int64_t outer, const void *dy, int64_t ld_dy,
@@ -81,7 +83,7 @@ int ocean_grouped_weight_grad(const ocean_groups *g, int32_t dtype, int64_t inne
     REFUSE(matrix_fault(x, g->x_rows, inner, ld_x, dtype));
     REFUSE(matrices_fault(dw, g->experts, stride_dw, transposed ? inner : outer, transposed ? outer : inner, ld_dw, dtype, true));
     return launched(launch_grouped_weight_grad(*g, dtype, inner, outer, dy, ld_dy, x, ld_x, dw, ld_dw, stride_dw, transposed != 0,
-                                               static_cast<hipStream_t>(stream)), "ocean_grouped_weight_grad");
+                                               static_cast<hipStream_t>(stream)), "ocean_grouped_weight_grad", HEADER);
 }
 
 size_t ocean_adapter_workspace(int64_t rows, int64_t inner, int64_t outer, int64_t adapters, int64_t rank, int32_t dtype)
@@ -109,7 +111,7 @@ int ocean_adapter_matmul(const ocean_adapters *l, const int32_t *ids, int32_t dt
     if (!workspace || !aligned(workspace, 256) || workspace_bytes < adapter_workspace(rows, inner, outer, l->adapters, l->rank, dtype))
         return bad("workspace is null, not aligned to 256 bytes or smaller than ocean_adapter_workspace");
     return launched(launch_adapter(*l, ids, dtype, rows, inner, outer, x, ld_x, w, ld_w, y, ld_y, workspace, static_cast<hipStream_t>(stream)),
-                    "ocean_adapter_matmul");
+                    "ocean_adapter_matmul", HEADER);
 }
 
 }  // extern "C"

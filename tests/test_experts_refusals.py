@@ -1,0 +1,26 @@
+"""What the entry points of ocean_experts.h refuse and what they take, where nothing is launched yet: without a GPU."""
+import ctypes
+import os
+
+import pytest
+
+
+@pytest.fixture(scope="module")
+def ex():
+    from paper_2604_19004_amd import build, experts
+    if not os.path.exists(build.lib_path()):
+        build.build()
+    experts.load()
+    return experts
+
+
+def test_refused_sizes_name_their_header(ex):
+    """What one launch does not take is refused with the header that has the sizes: that of the operator that was called."""
+    lib, b = ex.load(), ctypes.byref
+    n = 1 << 23
+    groups = ex.ocean_groups(n, 1, 0x1000, None, n)
+    tall, rows = ex.ocean_mx4(1, n, 64, 0x1000, 32, 0, 0x1000, 16, 0), ex.ocean_mx4(1, n, 64, 0x1000, 32, 0, 0x1000, 16, 0)
+    for call, header in ((lambda: lib.ocean_grouped_matmul_mx4(b(groups), 1, 0x1000, 64, b(tall), 0, 0x1000, n, None), "ocean_experts.h"),
+                         (lambda: lib.ocean_grouped_matmul_mx4_mx4(b(groups), b(rows), b(tall), 2, 0x1000, n, None), "ocean_experts.h"),
+                         (lambda: lib.ocean_grouped_matmul(b(groups), 1, 64, n, 0x1000, 64, 0x1000, 64, 64 * n, 0, 0x1000, n, None), "ocean_routed.h")):
+        assert call() == 1 and header in lib.ocean_last_error().decode(), (header, lib.ocean_last_error())
