@@ -66,11 +66,12 @@ typedef struct ocean_mx4 {
 /*
  * x, `count` matrices of rows x inner at stride_x elements, into q.  A block's scale is 2^(floor(log2 of its largest magnitude) - 2), not below
  * 2^-127, or 1 where all are 0; its numbers are rounded to the nearest (ties to the even code) and magnitudes beyond 6 become 6.  A block that holds an
- * infinite number or NaN becomes NaN.  Codes behind `inner` are 0, and so are scales' bytes up to the next multiple of 16.  count * rows < 2^31 - 4096.
+ * infinite number or NaN becomes NaN.  Codes behind `inner` are 0, and so are scales' bytes up to the next multiple of 16.  count * rows < 2^31 - 4096, and
+ * count at most OCEAN_GROUPS_MAX.
  */
 int ocean_mx4_quantize(const void *x, int32_t dtype, int64_t ld_x, int64_t stride_x, const ocean_mx4 *q, ocean_stream_t stream);
 
-/* And back: out, count matrices of rows x inner. */
+/* And back: out, count matrices of rows x inner, of the same limits. */
 int ocean_mx4_dequantize(const ocean_mx4 *q, int32_t dtype, void *out, int64_t ld_out, int64_t stride_out, ocean_stream_t stream);
 
 /*

@@ -43,7 +43,7 @@ const char *converted_fault(const ocean_mx4 *q, const void *p, int32_t dtype, in
 {
     if (!known_type(dtype)) return "dtype must be OCEAN_F32, OCEAN_BF16 or OCEAN_F16";
     if (const char *why = mx4_fault(q, to_q)) return why;
-    if (q->count > 0 && q->rows >= MAX_DIM / q->count) return "count * rows of the matrix in four bits must be below 2^31 - 4096";
+    if (q->count * q->rows >= MAX_DIM) return "count * rows of the matrix in four bits must be below 2^31 - 4096";
     return matrices_fault(p, q->count, stride, q->rows, q->inner, ld, dtype, !to_q);
 }
 

@@ -24,3 +24,15 @@ def test_refused_sizes_name_their_header(ex):
                          (lambda: lib.ocean_grouped_matmul_mx4_mx4(b(groups), b(rows), b(tall), 2, 0x1000, n, None), "ocean_experts.h"),
                          (lambda: lib.ocean_grouped_matmul(b(groups), 1, 64, n, 0x1000, 64, 0x1000, 64, 64 * n, 0, 0x1000, n, None), "ocean_routed.h")):
         assert call() == 1 and header in lib.ocean_last_error().decode(), (header, lib.ocean_last_error())
+
+
+def test_rows_of_all_matrices_up_to_the_limit(ex):
+    """Conversions take fewer than 2^31 - 4096 rows in all, whatever the number of matrices divides (rows of no numbers: nothing is launched)."""
+    lib, b = ex.load(), ctypes.byref
+    most = 2 ** 31 - 4096 - 1
+    for count in (1, 2, 3, 7, 16384):
+        rows = most // count
+        fits, beyond = (ex.ocean_mx4(count, r, 0, None, 0, 0, None, 0, 0) for r in (rows, rows + 1))
+        for convert in (lambda q: lib.ocean_mx4_quantize(None, 1, 0, 0, b(q), None), lambda q: lib.ocean_mx4_dequantize(b(q), 1, None, 0, 0, None)):
+            assert convert(fits) == 0, (count, rows, lib.ocean_last_error())
+            assert convert(beyond) == 1 and "2^31" in lib.ocean_last_error().decode() or count == 1
