@@ -22,7 +22,8 @@ extern "C" {
  * prob[e] = the mean of softmax(row)[e], counts[e] = the entries of expert e in the routing (n of all), and
  *   loss[0] = experts * sum over e of counts[e] / n * prob[e]   (1 where all are used evenly),
  *   loss[1] = the mean of logsumexp(row)^2.
- * Without such rows, or without entries, what has no value is 0.  Row strides of logits and of their gradient are below 2^23 elements.
+ * Without such rows, or without entries, what has no value is 0.  Row strides of logits and of their gradient are below 2^23 elements, tokens
+ * at most 2^28.
  */
 typedef struct ocean_balance {
     float *loss;        /* 2 */
@@ -42,7 +43,7 @@ int ocean_route_balance(const ocean_routing *r, const void *logits, int32_t dtyp
  * devices, where a program has added them up), its loss and prob are not (they may be NULL).
  * dval: NULL, or tokens * k gradients of the routing's weights: what ocean_route_backward gives for them (normalize as there; reads row_ptr,
  * col_idx and val; the columns of a row differ, as ocean_route makes them) is added before the one rounding to the logits' type.
- * Masked logits get 0.
+ * Masked logits get 0.  Without dval, only tokens and experts of the routing are read.
  */
 int ocean_route_balance_backward(const ocean_balance *b, const ocean_routing *r, const void *logits, int32_t dtype, int64_t ld, const float *dloss,
                                  const float *dval, int32_t normalize, void *dlogits, int64_t ld_dlogits, ocean_stream_t stream);

@@ -39,12 +39,20 @@ inline const char *matrix_fault(const void *p, int64_t rows, int64_t width, int6
     return nullptr;
 }
 
-inline const char *routing_fault(const ocean_routing *r, bool need_val, bool need_all)
+// (what has no entries of its own: a routing's rows and columns)
+inline const char *routing_size_fault(const ocean_routing *r)
 {
     if (!r) return "the routing is null";
-    if (r->tokens < 0 || r->experts < 1 || r->experts > OCEAN_ROUTE_MAX_EXPERTS) return "tokens or experts out of range (experts <= OCEAN_ROUTE_MAX_EXPERTS)";
+    if (r->tokens < 0 || r->tokens > (1ll << 28) || r->experts < 1 || r->experts > OCEAN_ROUTE_MAX_EXPERTS)
+        return "tokens (at most 2^28) or experts (1 to OCEAN_ROUTE_MAX_EXPERTS) out of range";
+    return nullptr;
+}
+
+inline const char *routing_fault(const ocean_routing *r, bool need_val, bool need_all)
+{
+    if (const char *why = routing_size_fault(r)) return why;
     if (r->k < 1 || r->k > OCEAN_ROUTE_MAX_K || r->k > r->experts) return "k must be 1 to min(experts, OCEAN_ROUTE_MAX_K)";
-    if (r->tokens > (1ll << 28) || r->tokens * r->k >= MAX_DIM) return "tokens * k must be below 2^31 (and tokens at most 2^28)";
+    if (r->tokens * r->k >= MAX_DIM) return "tokens * k must be below 2^31 - 4096";
     if (!r->row_ptr) return "row_ptr is null";
     if (r->tokens > 0 && need_val && !r->val) return "val is null";
     if (need_all && (!r->expert_ptr || (r->tokens > 0 && (!r->col_idx || !r->token || !r->slot)))) return "an array of the routing is null";

@@ -68,7 +68,7 @@ int ocean_route_balance(const ocean_routing *r, const void *logits, int32_t dtyp
                         size_t workspace_bytes, ocean_stream_t stream)
 {
     if (!known_type(dtype)) return bad("dtype must be OCEAN_F32, OCEAN_BF16 or OCEAN_F16");
-    REFUSE(routing_fault(r, false, false));
+    REFUSE(routing_size_fault(r));
     if (!r->expert_ptr) return bad("expert_ptr is null");
     REFUSE(logits_fault(logits, r, ld, dtype));
     if (!out || !out->loss || !out->counts || !out->prob || !out->rows) return bad("the balance or an array of it is null");
@@ -81,7 +81,7 @@ int ocean_route_balance_backward(const ocean_balance *b, const ocean_routing *r,
                                  const float *dval, int32_t normalize, void *dlogits, int64_t ld_dlogits, ocean_stream_t stream)
 {
     if (!known_type(dtype)) return bad("dtype must be OCEAN_F32, OCEAN_BF16 or OCEAN_F16");
-    REFUSE(routing_fault(r, dval != nullptr, false));
+    REFUSE(dval ? routing_fault(r, true, false) : routing_size_fault(r));
     if (dval && r->tokens > 0 && !r->col_idx) return bad("col_idx is null");
     if (!b || !b->counts || !b->rows || !dloss) return bad("the balance, its counts or rows, or dloss is null");
     REFUSE(logits_fault(logits, r, ld, dtype));

@@ -36,3 +36,20 @@ def test_rows_of_all_matrices_up_to_the_limit(ex):
         for convert in (lambda q: lib.ocean_mx4_quantize(None, 1, 0, 0, b(q), None), lambda q: lib.ocean_mx4_dequantize(b(q), 1, None, 0, 0, None)):
             assert convert(fits) == 0, (count, rows, lib.ocean_last_error())
             assert convert(beyond) == 1 and "2^31" in lib.ocean_last_error().decode() or count == 1
+
+
+def test_the_balance_asks_for_what_it_reads(ex):
+    """ocean_route_balance reads tokens, experts and expert_ptr of the routing, its gradient without dval tokens and experts: the other members may hold anything.  (Each call
+    is refused for its workspace or its dlogits, the last arguments that are looked at.)"""
+    lib, b = ex.load(), ctypes.byref
+    out = ex.ocean_balance(0x1000, 0x1000, 0x1000, 0x1000)
+    for k, row_ptr in ((2, None), (0, 0x1000), (-1, None), (70, 0x1000), (1 << 30, None)):
+        r = ex.ocean_routing(1 << 20, 4, k, 0, row_ptr, None, None, 0x1000, None, None)
+        assert lib.ocean_route_balance(b(r), 0x1000, 1, 4, b(out), None, 0, None) == 1 and "workspace" in lib.ocean_last_error().decode(), (k, lib.ocean_last_error())
+        assert lib.ocean_route_balance_backward(b(out), b(r), 0x1000, 1, 4, 0x1000, None, 1, None, 4, None) == 1 and "a matrix is null" in lib.ocean_last_error().decode(), (k, lib.ocean_last_error())
+        # with the gradient of the weights all of it is read
+        assert lib.ocean_route_balance_backward(b(out), b(r), 0x1000, 1, 4, 0x1000, 0x1000, 1, None, 4, None) == 1 and "a matrix is null" not in lib.ocean_last_error().decode()
+    for bad in (ex.ocean_routing(-1, 4, 2, 0, 0x1000, None, None, 0x1000, None, None), ex.ocean_routing((1 << 28) + 1, 4, 2, 0, 0x1000, None, None, 0x1000, None, None),
+                ex.ocean_routing(10, 1025, 2, 0, 0x1000, None, None, 0x1000, None, None), ex.ocean_routing(10, 0, 2, 0, 0x1000, None, None, 0x1000, None, None)):
+        assert lib.ocean_route_balance(b(bad), 0x1000, 1, 1025, b(out), None, 0, None) == 1 and "tokens" in lib.ocean_last_error().decode()
+        assert lib.ocean_route_balance_backward(b(out), b(bad), 0x1000, 1, 1025, 0x1000, None, 1, None, 1025, None) == 1 and "tokens" in lib.ocean_last_error().decode()
