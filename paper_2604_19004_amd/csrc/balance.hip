@@ -12,10 +12,10 @@ constexpr int TPB = 256, SUM_TPB = 1024, FINISH_TPB = 1024;
 constexpr int64_t AT_ONCE = 1536;     // workgroups of the gradient that run together, six a compute unit
 constexpr int64_t MAX_BLOCKS = 256;   // workgroups of the first pass, each of which leaves a sum per expert
 
-// Sums of a workgroup's rows, per expert, of logsumexp^2, and its rows that have an open logit.
+// Sums of a workgroup's rows, per expert, of logsumexp^2 (in 64 bits: those of a mean that single precision has may be beyond it), and its rows that have an open logit.
 struct BalanceSpace {
     float *prob;        // [blocks][experts]
-    float *z;           // [blocks]
+    double *z;          // [blocks]
     int64_t *rows;      // [blocks]
 };
 inline size_t up256(size_t n) { return (n + 255) & ~(size_t)255; }
@@ -26,8 +26,8 @@ inline BalanceSpace balance_space(void *at, int64_t experts, size_t *bytes)
     BalanceSpace w;
     w.rows = reinterpret_cast<int64_t *>(p + o);
     o += up256(MAX_BLOCKS * 8);
-    w.z = reinterpret_cast<float *>(p + o);
-    o += up256(MAX_BLOCKS * 4);
+    w.z = reinterpret_cast<double *>(p + o);
+    o += up256(MAX_BLOCKS * 8);
     w.prob = reinterpret_cast<float *>(p + o);
     o += up256((size_t)MAX_BLOCKS * experts * 4);
     *bytes = o;
@@ -97,6 +97,13 @@ __device__ __forceinline__ float row_softmax(const T (&row)[NV], const uint32_t 
     return there ? sum : 0.0f;
 }
 
+template <class V> __device__ __forceinline__ V wave_total(V v)
+{
+#pragma unroll
+    for (int d = WAVE / 2; d > 0; d >>= 1) v += __shfl_xor(v, d);
+    return v;
+}
+
 // G lanes share a row and keep their columns' sums over all rows that they see; those of a workgroup meet in LDS in a fixed order.  65536 rows of 100, f32: 9.6 us for
 // 26 MB, of which 856 instructions a wave, four waves to a SIMD, are 6.
 template <class T, int G, int NV>
@@ -104,10 +111,11 @@ __global__ void __launch_bounds__(SUM_TPB) k_balance(const T *logits, int64_t ld
 {
     constexpr int GROUPS = SUM_TPB / G;
     __shared__ float s_prob[GROUPS][NV * G];
-    __shared__ float s_z[GROUPS];
+    __shared__ double s_z[GROUPS];
     __shared__ int s_rows[GROUPS];
     const int sub = lane_id() % G, group = threadIdx.x / G;
-    float prob[NV] = {}, z = 0.0f;
+    float prob[NV] = {};
+    double z = 0.0;
     int rows = 0;
     uint32_t at[NV];
     offsets_of<T, G, NV>(at, group, ld, experts);
@@ -125,7 +133,7 @@ __global__ void __launch_bounds__(SUM_TPB) k_balance(const T *logits, int64_t ld
         const float scale = sum > 0.0f ? 1.0f / sum : 0.0f, lse = sum > 0.0f ? top + logf(sum) : 0.0f;
 #pragma unroll
         for (int i = 0; i < NV; ++i) prob[i] += e[i] * scale;
-        z += lse * lse;
+        z = fma((double)lse, (double)lse, z);
         rows += sum > 0.0f;
 #pragma unroll
         for (int i = 0; i < NV; ++i) now[i] = next[i];
@@ -145,13 +153,13 @@ __global__ void __launch_bounds__(SUM_TPB) k_balance(const T *logits, int64_t ld
     }
     if (threadIdx.x >= SUM_TPB - WAVE) {   // (the last wave, which has no column unless there are many)
         const int lane = lane_id();
-        float v = 0.0f;
+        double v = 0.0;
         uint32_t n = 0;
         for (int i = lane; i < GROUPS; i += WAVE) {
             v += s_z[i];
             n += (uint32_t)s_rows[i];   // (a workgroup has fewer than 2^32 rows)
         }
-        v = wave_sum(v);
+        v = wave_total(v);
         n = wave_sum_u32(n);
         if (lane == 0) {
             w.z[blockIdx.x] = v;
@@ -161,12 +169,6 @@ __global__ void __launch_bounds__(SUM_TPB) k_balance(const T *logits, int64_t ld
 }
 
 __device__ __forceinline__ int64_t entries_of(const int64_t *expert_ptr, int e) { return max(expert_ptr[e + 1] - expert_ptr[e], (int64_t)0); }
-template <class V> __device__ __forceinline__ V wave_total(V v)
-{
-#pragma unroll
-    for (int d = WAVE / 2; d > 0; d >>= 1) v += __shfl_xor(v, d);
-    return v;
-}
 
 // The workgroups' sums together, in 64 bits: 1024 / experts threads an expert, each every so many workgroups.  A chain of two trips to memory and three barriers, 5 to 6 us.
 __global__ void __launch_bounds__(FINISH_TPB) k_balance_finish(const int64_t *expert_ptr, int experts, int blocks, BalanceSpace w, ocean_balance out)
@@ -194,7 +196,7 @@ __global__ void __launch_bounds__(FINISH_TPB) k_balance_finish(const int64_t *ex
         for (int i = 0; i < (int)(MAX_BLOCKS / WAVE); ++i) {
             const int b = i * WAVE + lane_id();
             rows += b < blocks ? w.rows[b] : 0;
-            z += b < blocks ? (double)w.z[b] : 0.0;
+            z += b < blocks ? w.z[b] : 0.0;
         }
         rows = wave_total(rows);
         z = wave_total(z);

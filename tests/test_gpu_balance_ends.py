@@ -35,3 +35,22 @@ def test_a_routing_of_what_is_read(ex):
     bare.expert_ptr = None
     assert lib.ocean_route_balance_backward(ctypes.byref(held), ctypes.byref(bare), x.data_ptr(), 1, 21, g.data_ptr(), None, 1, out.data_ptr(), 21, s) == 0
     assert torch.equal(c.loss, b.loss) and torch.equal(c.counts, b.counts) and torch.equal(c.prob, b.prob) and torch.equal(c.rows, b.rows) and torch.equal(out, d)
+
+
+@pytest.mark.parametrize("E", [1, 5, 100, 700])
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+def test_squares_whose_sum_is_beyond_single_precision(ex, E, dtype):
+    """Logits about 1.5e19: the mean of logsumexp^2, 2.25e38, is a number of single precision, the sum of two of them is not.  A row's logsumexp is its largest logit (the others are
+    further below than exp reaches) or that plus log of how often it is there, which single precision does not tell from it, so the mean is one of exact squares, rounded once; 300
+    additions in 64 bits, or 32, add at most as many roundings."""
+    import torch
+    from paper_2604_19004_amd import routed
+    gen = torch.Generator().manual_seed(E)
+    x = (torch.rand(300, E, generator=gen) * 0.6e19 + 1.2e19).to(getattr(torch, dtype))
+    x[7] = float("-inf")
+    d = x.cuda()
+    b = ex.route_balance(d, routed.route(d, 1))
+    top = np.delete(x.double().amax(1).numpy(), 7)
+    want = float((top ** 2).mean())
+    assert 1.4e38 < want < 3.3e38 and float((top ** 2).sum()) > 1e40
+    assert int(b.rows) == 299 and abs(float(b.loss[1]) - want) <= 302 * 2.0 ** -24 * want
