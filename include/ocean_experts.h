@@ -80,6 +80,7 @@ int ocean_mx4_dequantize(const ocean_mx4 *q, int32_t dtype, void *out, int64_t l
  * w->rows), or y[s] = x[row(s)] * W_e (transposed != 0; x: x_rows x w->rows, y: rows x w->inner), which is the gradient of x's rows.
  * w->count is the groups' `experts`, and its row strides are below 2^23.  The matrices' numbers are taken as they are, x's too: in the type they have, or, float16
  * where the matrices' numbers are beyond it and single precision, as the exact sum of two and three bfloat16 numbers (what is left of a number below 2^-133 is not kept).
+ * Matrix numbers beyond bfloat16 (some of those with s = 253 or 254) count as infinite, times x an infinity or, for a 0, NaN; beside rows in four bits they count as they are.
  * Beside float16 rows, matrices' numbers of scales up to 51 (below 2^-73) may count as 0, also where x is infinite.
  * One launch has fewer than 2^32 threads.  In tiles of 256 x 256 that is 2^23 (16 bits, rows at 16 bytes), of 128 x 128 2^24 (16 bits), of 64 x 64 2^24 (single precision),
  * those that groups' last tiles add among them: what has more is refused.

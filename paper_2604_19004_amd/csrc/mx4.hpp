@@ -52,6 +52,9 @@ template <class T> __device__ __forceinline__ Frag<T> mx4_fragment(uint32_t code
 // 51 count as 0 there: 2^31 products of them with float16 numbers come to less than half its least number.  (255 stays NaN.)
 __device__ __forceinline__ bool mx4_far(uint32_t s) { return (s > 140u && s != 255u) || (s > 51u && s < 104u); }
 
+// Whether bfloat16 has no number for some of this scale's, which are infinite there (4 * 2^126 and on, 2 * 2^127 and on).
+__device__ __forceinline__ bool mx4_infinite(uint32_t s) { return s - 253u < 2u; }
+
 // And back.
 template <class T> __device__ __forceinline__ uint32_t mx4_narrow(const T (&x)[8], float scale)
 {

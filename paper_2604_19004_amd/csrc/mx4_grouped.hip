@@ -3,6 +3,9 @@
 // Every number of four bits is a bfloat16 number, every float16 number the sum of two and every single precision number of three: so all products can be
 // made by the bfloat16 matrix instructions, x in 1, 2 or 3 parts (exactly: single precision at a third of their rate is three times that of its own).  float16 goes
 // through its own as long as it holds the matrix's numbers (mx4_far), and through two parts where it does not.
+//
+// A matrix number that is infinite makes NaN of a part that is 0, which the second and third may be where x is not: results that are NaN are looked at once more (Settle).  All
+// parts of a number have its sign, so a sum that is infinite is right.
 #include "mx4_tiles.hpp"
 
 namespace ocean {
@@ -53,6 +56,55 @@ __device__ __forceinline__ void split_finite(const float (&x)[8], bf16x8 (&out)[
     for (int p = 0; p < 3; ++p) out[p] = __builtin_bit_cast(bf16x8, words[p]);
     if (other != other) split<float>(x, out);
 }
+
+// Results that came out as NaN, of columns for which the matrix has scales of infinite numbers: the sum from the definition in 64 bits where that is infinite.  As slow as it is
+// simple; matrices that mx4_quantize has made have no such scale.
+//
+// The arguments are read anew where they are wanted: kept until here, their registers cost every tile 1 to 2 % (eight groups of 256 rows, 4096 x 4096, float, 300 us and 293).
+struct ProductArgs {
+    GmmArgs a;
+    Mx4Args m;
+};
+__device__ __forceinline__ const ProductArgs &product_args_again()
+{
+    auto p = (const __attribute__((address_space(4))) ProductArgs *)__builtin_amdgcn_kernarg_segment_ptr();   // (a kernel's first two arguments)
+    asm volatile("" : "+s"(p));
+    return *(const ProductArgs *)p;
+}
+template <class T, bool RCOL> struct Settle {
+    int group;
+
+    __device__ __forceinline__ const uint8_t *scale_at(const Mx4Args &m, int64_t line, int64_t number) const { return m.scales + group * m.stride_scales + line * m.ld_scales + number / MX4_BLOCK; }
+    __device__ __forceinline__ bool of_column(int64_t n) const
+    {
+        const ProductArgs &args = product_args_again();
+        const Mx4Args m = args.m;
+        const int64_t depth = args.a.c;
+        bool infinite = false;
+#pragma unroll 8
+        for (int64_t c = 0; c < depth; c += RCOL ? 1 : MX4_BLOCK) infinite |= mx4_infinite(*(RCOL ? scale_at(m, c, n) : scale_at(m, n, c)));
+        return infinite;
+    }
+    __device__ __forceinline__ float result(int slot, int64_t n) const
+    {
+        const ProductArgs &args = product_args_again();
+        const GmmArgs a = args.a;
+        const Mx4Args m = args.m;
+        const int64_t row = a.index ? a.index[slot] : slot;
+        if ((uint64_t)row >= (uint64_t)a.index_rows) return 0.0f;
+        const T *x = static_cast<const T *>(a.l) + row * a.ldl;
+        double sum = 0.0;
+#pragma unroll 1
+        for (int64_t c = 0; c < a.c; ++c) {
+            const int64_t line = RCOL ? c : n, at = RCOL ? n : c;
+            const uint32_t codes = m.codes[group * m.stride_codes + line * m.ld_codes + at / 2];
+            bf16_t e[8];
+            mx4_widen<bf16_t>(codes >> at % 2 * 4, mx4_scale(*scale_at(m, line, at)), e);
+            sum += (double)(float)x[c] * (double)(float)e[0];   // (finite products are below 2^256)
+        }
+        return fabs(sum) == INFINITY ? (float)sum : NAN;
+    }
+};
 
 // Whether a tile has a scale that float16 does not take; every thread calls it.
 template <bool RCOL, int BN, int THREADS> __device__ __forceinline__ bool any_far(const Mx4Args &m, const uint8_t *scales, int n0, int64_t n, int depth)
@@ -316,7 +368,10 @@ __global__ void __launch_bounds__(WAVES_M * WAVES_N * WAVE, 2) k_gmm_mx4(GmmArgs
 #pragma unroll
                 for (int j = 0; j < TN; ++j) acc[i][j] += sums[i][j];
         }
-        store_tile<T, BM, BN, WAVES_M, WAVES_N, !RCOL, sizeof(lds)>(a, w, acc, lds);
+        if constexpr (PARTS > 1 || WIDE)
+            store_tile<T, BM, BN, WAVES_M, WAVES_N, !RCOL, sizeof(lds)>(a, w, acc, lds, Settle<T, RCOL>{w.group});
+        else
+            store_tile<T, BM, BN, WAVES_M, WAVES_N, !RCOL, sizeof(lds)>(a, w, acc, lds);
     };
     if constexpr (HALF) {
         if (any_far<RCOL, BN, THREADS>(m, m.scales + w.group * m.stride_scales, w.n0, a.n, depth)) {
@@ -345,7 +400,12 @@ __global__ void __launch_bounds__(WAVES * WAVE, 2) k_few_mx4(GmmArgs a, Mx4Args 
     for (int j = 0; j < TN; ++j) codes[j] = m.codes + w.group * m.stride_codes + min(w.n0 + j * 16 + r, (int)a.n - 1) * m.ld_codes;
     const int whole = (int)(a.c / 128), steps = (int)((a.c + 127) / 128), rows = min(ROWS, w.hi - w.m0);
     T *out = static_cast<T *>(a.out);
-    auto store = [&](int row, int64_t col, float v) { out[(int64_t)(w.m0 + row) * a.ldo + col] = (T)(s_row[row] < 0 ? 0.0f : v); };
+    bool nan = false;   // (a result of this thread)
+    auto store = [&](int row, int64_t col, float v) {
+        v = s_row[row] < 0 ? 0.0f : v;
+        nan |= v != v;
+        out[(int64_t)(w.m0 + row) * a.ldo + col] = (T)v;
+    };
     auto tile = [&](auto tm) {
         constexpr int TM = decltype(tm)::value, U = TM == 4 || sizeof(T) * TM > 4 ? 1 : sizeof(T) * TM * TN > 4 ? 2 : 4;
         // (on their way while the rows are found)
@@ -443,6 +503,19 @@ __global__ void __launch_bounds__(WAVES * WAVE, 2) k_few_mx4(GmmArgs a, Mx4Args 
     else if constexpr (ROWS >= 32) {
         if (ROWS == 32 || rows <= 32) tile(std::integral_constant<int, 2>{});
         else if constexpr (ROWS == 64) tile(std::integral_constant<int, 4>{});
+    }
+    if constexpr (PARTS > 1) {
+        constexpr int COLS = TN * 16, AT_ONCE = WAVES * WAVE / COLS;
+        static_assert(WAVES * WAVE % COLS == 0 && 16 % AT_ONCE == 0, "a thread stores one column's results");
+        const Settle<T, false> settle{w.group};
+        const int64_t n = w.n0 + threadIdx.x % COLS;
+        if (nan && settle.of_column(n)) {   // (each thread goes through what few_meet had it store)
+#pragma unroll 1
+            for (int row = threadIdx.x / COLS; row < rows; row += AT_ONCE) {
+                T *to = out + (int64_t)(w.m0 + row) * a.ldo + n;
+                if (*to != *to) *to = (T)settle.result(w.m0 + row, n);
+            }
+        }
     }
 }
 

@@ -57,9 +57,10 @@ __device__ __forceinline__ int64_t tile_row(const GmmArgs &a, const RowsTile &w,
 }
 
 // Results pass through LDS, a region for each wave, and leave in whole lines of memory (the largest tiles' past the cache).  INTER: a lane has 16
-// columns of a row side by side, else 4.
-template <class O, int BM, int BN, int WAVES_M, int WAVES_N, bool INTER, size_t LDS>
-__device__ __forceinline__ void store_tile(const GmmArgs &a, const RowsTile &w, const f32x4 (&acc)[BM / WAVES_M / 16][BN / WAVES_N / 16], char *lds)
+// columns of a row side by side, else 4.  settle: of which columns NaN are looked at once more, and what stands in their place (NoSettle: none).
+struct NoSettle {};
+template <class O, int BM, int BN, int WAVES_M, int WAVES_N, bool INTER, size_t LDS, class Settle = NoSettle>
+__device__ __forceinline__ void store_tile(const GmmArgs &a, const RowsTile &w, const f32x4 (&acc)[BM / WAVES_M / 16][BN / WAVES_N / 16], char *lds, Settle settle = {})
 {
     constexpr int WM = BM / WAVES_M, WN = BN / WAVES_N, TM = WM / 16, TN = WN / 16, RUN = INTER ? 4 : 1;
     constexpr int E = PIECE<O>, ROW = WN * (int)sizeof(O), PIECES = ROW / 16, ROWS = WAVE / PIECES;
@@ -89,11 +90,16 @@ __device__ __forceinline__ void store_tile(const GmmArgs &a, const RowsTile &w, 
     }
     wave_sync();
     const int piece = lane % PIECES, col = w.n0 + wn + piece * E, valid = (int)min(a.n - col, (int64_t)E);
+    bool nan = false;   // (a result of this lane)
 #pragma unroll 4
     for (int i = 0; i < WM / ROWS; ++i) {
         const int row = i * ROWS + lane / PIECES, slot = w.m0 + wm + row;
         const auto o = *reinterpret_cast<const Vec<O, E> *>(place(row, piece * E));
         if (slot >= w.hi) continue;
+        if constexpr (!std::is_same<Settle, NoSettle>::value) {
+#pragma unroll
+            for (int k = 0; k < E; ++k) nan |= o.e[k] != o.e[k];
+        }
         O *p = static_cast<O *>(a.out) + (int64_t)slot * a.ldo + col;
         if (valid == E) {
             store_any<PAST>(p, o);
@@ -101,6 +107,19 @@ __device__ __forceinline__ void store_tile(const GmmArgs &a, const RowsTile &w, 
 #pragma unroll
             for (int k = 0; k < E; ++k)
                 if (k < valid) p[k] = o.e[k];
+        }
+    }
+    if constexpr (!std::is_same<Settle, NoSettle>::value) {
+        if (nan) {   // (each lane goes through what it has stored itself)
+#pragma unroll 1
+            for (int k = 0; k < min(valid, E); ++k) {
+                if (!settle.of_column(col + k)) continue;
+#pragma unroll 1
+                for (int slot = w.m0 + wm + lane / PIECES; slot < min(w.m0 + wm + WM, w.hi); slot += ROWS) {
+                    O *p = static_cast<O *>(a.out) + (int64_t)slot * a.ldo + col + k;
+                    if (*p != *p) *p = (O)settle.result(slot, col + k);
+                }
+            }
         }
     }
 }
