@@ -113,3 +113,56 @@ def test_infinite_numbers_of_the_matrix(ex, sizes, K, N, dtype):
         got, ok = _same_ends(ex.grouped_matmul_mx4(x.cuda(), w, _ptr(sizes).cuda(), transposed=across), want)
         assert ok.any() and np.isinf(want).any() and np.isnan(want).any()
         assert np.all(np.abs(got[ok] - want[ok]) <= (TERMS[dtype] * (inner + 2) * 2.0 ** -24 * mag[ok] + EPS[dtype] * np.abs(want[ok]) + TINY[dtype]))
+
+
+@pytest.mark.parametrize("sizes,K,N", SIZES)
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+@pytest.mark.parametrize("low,high,exponent", [(0, 8, 100), (0, 0, 120), (1, 30, 90), (245, 250, -118), (248, 252, -126), (252, 252, -130), (236, 244, -118), (250, 252, -30)])
+def test_products_at_the_ends_of_the_scales(ex, sizes, K, N, dtype, low, high, exponent):
+    """Scales 0 and the next (subnormal numbers of the matrix) with large rows, 236 to 252 with rows whose last parts, or which themselves, are subnormal."""
+    import torch
+    rng = np.random.default_rng(low * 1000 + high + K)
+    w, value = _random(ex, rng, (len(sizes), N, K), low, high)
+    ptr, S = _ptr(sizes).cuda(), sum(sizes)
+    lost = 2.0 ** -133 if dtype == "float32" else 0.0
+    for x, across in ((_rows(rng, (S, K), dtype, exponent), False), (_rows(rng, (S, N), dtype, exponent), True)):
+        want, mag, size = _wanted(sizes, _np(x), value.transpose(0, 2, 1) if across else value)
+        got = _np(ex.grouped_matmul_mx4(x.cuda(), w, ptr, transposed=across))
+        assert np.abs(want).max() < 2.0 ** 127 and np.abs(want).max() > 2.0 ** -60
+        assert np.all(np.abs(got - want) <= TERMS[dtype] * (x.shape[1] + 2) * 2.0 ** -24 * mag + lost * size + EPS[dtype] * np.abs(want) + TINY[dtype])
+
+
+@pytest.mark.parametrize("sizes,K,N", SIZES)
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16", "float16"])
+@pytest.mark.parametrize("rows,matrix", [((0, 0), (250, 250)), ((254, 254), (0, 0)), ((0, 4), (246, 254)), ((246, 254), (0, 4)), ((127, 127), (0, 2)), ((1, 1), (127, 127)),
+                                         ((100, 150), (100, 150))])
+def test_rows_in_four_bits_at_the_ends_of_the_scales(ex, sizes, K, N, dtype, rows, matrix):
+    """Both sides' scales go into the matrix instruction as they are: numbers that no type has meet others that bring them back."""
+    import torch
+    rng = np.random.default_rng(rows[0] * 7 + matrix[0] + K)
+    w, value = _random(ex, rng, (len(sizes), N, K), *matrix)
+    q, rows_value = _random(ex, rng, (sum(sizes), K), *rows)
+    want, mag, _ = _wanted(sizes, rows_value, value)
+    got = _np(ex.grouped_matmul_mx4(q, w, _ptr(sizes).cuda(), dtype=getattr(torch, dtype)))
+    most = float(torch.finfo(getattr(torch, dtype)).max)
+    off = (K + 2) * 2.0 ** -24 * mag
+    ok = np.abs(want) < most / 2
+    assert np.all(np.abs(got[ok] - want[ok]) <= off[ok] + EPS[dtype] * np.abs(want[ok]) + TINY[dtype])
+    # (a sum that is off by less than its size has its sign; one whose terms all but cancel need not)
+    sure = ~ok & (np.abs(want) > off)
+    assert np.array_equal(np.sign(got[sure]), np.sign(want[sure]))
+
+
+def test_float16_rows_at_the_least_scales(ex):
+    """Numbers of scales up to 51 may count as 0 beside float16 rows; from 52 on an infinite row makes infinities of them, and finite ones less than half float16's least number."""
+    import torch
+    rng = np.random.default_rng(5)
+    for sizes, K, N in SIZES:
+        for low in (0, 51, 52):
+            codes, scales = rng.integers(1, 8, (len(sizes), N, (K + 31) // 32 * 32)), np.full((len(sizes), N, (K + 31) // 32), low)
+            w, _ = _made(ex, codes, scales, K)
+            x = _rows(rng, (sum(sizes), K), "float16", 10)
+            x[2, K // 2] = float("-inf")
+            y = _np(ex.grouped_matmul_mx4(x.cuda(), w, _ptr(sizes).cuda()))
+            rest = np.delete(y, 2, 0)
+            assert np.all(np.abs(rest) == 0) and (np.all(y[2] == -np.inf) if low == 52 else np.all(np.isnan(y[2]) | (y[2] == -np.inf)))
