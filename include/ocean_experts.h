@@ -89,8 +89,8 @@ int ocean_grouped_matmul_mx4(const ocean_groups *g, int32_t dtype, const void *x
                              int64_t ld_y, ocean_stream_t stream);
 
 /* The same with x in four bits too (one matrix, x->count == 1, x->rows == x_rows, x->inner == w->inner); y has type dtype.  (Tiles as above, of 256 x 256
- * for results of 16 bits.)  Codes or scales of x that span 4 GB or more and are gathered go 16 rows at a time: there rows / 16 + groups may be up to 65533 and w->rows
- * below 2^27, and more is refused. */
+ * for results of 16 bits.  Where 256 rows of x's codes or scales, or all of them if they are gathered, span 4 GB or more, those of 64 x 64 and 128 x 128.)
+ */
 int ocean_grouped_matmul_mx4_mx4(const ocean_groups *g, const ocean_mx4 *x, const ocean_mx4 *w, int32_t dtype, void *y, int64_t ld_y,
                                  ocean_stream_t stream);
 

@@ -30,7 +30,9 @@ __device__ __forceinline__ u32x4 first_codes(u32x4 v, int valid)
 // bytes of a line at a time (4 bytes a step, each a line of memory looked up, cost more than the codes: 32668 rows of 4096 by eight 8192 x 4096 746 us).
 // There now 650 to 690 us, 3.2 to 3.4 PFLOP/s; matrix cores are busy 43 %, LDS 34 %.  A step is a chain: without its loads it would be a sixth shorter, with a quarter of its
 // products a quarter, and a tile's 16 steps have a beginning and an end that nothing overlaps, as one workgroup fills a compute unit's LDS.
-template <class O, int BM, int BN, int WAVES_M, int WAVES_N, int STAGES>
+// FAR: lines of x by 64-bit addresses, for those that 32-bit offsets do not reach.  There is no range check on that way: pieces behind a line's end are its last one, which
+// end_lines clears as it does the others.
+template <class O, int BM, int BN, int WAVES_M, int WAVES_N, int STAGES, bool FAR>
 __global__ void __launch_bounds__(WAVES_M * WAVES_N * WAVE, 2) k_gmm_mx4_mx4(GmmArgs a, Mx4Args x, Mx4Args m, int nt)
 {
     constexpr int THREADS = WAVES_M * WAVES_N * WAVE, WM = BM / WAVES_M, WN = BN / WAVES_N, TM = WM / 16, TN = WN / 16;
@@ -50,9 +52,11 @@ __global__ void __launch_bounds__(WAVES_M * WAVES_N * WAVE, 2) k_gmm_mx4_mx4(Gmm
 
     const int64_t first = a.index ? 0 : w.m0;
     const Memory l_codes = memory_at(x.codes + first * x.ld_codes), r_codes = memory_at(w_codes + (int64_t)w.n0 * m.ld_codes);
-    uint32_t off_l[TL::LOADS], off_r[TR::LOADS], off_s[SCALE_LOADS];
+    using Off = std::conditional_t<FAR, int64_t, uint32_t>;
+    Off off_l[TL::LOADS], off_s[SCALE_LOADS];   // (FAR: without the piece, which the end of the line decides)
+    uint32_t off_r[TR::LOADS];
 #pragma unroll
-    for (int i = 0; i < TL::LOADS; ++i) off_l[i] = (uint32_t)(tile_row(a, w, TL::line_of(tid, i)) - first) * (uint32_t)x.ld_codes + TL::piece_of(tid, i) * 16;
+    for (int i = 0; i < TL::LOADS; ++i) off_l[i] = (Off)(tile_row(a, w, TL::line_of(tid, i)) - first) * (Off)x.ld_codes + (FAR ? 0 : TL::piece_of(tid, i) * 16);
 #pragma unroll
     for (int i = 0; i < TR::LOADS; ++i) off_r[i] = (uint32_t)min(TR::line_of(tid, i), (int)a.n - 1 - w.n0) * (uint32_t)m.ld_codes + TR::piece_of(tid, i) * 16;
     // (a wave's lines are all of one operand; where there are more threads than lines, some load the same.  The matrix's lie as a wave takes them, 16 side by side: as
@@ -61,7 +65,7 @@ __global__ void __launch_bounds__(WAVES_M * WAVES_N * WAVE, 2) k_gmm_mx4_mx4(Gmm
 #pragma unroll
     for (int i = 0; i < SCALE_LOADS; ++i) {
         const int line = (i * THREADS + tid) % LINES;
-        off_s[i] = line < BM ? (uint32_t)(tile_row(a, w, line) - first) * (uint32_t)x.ld_scales : (uint32_t)min(tile_line<true>((line - BM) / 16, line % 16), (int)a.n - 1 - w.n0) * (uint32_t)m.ld_scales;
+        off_s[i] = line < BM ? (Off)(tile_row(a, w, line) - first) * (Off)x.ld_scales : (Off)min(tile_line<true>((line - BM) / 16, line % 16), (int)a.n - 1 - w.n0) * (Off)m.ld_scales;
     }
     // (the order of the steps is that of k_gmm_mx4, by periods)
     const int whole = (int)(a.c / (STEP_BLOCKS * MX4_BLOCK)), periods = whole / 2, turn = periods == 0 ? 0 : (w.n0 / BN + w.group * 5) % periods;
@@ -75,12 +79,16 @@ __global__ void __launch_bounds__(WAVES_M * WAVES_N * WAVE, 2) k_gmm_mx4_mx4(Gmm
 #pragma unroll
             for (int i = 0; i < SCALE_LOADS; ++i) {
                 const int line = (i * THREADS + wave * WAVE) % LINES;
-                memory_to_lds<16>(memory_at(line < BM ? l_scales : r_scales), off_s[i], p * PERIOD_BLOCKS, reinterpret_cast<char *>(s_scales[t_ / 2 % PERIODS][line]));
+                char *const scales = reinterpret_cast<char *>(s_scales[t_ / 2 % PERIODS][line]);
+                if constexpr (FAR) load_to_lds((line < BM ? l_scales : r_scales) + off_s[i] + p * PERIOD_BLOCKS, scales);
+                else memory_to_lds<16>(memory_at(line < BM ? l_scales : r_scales), off_s[i], p * PERIOD_BLOCKS, scales);
             }
         }
 #pragma unroll
-        for (int i = TL::LOADS * PART / PARTS; i < TL::LOADS * (PART + 1) / PARTS; ++i)
-            memory_to_lds<16>(l_codes, TL::piece_of(tid, i) * 16 < left ? off_l[i] : NOWHERE, t * LINE, to + i * THREADS * 16);
+        for (int i = TL::LOADS * PART / PARTS; i < TL::LOADS * (PART + 1) / PARTS; ++i) {
+            if constexpr (FAR) load_to_lds(x.codes + first * x.ld_codes + off_l[i] + min(t * LINE + TL::piece_of(tid, i) * 16, depth - 16), to + i * THREADS * 16);
+            else memory_to_lds<16>(l_codes, TL::piece_of(tid, i) * 16 < left ? off_l[i] : NOWHERE, t * LINE, to + i * THREADS * 16);
+        }
 #pragma unroll
         for (int i = TR::LOADS * PART / PARTS; i < TR::LOADS * (PART + 1) / PARTS; ++i)
             memory_to_lds<16>(r_codes, TR::piece_of(tid, i) * 16 < left ? off_r[i] : NOWHERE, t * LINE, to + TL::BYTES + i * THREADS * 16);
@@ -234,32 +242,30 @@ __global__ void __launch_bounds__(WAVES * WAVE, 2) k_few_mx4_mx4(GmmArgs a, Mx4A
     });
 }
 
-template <class O, int BM, int BN, int WAVES_M, int WAVES_N, int STAGES> hipError_t launch_tile(const GmmArgs &a, const Mx4Args &x, const Mx4Args &m, hipStream_t s)
+template <class O, int BM, int BN, int WAVES_M, int WAVES_N, int STAGES, bool FAR = false> hipError_t launch_tile(const GmmArgs &a, const Mx4Args &x, const Mx4Args &m, hipStream_t s)
 {
     const Grid g = grid_of<GM_ROWS>(a, BM, BN);
     constexpr int threads = WAVES_M * WAVES_N * WAVE;
     if (g.blocks * threads >= (1ll << 32)) return TOO_MANY_TILES;
-    hipLaunchKernelGGL((k_gmm_mx4_mx4<O, BM, BN, WAVES_M, WAVES_N, STAGES>), dim3((uint32_t)g.blocks), dim3(threads), 0, s, a, x, m, (int)g.nt);
+    hipLaunchKernelGGL((k_gmm_mx4_mx4<O, BM, BN, WAVES_M, WAVES_N, STAGES, FAR>), dim3((uint32_t)g.blocks), dim3(threads), 0, s, a, x, m, (int)g.nt);
     return hipGetLastError();
 }
 
 template <class O> hipError_t pick(const GmmArgs &a, const Mx4Args &x, const Mx4Args &m, hipStream_t s)
 {
-    // Up to 12 rows a group by themselves (us here and in tiles: 16 groups of 6 rows, 4096 x 4096, 25 and 28, eight of 8 15 and 16, of 16 19 and 16), and what
-    // tiles do not reach: 256 lines of the matrix and the rows of x that they gather, by 32-bit offsets.
+    // Up to 12 rows a group by themselves (us here and in tiles: 16 groups of 6 rows, 4096 x 4096, 25 and 28, eight of 8 15 and 16, of 16 19 and 16).
     const int64_t groups = std::min(a.groups, a.rows);
-    const bool reached = offsets_fit(a.index ? std::max<int64_t>(a.index_rows, 256) : 256, std::max(x.ld_codes, x.ld_scales), 1);
-    const bool few = groups > 0 && a.rows <= groups * 12 && a.n <= (1 << 20) && a.rows / 16 + groups < 65535;
-    if (few || !reached)
+    if (groups > 0 && a.rows <= groups * 12 && a.n <= (1 << 20) && a.rows / 16 + groups < 65535)
         return with_columns_and_waves(a, [&](auto tn, auto waves) {
             constexpr int TN = decltype(tn)::value, WAVES = decltype(waves)::value;
-            const dim3 grid = few_grid(a, 16, TN * 16);
-            if (grid.x >= 1u << 22 || grid.y > 65535u) return TOO_MANY_TILES;
-            hipLaunchKernelGGL((k_few_mx4_mx4<O, TN, WAVES>), grid, dim3(WAVES * WAVE), 0, s, a, x, m);
+            hipLaunchKernelGGL((k_few_mx4_mx4<O, TN, WAVES>), few_grid(a, 16, TN * 16), dim3(WAVES * WAVE), 0, s, a, x, m);
             return hipGetLastError();
         });
     constexpr TileTimes TIMES = {12.5, 3.5, 0.0248, 26, 19.5, 41, 32};
-    const int lines = pick_lines(a, TIMES, sizeof(O) == 2);   // (results of 32 bits do not fit the operands' place in LDS)
+    // (32-bit offsets reach 4 GB: 256 lines side by side, or all of x where its rows are gathered)
+    const bool far = !offsets_fit(a.index ? std::max<int64_t>(a.index_rows, 256) : 256, std::max(x.ld_codes, x.ld_scales), 1);
+    const int lines = pick_lines(a, TIMES, sizeof(O) == 2 && !far);   // (results of 32 bits do not fit the operands' place in LDS)
+    if (far) return lines == 64 ? launch_tile<O, 64, 64, 4, 1, 4, true>(a, x, m, s) : launch_tile<O, 128, 128, 2, 2, 2, true>(a, x, m, s);
     if (lines == 64) return launch_tile<O, 64, 64, 4, 1, 4>(a, x, m, s);
     if constexpr (sizeof(O) == 2)
         if (lines == 256) return launch_tile<O, 256, 256, 2, 4, 2>(a, x, m, s);
