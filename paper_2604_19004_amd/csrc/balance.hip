@@ -104,8 +104,8 @@ template <class V> __device__ __forceinline__ V wave_total(V v)
     return v;
 }
 
-// G lanes share a row and keep their columns' sums over all rows that they see; those of a workgroup meet in LDS in a fixed order.  65536 rows of 100, f32: 9.6 us for
-// 26 MB, of which 856 instructions a wave, four waves to a SIMD, are 6.
+// G lanes share a row and keep their columns' sums over all rows that they see; those of a workgroup meet in LDS in a fixed order.  65536 rows of 100, f32: 9.5 us for
+// 26 MB, of which 870 instructions a wave, four waves to a SIMD, are 6.
 template <class T, int G, int NV>
 __global__ void __launch_bounds__(SUM_TPB) k_balance(const T *logits, int64_t ld, int64_t tokens, int experts, BalanceSpace w)
 {
@@ -228,7 +228,8 @@ __global__ void __launch_bounds__(FINISH_TPB) k_balance_finish(const int64_t *ex
 }
 
 // dl_c = p_c (a (f_c - sum f p) + b lse) with f the experts' shares of the entries, a = dloss[0] experts / rows and b = 2 dloss[1] / rows; with `dval` what
-// k_route_backward gives beside it.  65536 rows of 100, k 8, f32: 21 us for 59 MB (4.9 at the rate of a copy would be 12); 1315 instructions a wave are 12 of them.
+// k_route_backward gives beside it.  65536 rows of 100, k 8, f32: 19 us for 59 MB (12 at the rate of a copy); 1315 instructions a wave are 12 of
+// them.  Without dval 14.5 us for 52 MB.
 template <class T, int G, int NV, bool WEIGHTS>
 __global__ void __launch_bounds__(TPB) k_balance_backward(ocean_balance b, ocean_routing r, const float *dloss, const float *dval, const T *logits,
                                                           int64_t ld, int normalize, T *dlogits, int64_t ldd)
