@@ -58,7 +58,8 @@ __device__ __forceinline__ void split_finite(const float (&x)[8], bf16x8 (&out)[
 }
 
 // Results that came out as NaN, of columns for which the matrix has scales of infinite numbers: the sum from the definition in 64 bits where that is infinite.  As slow as it is
-// simple; matrices that mx4_quantize has made have no such scale.
+// simple (512 rows of ones by two 1024 x 1024 of nothing else, 1.0 ms); matrices that mx4_quantize has made have no such scale, and looking for one is what a NaN costs there (8000 rows of
+// NaN, single precision, across 8192 x 4096: 3.7 ms, with what the other way of split takes).
 //
 // The arguments are read anew where they are wanted: kept until here, their registers cost every tile 1 to 2 % (eight groups of 256 rows, 4096 x 4096, float, 300 us and 293).
 struct ProductArgs {
@@ -75,14 +76,32 @@ template <class T, bool RCOL> struct Settle {
     int group;
 
     __device__ __forceinline__ const uint8_t *scale_at(const Mx4Args &m, int64_t line, int64_t number) const { return m.scales + group * m.stride_scales + line * m.ld_scales + number / MX4_BLOCK; }
-    __device__ __forceinline__ bool of_column(int64_t n) const
+    // (RCOL: bit i, whether the i-th block of the WN columns from `first` on has such a scale in any line, 64 lines at a time; all lanes of the wave)
+    template <int WN> __device__ __forceinline__ uint32_t of_wave(int first) const
     {
+        uint32_t mine = 0, all = 0;
+        if constexpr (RCOL) {
+            const ProductArgs &args = product_args_again();
+            const Mx4Args m = args.m;
+            const int64_t depth = args.a.c;
+#pragma unroll 2
+            for (int64_t c = lane_id(); c < depth; c += WAVE)
+#pragma unroll
+                for (int i = 0; i < WN / MX4_BLOCK; ++i) mine |= (uint32_t)mx4_infinite(*scale_at(m, c, min(first / MX4_BLOCK + i, m.blocks - 1) * (int64_t)MX4_BLOCK)) << i;
+#pragma unroll
+            for (int i = 0; i < WN / MX4_BLOCK; ++i) all |= (uint32_t)(__any(mine >> i & 1u) != 0) << i;
+        }
+        return all;
+    }
+    __device__ __forceinline__ bool of_column(int64_t n, int first = 0, uint32_t blocks = 0) const
+    {
+        if constexpr (RCOL) return blocks >> (n - first) / MX4_BLOCK & 1u;
         const ProductArgs &args = product_args_again();
         const Mx4Args m = args.m;
         const int64_t depth = args.a.c;
         bool infinite = false;
 #pragma unroll 8
-        for (int64_t c = 0; c < depth; c += RCOL ? 1 : MX4_BLOCK) infinite |= mx4_infinite(*(RCOL ? scale_at(m, c, n) : scale_at(m, n, c)));
+        for (int64_t c = 0; c < depth; c += MX4_BLOCK) infinite |= mx4_infinite(*scale_at(m, n, c));
         return infinite;
     }
     __device__ __forceinline__ float result(int slot, int64_t n) const
@@ -93,8 +112,9 @@ template <class T, bool RCOL> struct Settle {
         const int64_t row = a.index ? a.index[slot] : slot;
         if ((uint64_t)row >= (uint64_t)a.index_rows) return 0.0f;
         const T *x = static_cast<const T *>(a.l) + row * a.ldl;
+        constexpr int AT_ONCE = RCOL ? 2 : 4;   // (more spill in tiles of 256 x 256 across)
         double sum = 0.0;
-#pragma unroll 1
+#pragma unroll AT_ONCE
         for (int64_t c = 0; c < a.c; ++c) {
             const int64_t line = RCOL ? c : n, at = RCOL ? n : c;
             const uint32_t codes = m.codes[group * m.stride_codes + line * m.ld_codes + at / 2];

@@ -110,10 +110,11 @@ __device__ __forceinline__ void store_tile(const GmmArgs &a, const RowsTile &w, 
         }
     }
     if constexpr (!std::is_same<Settle, NoSettle>::value) {
-        if (nan) {   // (each lane goes through what it has stored itself)
+        if (__any(nan)) {
+            const uint32_t blocks = settle.template of_wave<WN>(w.n0 + wn);
 #pragma unroll 1
-            for (int k = 0; k < min(valid, E); ++k) {
-                if (!settle.of_column(col + k)) continue;
+            for (int k = 0; k < (nan ? min(valid, E) : 0); ++k) {   // (each lane goes through what it has stored itself)
+                if (!settle.of_column(col + k, w.n0 + wn, blocks)) continue;
 #pragma unroll 1
                 for (int slot = w.m0 + wm + lane / PIECES; slot < min(w.m0 + wm + WM, w.hi); slot += ROWS) {
                     O *p = static_cast<O *>(a.out) + (int64_t)slot * a.ldo + col + k;
