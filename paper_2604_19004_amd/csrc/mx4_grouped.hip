@@ -66,6 +66,7 @@ struct ProductArgs {
     GmmArgs a;
     Mx4Args m;
 };
+static_assert(alignof(GmmArgs) == alignof(Mx4Args) && sizeof(ProductArgs) == sizeof(GmmArgs) + sizeof(Mx4Args), "as a kernel's arguments lie");
 __device__ __forceinline__ const ProductArgs &product_args_again()
 {
     auto p = (const __attribute__((address_space(4))) ProductArgs *)__builtin_amdgcn_kernarg_segment_ptr();   // (a kernel's first two arguments)
